@@ -48,7 +48,7 @@ enum {
   SIF_E_DEVICE = -6     /* a HIP call failed; text in sif_last_error() */
 };
 
-enum { SIF_F32 = 0, SIF_BF16 = 1 };
+enum { SIF_F32 = 0, SIF_BF16 = 1, SIF_E4M3 = 2 /* 8 bits: 4 of exponent, 3 of mantissa, finite up to 448, no infinities */ };
 enum { SIF_STATUS_BUSY = 0, SIF_STATUS_IDLE = 1 };
 
 const char* sif_last_error(void);
@@ -298,6 +298,124 @@ sif_status sif_k_attn_fwd_varlen(const void* qkv_dev, void* o_dev, const uint32_
 sif_status sif_k_attn_bwd(const void* qkv_dev, const void* o_dev, const void* d_o_dev, const float* lse_dev, float* delta_dev,
                           void* dqkv_dev, uint32_t batch, uint32_t seq, uint32_t heads, uint32_t d_head, uint32_t ld_qkv,
                           uint32_t ld_o, uint32_t ld_dqkv, uint32_t causal, void* stream);
+
+/* --- Attention with a sliding window and sinks ------------------------------------------------------------------
+ * Query t of a sequence stands at position p = t + seq_k - seq_q (the queries are the last ones of the keys' sequence).
+ * It sees key j iff  j <= p  and  (window = 0  or  p - j < window  or  j < sinks):  the `window` newest keys, itself
+ * among them, and the first `sinks` keys, the latter for good.  window = 0: no limit (a causal mask).
+ *   o = softmax(scale q k^T over the visible keys) v,   lse = log sum exp of the visible scaled scores (natural log)
+ * A query that sees no key (seq_q > seq_k) gets o = 0, lse = -inf and passes no gradient on.  What stands in keys that no query sees
+ * has no influence, whatever it is.
+ * Query head h reads key/value head h / (heads / kv_heads).  bf16 operands, fp32 sums and softmax; the probabilities
+ * (and, backward, their gradients) are rounded to bf16 as operands of the matrix units, once. */
+typedef struct sif_window_attn_args {
+  uint32_t struct_size;
+  uint32_t heads, kv_heads, d_head;   /* heads a multiple of kv_heads; d_head 64 or 128                              */
+  uint32_t batch, seq_q, seq_k;       /* sequence b has the query rows b*seq_q .. and the key rows b*seq_k ..; both >= 1 */
+  uint32_t window;                    /* 0 = no limit                                                                */
+  uint32_t sinks;                     /* at most 128                                                                 */
+  float scale;                        /* 0 = 1 / sqrt(d_head)                                                        */
+  uint32_t ld_q, ld_k, ld_v, ld_o;    /* elements from a row to the next, multiples of 8; head h in columns h*d_head .. */
+  uint32_t ld_do, ld_dq, ld_dk, ld_dv;
+  uint32_t rows;                      /* with starts_dev: rows of all tensors                                        */
+  uint32_t reserved;
+  const void* q_dev; const void* k_dev; const void* v_dev;   /* bf16                                                 */
+  void* o_dev;                        /* bf16; written by forward, read by backward                                   */
+  float* lse_dev;                     /* fp32 [heads][query rows]; written by forward (null: not kept), read by backward */
+  const int32_t* starts_dev;          /* null, or [batch + 1] ascending: sequence b has the rows starts[b] .. starts[b+1] - 1 of
+                                         queries and keys alike (it may be empty).  seq_q = seq_k = the most rows a sequence
+                                         has: of a longer one only the first seq_q rows exist.  Rows of no sequence are
+                                         neither read nor written.  Numbers outside 0 .. rows are taken as the nearest one */
+  const void* do_dev;                 /* backward: gradient of o, bf16                                                */
+  void* dq_dev; void* dk_dev; void* dv_dev;   /* backward: results, bf16, overwritten                                */
+  void* workspace_dev; uint64_t workspace_bytes;   /* backward: 256-byte aligned scratch, not shared by calls that may overlap */
+} sif_window_attn_args;
+
+sif_status sif_k_window_attn_fwd(const sif_window_attn_args* a, void* stream);
+/* Gradients of the forward pass that wrote o and lse.  Several launches, no atomics: the same bits every time. */
+sif_status sif_k_window_attn_bwd(const sif_window_attn_args* a, void* stream);
+uint64_t sif_window_attn_bwd_workspace_bytes(const sif_window_attn_args* a);    /* 0: refused, see sif_last_error() */
+
+/* --- A paged key-value cache -------------------------------------------------------------------------------------
+ * Pages of page_tokens tokens, for all layers at once: page p of layer l holds keys as [kv_head][token][d_head] and
+ * values as [kv_head][d_head][token], so that the matrix units take both as they lie.  Sequence s holds the pages
+ * table[s][0 .. ceil(lengths[s] / page_tokens) - 1], every other entry of its row is -1; a page may belong to several sequences,
+ * refs[p] says to how many; refs[p] = 0 is a free page.  The caller owns all of it; the operations below keep it in
+ * order on the device, in stream order, without a host synchronisation (they can be captured into a graph).  All of
+ * them give the same result every time: pages are taken lowest number first, in the order in which sequences are listed.
+ * Two operations on one cache must not overlap.
+ * Lists: seqs_dev names n sequences (int32; null = 0 .. n-1).  A sequence number outside 0 .. n_seqs-1, and a
+ * sequence that was listed before in the same call, is left out.  status_dev (int32 [n], may be null) receives SIF_OK
+ * or what was wrong with an entry; an entry in error changes nothing.  A page number outside 0 .. n_pages-1 in a table row
+ * stands for no page.  The page operations take n from 1 to 1024. */
+typedef struct sif_kv_cache {
+  uint32_t struct_size;
+  uint32_t dtype;                     /* SIF_BF16 or SIF_E4M3                                                        */
+  uint32_t layers, kv_heads, d_head;  /* d_head 64 or 128                                                            */
+  uint32_t page_tokens;               /* 16, 32, 64, 128 or 256                                                      */
+  uint32_t n_pages, n_seqs, table_ld; /* n_pages at most 2^21; table_ld: pages that a row of the table holds           */
+  uint32_t reserved;
+  void* k_dev;                        /* [layers][n_pages][kv_heads][page_tokens][d_head], 16-byte aligned             */
+  void* v_dev;                        /* [layers][n_pages][kv_heads][d_head][page_tokens], 16-byte aligned             */
+  const float* k_scale_dev;           /* SIF_E4M3: [layers][kv_heads], a key is what is held times its scale (null = 1) */
+  const float* v_scale_dev;
+  int32_t* table_dev;                 /* [n_seqs][table_ld]                                                          */
+  int32_t* lengths_dev;               /* [n_seqs] tokens                                                             */
+  int32_t* refs_dev;                  /* [n_pages], 16-byte aligned                                                  */
+} sif_kv_cache;
+
+/* Scratch of sif_k_kv_extend and sif_k_kv_compact, 256-byte aligned. */
+uint64_t sif_kv_workspace_bytes(const sif_kv_cache* c);
+/* Empties the cache: all table entries -1, all lengths and reference counts 0.  (The pages' contents stay.) */
+sif_status sif_k_kv_reset(const sif_kv_cache* c, void* stream);
+/* Makes room for counts[i] more tokens in sequence i of the list (counts_dev null = 1 each) and lengthens it by them.  New pages
+ * are the lowest free ones.  A last page that is not full and that other sequences hold too (as refs stood before the
+ * call) is copied, in all layers, and the copy takes its place.  Status: SIF_E_INVAL for a negative count, a row too short for the
+ * pages, or a last page that is none; SIF_E_NOMEM where the free pages do not suffice for this entry and those before it. */
+sif_status sif_k_kv_extend(const sif_kv_cache* c, const int32_t* seqs_dev, const int32_t* counts_dev, uint32_t n, int32_t* status_dev,
+                           void* workspace_dev, uint64_t workspace_bytes, void* stream);
+/* Writes the newest tokens' keys and values (bf16 rows of kv_heads * d_head, ld_k / ld_v elements apart) of one layer.
+ * Rows starts[i] .. starts[i+1] - 1 (starts_dev int32 [n+1], ascending, within 0 .. rows) are the last tokens of sequence i of the
+ * list; starts_dev null: one row each, rows = n.  In SIF_E4M3 a value is divided by its scale, held at +-448 and rounded to
+ * nearest even (NaN stays NaN).  A token that has no page is left out. */
+sif_status sif_k_kv_write(const sif_kv_cache* c, uint32_t layer, const void* k_dev, const void* v_dev, uint32_t ld_k, uint32_t ld_v,
+                          const int32_t* seqs_dev, const int32_t* starts_dev, uint32_t n, uint32_t rows, void* stream);
+/* Sequence dst[i] becomes a copy of src[i] and shares its pages.  Status SIF_E_INVAL: a number outside the table, a dst that is
+ * not empty or was listed before, a src that is listed as a dst. */
+sif_status sif_k_kv_fork(const sif_kv_cache* c, const int32_t* src_dev, const int32_t* dst_dev, uint32_t n, int32_t* status_dev, void* stream);
+/* Empties the listed sequences; pages that no sequence holds any more are free. */
+sif_status sif_k_kv_free(const sif_kv_cache* c, const int32_t* seqs_dev, uint32_t n, void* stream);
+/* Gives up the listed sequences' pages that hold neither one of the first `sinks` tokens nor one of the `window` newest (window
+ * >= 1): their entries become -1, lengths stay.  Attention with this window and these sinks does not miss them. */
+sif_status sif_k_kv_trim(const sif_kv_cache* c, const int32_t* seqs_dev, uint32_t n, uint32_t window, uint32_t sinks, void* stream);
+/* Moves pages so that the used ones are 0 .. (their number)-1: the used pages above that, in ascending order, go to the free ones below,
+ * in ascending order, in all layers; table and refs follow. */
+sif_status sif_k_kv_compact(const sif_kv_cache* c, void* workspace_dev, uint64_t workspace_bytes, void* stream);
+/* Copies the contents of page src[i] to page dst[i] in all layers; table and refs stay.  Status SIF_E_INVAL: a number outside the
+ * pool, a dst that was listed before, a src that is listed as a dst. */
+sif_status sif_k_kv_copy_pages(const sif_kv_cache* c, const int32_t* src_dev, const int32_t* dst_dev, uint32_t n, int32_t* status_dev, void* stream);
+
+/* --- Attention of one new token per sequence over a paged cache ---------------------------------------------------
+ * The query of sequence i of the list stands at its last position, lengths - 1 (its key and value are in the cache); mask,
+ * softmax and heads as in sif_k_window_attn_fwd.  Tokens without a page, and tokens past the row of the table, are not visible.  A
+ * sequence that sees nothing (empty, or a number outside the table) gets o = 0, lse = -inf.  A sequence may be listed more than once. */
+typedef struct sif_attn_decode_args {
+  uint32_t struct_size;
+  uint32_t layer, n, heads;           /* n >= 1 sequences; heads a multiple of the cache's kv_heads                    */
+  uint32_t window, sinks;             /* window 0 = no limit; any number of sinks                                    */
+  uint32_t max_tokens;                /* what the longest listed sequence is expected to hold (0: a whole row of the table).  Only the
+                                         division of the work depends on it: a longer sequence is computed all the same */
+  float scale;                        /* 0 = 1 / sqrt(d_head)                                                        */
+  uint32_t ld_q, ld_o;                /* elements from a sequence's row to the next, multiples of 8; rows of heads * d_head */
+  const int32_t* seqs_dev;            /* [n], or null = 0 .. n-1                                                     */
+  const void* q_dev;                  /* bf16                                                                        */
+  void* o_dev;                        /* bf16                                                                        */
+  float* lse_dev;                     /* fp32 [n][heads], or null                                                    */
+  void* workspace_dev; uint64_t workspace_bytes;   /* 256-byte aligned scratch, not shared by calls that may overlap    */
+} sif_attn_decode_args;
+
+uint64_t sif_attn_decode_workspace_bytes(const sif_kv_cache* c, const sif_attn_decode_args* a);   /* 0: refused, see sif_last_error() */
+sif_status sif_k_attn_decode(const sif_kv_cache* c, const sif_attn_decode_args* a, void* stream);
 
 /* x[t,:] = wte[ids[t],:] + wpe[t % seq,:]   (bf16).  wte has `vocab` rows; an id outside [0, vocab) is taken as the
  * nearest valid one (here and in every kernel that indexes a table with caller data: embedding backward, the targets

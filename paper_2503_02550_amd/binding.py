@@ -20,7 +20,7 @@ u32, u64, i32, i64, f32, vp = C.c_uint32, C.c_uint64, C.c_int32, C.c_int64, C.c_
 # status codes / enums (mirrors of the header)
 SIF_OK, SIF_W_SLO_RISK = 0, 1
 SIF_E_INVAL, SIF_E_NOMEM, SIF_E_AGAIN, SIF_E_CANCELLED, SIF_E_TIMEOUT, SIF_E_DEVICE = -1, -2, -3, -4, -5, -6
-SIF_F32, SIF_BF16 = 0, 1
+SIF_F32, SIF_BF16, SIF_E4M3 = 0, 1, 2
 SIF_STATUS_BUSY, SIF_STATUS_IDLE = 0, 1
 SIF_A_ROW_K, SIF_A_ROW_M = 0, 1
 SIF_B_ROW_K, SIF_B_ROW_N = 0, 1
@@ -590,3 +590,168 @@ def sif_k_attn_fwd_varlen(qkv, o, seq_starts, heads, d_head, ld_qkv, ld_o, causa
 def sif_k_attn_bwd(qkv, o, d_o, lse, delta, dqkv, batch, seq, heads, d_head, ld_qkv, ld_o, ld_dqkv, causal, stream=None):
     return check(lib.sif_k_attn_bwd(ptr(qkv), ptr(o), ptr(d_o), ptr(lse), ptr(delta), ptr(dqkv), batch, seq, heads, d_head, ld_qkv, ld_o,
                                     ld_dqkv, causal, stream_ptr(stream)))
+
+
+# ---- attention with a window and sinks; a paged cache, its page operations and attention over it ------------------------
+class sif_window_attn_args(C.Structure):
+    _fields_ = [("struct_size", u32), ("heads", u32), ("kv_heads", u32), ("d_head", u32), ("batch", u32), ("seq_q", u32), ("seq_k", u32),
+                ("window", u32), ("sinks", u32), ("scale", f32), ("ld_q", u32), ("ld_k", u32), ("ld_v", u32), ("ld_o", u32),
+                ("ld_do", u32), ("ld_dq", u32), ("ld_dk", u32), ("ld_dv", u32), ("rows", u32), ("reserved", u32),
+                ("q_dev", vp), ("k_dev", vp), ("v_dev", vp), ("o_dev", vp), ("lse_dev", vp), ("starts_dev", vp),
+                ("do_dev", vp), ("dq_dev", vp), ("dk_dev", vp), ("dv_dev", vp), ("workspace_dev", vp), ("workspace_bytes", u64)]
+
+
+class sif_kv_cache(C.Structure):
+    _fields_ = [("struct_size", u32), ("dtype", u32), ("layers", u32), ("kv_heads", u32), ("d_head", u32), ("page_tokens", u32),
+                ("n_pages", u32), ("n_seqs", u32), ("table_ld", u32), ("reserved", u32),
+                ("k_dev", vp), ("v_dev", vp), ("k_scale_dev", vp), ("v_scale_dev", vp), ("table_dev", vp), ("lengths_dev", vp), ("refs_dev", vp)]
+
+
+class sif_attn_decode_args(C.Structure):
+    _fields_ = [("struct_size", u32), ("layer", u32), ("n", u32), ("heads", u32), ("window", u32), ("sinks", u32), ("max_tokens", u32),
+                ("scale", f32), ("ld_q", u32), ("ld_o", u32), ("seqs_dev", vp), ("q_dev", vp), ("o_dev", vp), ("lse_dev", vp),
+                ("workspace_dev", vp), ("workspace_bytes", u64)]
+
+
+_sig("sif_k_window_attn_fwd", i32, P(sif_window_attn_args), vp)
+_sig("sif_k_window_attn_bwd", i32, P(sif_window_attn_args), vp)
+_sig("sif_window_attn_bwd_workspace_bytes", u64, P(sif_window_attn_args))
+_sig("sif_kv_workspace_bytes", u64, P(sif_kv_cache))
+_sig("sif_k_kv_reset", i32, P(sif_kv_cache), vp)
+_sig("sif_k_kv_extend", i32, P(sif_kv_cache), vp, vp, u32, vp, vp, u64, vp)
+_sig("sif_k_kv_write", i32, P(sif_kv_cache), u32, vp, vp, u32, u32, vp, vp, u32, u32, vp)
+_sig("sif_k_kv_fork", i32, P(sif_kv_cache), vp, vp, u32, vp, vp)
+_sig("sif_k_kv_free", i32, P(sif_kv_cache), vp, u32, vp)
+_sig("sif_k_kv_trim", i32, P(sif_kv_cache), vp, u32, u32, u32, vp)
+_sig("sif_k_kv_compact", i32, P(sif_kv_cache), vp, u64, vp)
+_sig("sif_k_kv_copy_pages", i32, P(sif_kv_cache), vp, vp, u32, vp, vp)
+_sig("sif_attn_decode_workspace_bytes", u64, P(sif_kv_cache), P(sif_attn_decode_args))
+_sig("sif_k_attn_decode", i32, P(sif_kv_cache), P(sif_attn_decode_args), vp)
+
+
+def _ld(t, given, width):
+    """Elements from a row to the next: as given, a two-dimensional tensor's own, or the rows' width."""
+    if given is not None:
+        return given
+    return t.stride(0) if hasattr(t, "stride") and t.dim() == 2 else width
+
+
+def window_attn_args(q, k, v, o, heads, kv_heads, d_head, batch, seq_q, seq_k, window, sinks, lse=None, starts=None, rows=0, scale=0.0,
+                     d_o=None, dq=None, dk=None, dv=None, workspace=None, workspace_bytes=0, ld_q=None, ld_k=None, ld_v=None, ld_o=None,
+                     ld_do=None, ld_dq=None, ld_dk=None, ld_dv=None):
+    """A filled sif_window_attn_args (argument marshalling only: the tensors stay the caller's to keep)."""
+    a = sif_window_attn_args()
+    a.struct_size = C.sizeof(sif_window_attn_args)
+    a.heads, a.kv_heads, a.d_head, a.batch, a.seq_q, a.seq_k = heads, kv_heads, d_head, batch, seq_q, seq_k
+    a.window, a.sinks, a.scale, a.rows = window, sinks, scale, rows
+    wq, wk = heads * d_head, kv_heads * d_head
+    a.ld_q, a.ld_k, a.ld_v, a.ld_o = _ld(q, ld_q, wq), _ld(k, ld_k, wk), _ld(v, ld_v, wk), _ld(o, ld_o, wq)
+    a.ld_do, a.ld_dq, a.ld_dk, a.ld_dv = _ld(d_o, ld_do, wq), _ld(dq, ld_dq, wq), _ld(dk, ld_dk, wk), _ld(dv, ld_dv, wk)
+    a.q_dev, a.k_dev, a.v_dev, a.o_dev, a.lse_dev, a.starts_dev = ptr(q), ptr(k), ptr(v), ptr(o), ptr(lse), ptr(starts)
+    a.do_dev, a.dq_dev, a.dk_dev, a.dv_dev = ptr(d_o), ptr(dq), ptr(dk), ptr(dv)
+    set_workspace(a, workspace, workspace_bytes)
+    return a
+
+
+def set_workspace(a, workspace, workspace_bytes):
+    """Puts a workspace into a filled argument structure."""
+    a.workspace_dev, a.workspace_bytes = ptr(workspace), workspace_bytes
+
+
+def sif_window_attn_bwd_workspace_bytes(a):
+    n = lib.sif_window_attn_bwd_workspace_bytes(C.byref(a))
+    if n == 0:
+        raise SifError(SIF_E_INVAL, last_error())
+    return n
+
+
+def sif_k_window_attn_fwd(a, stream=None):
+    return check(lib.sif_k_window_attn_fwd(C.byref(a), stream_ptr(stream)))
+
+
+def sif_k_window_attn_bwd(a, stream=None):
+    return check(lib.sif_k_window_attn_bwd(C.byref(a), stream_ptr(stream)))
+
+
+def kv_cache(k, v, table, lengths, refs, dtype, page_tokens, k_scale=None, v_scale=None):
+    """A filled sif_kv_cache for k [layers][pages][kv_heads][page_tokens][d_head], v [layers][pages][kv_heads][d_head][page_tokens],
+    table [sequences][pages of a row], lengths [sequences] and refs [pages] (the tensors stay the caller's to keep)."""
+    c = sif_kv_cache()
+    c.struct_size = C.sizeof(sif_kv_cache)
+    layers, n_pages, kv_heads, d_head = k.shape[0], k.shape[1], k.shape[2], k.shape[4]
+    size = {SIF_BF16: 2, SIF_E4M3: 1}.get(dtype)
+    ok = tuple(k.shape) == (layers, n_pages, kv_heads, page_tokens, d_head) and tuple(v.shape) == (layers, n_pages, kv_heads, d_head, page_tokens)
+    ok = ok and size == k.element_size() == v.element_size() and all(t.is_contiguous() for t in (k, v, table, lengths, refs))
+    ok = ok and lengths.shape[0] == table.shape[0] and refs.shape[0] == n_pages and all(t.dtype == torch.int32 for t in (table, lengths, refs))
+    ok = ok and all(t is None or (t.dtype == torch.float32 and t.is_contiguous() and tuple(t.shape) == (layers, kv_heads)) for t in (k_scale, v_scale))
+    if not ok:
+        raise SifError(SIF_E_INVAL, "kv_cache: tensors that do not fit each other, the type or the page size")
+    c.dtype, c.layers, c.kv_heads, c.d_head, c.page_tokens = dtype, layers, kv_heads, d_head, page_tokens
+    c.n_pages, c.n_seqs, c.table_ld = n_pages, table.shape[0], table.shape[1]
+    c.k_dev, c.v_dev, c.k_scale_dev, c.v_scale_dev = ptr(k), ptr(v), ptr(k_scale), ptr(v_scale)
+    c.table_dev, c.lengths_dev, c.refs_dev = ptr(table), ptr(lengths), ptr(refs)
+    return c
+
+
+def sif_kv_workspace_bytes(c):
+    n = lib.sif_kv_workspace_bytes(C.byref(c))
+    if n == 0:
+        raise SifError(SIF_E_INVAL, last_error())
+    return n
+
+
+def sif_k_kv_reset(c, stream=None):
+    return check(lib.sif_k_kv_reset(C.byref(c), stream_ptr(stream)))
+
+
+def sif_k_kv_extend(c, seqs, counts, n, workspace, workspace_bytes, status=None, stream=None):
+    return check(lib.sif_k_kv_extend(C.byref(c), ptr(seqs), ptr(counts), n, ptr(status), ptr(workspace), workspace_bytes, stream_ptr(stream)))
+
+
+def sif_k_kv_write(c, layer, k, v, seqs, n, starts=None, rows=None, ld_k=None, ld_v=None, stream=None):
+    width = c.kv_heads * c.d_head
+    return check(lib.sif_k_kv_write(C.byref(c), layer, ptr(k), ptr(v), _ld(k, ld_k, width), _ld(v, ld_v, width), ptr(seqs), ptr(starts), n,
+                                    n if rows is None else rows, stream_ptr(stream)))
+
+
+def sif_k_kv_fork(c, src, dst, n, status=None, stream=None):
+    return check(lib.sif_k_kv_fork(C.byref(c), ptr(src), ptr(dst), n, ptr(status), stream_ptr(stream)))
+
+
+def sif_k_kv_free(c, seqs, n, stream=None):
+    return check(lib.sif_k_kv_free(C.byref(c), ptr(seqs), n, stream_ptr(stream)))
+
+
+def sif_k_kv_trim(c, seqs, n, window, sinks, stream=None):
+    return check(lib.sif_k_kv_trim(C.byref(c), ptr(seqs), n, window, sinks, stream_ptr(stream)))
+
+
+def sif_k_kv_compact(c, workspace, workspace_bytes, stream=None):
+    return check(lib.sif_k_kv_compact(C.byref(c), ptr(workspace), workspace_bytes, stream_ptr(stream)))
+
+
+def sif_k_kv_copy_pages(c, src, dst, n, status=None, stream=None):
+    return check(lib.sif_k_kv_copy_pages(C.byref(c), ptr(src), ptr(dst), n, ptr(status), stream_ptr(stream)))
+
+
+def attn_decode_args(q, o, n, heads, window=0, sinks=0, layer=0, max_tokens=0, scale=0.0, seqs=None, lse=None, workspace=None, workspace_bytes=0,
+                     ld_q=None, ld_o=None):
+    """A filled sif_attn_decode_args (the tensors stay the caller's to keep)."""
+    a = sif_attn_decode_args()
+    a.struct_size = C.sizeof(sif_attn_decode_args)
+    a.layer, a.n, a.heads, a.window, a.sinks, a.max_tokens, a.scale = layer, n, heads, window, sinks, max_tokens, scale
+    a.ld_q, a.ld_o = _ld(q, ld_q, 0), _ld(o, ld_o, 0)
+    a.seqs_dev, a.q_dev, a.o_dev, a.lse_dev = ptr(seqs), ptr(q), ptr(o), ptr(lse)
+    set_workspace(a, workspace, workspace_bytes)
+    return a
+
+
+def sif_attn_decode_workspace_bytes(c, a):
+    n = lib.sif_attn_decode_workspace_bytes(C.byref(c), C.byref(a))
+    if n == 0:
+        raise SifError(SIF_E_INVAL, last_error())
+    return n
+
+
+def sif_k_attn_decode(c, a, stream=None):
+    return check(lib.sif_k_attn_decode(C.byref(c), C.byref(a), stream_ptr(stream)))

@@ -1,0 +1,537 @@
+// Attention with a sliding window of recent keys and a few first keys (sinks) that stay visible, forward and backward, with fewer key
+// heads than query heads if wanted (Sec. 5.1's transformer training on long sequences; prompts).
+//
+//   key j is visible to the query at position p  iff  j <= p  and  (window = 0  or  p - j < window  or  j < sinks)
+//   forward    o = softmax(scale q k^T | visible) v,  lse = log sum exp
+//   backward   delta = rowsum(do .* o),  P = exp(scale q k^T - lse),  dS = scale P .* (do v^T - delta)
+//              dq = dS k (a block per query rows),  dk = dS^T q,  dv = P^T do (a block per key rows, summed over the query heads of
+//              the key head in registers); P is recomputed in both, no atomics
+//
+// Products, operands and LDS tiles are those of attention.hip.  A block meets only the tiles that one of its rows sees: the sinks', then
+// from the first key of its first row's window to its last row.  Those ranges begin and end exactly there and are not rounded to
+// tiles, and what a fetch would read past the end is the last row again, so that a key or query that nobody sees is never read.
+// Bound by the matrix units, beside which the exponentials take three quarters of the time with heads of 128, all of it with 64.
+#include <math.h>
+#include <algorithm>
+
+#include "attn_tiles.h"
+#include "common.h"
+#include "launch.h"
+
+namespace sif {
+
+constexpr float kLog2e = 1.44269504088896f, kLn2 = 0.693147180559945f;
+
+struct WinArgs {
+  const bf16_t* q; const bf16_t* k; const bf16_t* v;
+  bf16_t* o;
+  float* lse;
+  const int32_t* starts;
+  const bf16_t* d_o;
+  bf16_t* dq; bf16_t* dk; bf16_t* dv;
+  float* delta;                      // [heads][query rows]
+  uint32_t heads, kv_heads, group, hb;      // hb: query heads of one key head that a block works on
+  uint32_t batch, sq, sk, window, sinks, rows, rows_q;
+  uint32_t ld_q, ld_k, ld_v, ld_o, ld_do, ld_dq, ld_dk, ld_dv;
+  float scale;
+};
+
+// Where a sequence's rows are.
+struct WinSeq { uint32_t q0, k0, nq, nk; };
+__device__ __forceinline__ WinSeq win_seq(const WinArgs& a, uint32_t b) {
+  if (a.starts == nullptr) return {b * a.sq, b * a.sk, a.sq, a.sk};
+  const int32_t top = (int32_t)a.rows, s0 = min(max(a.starts[b], 0), top), s1 = min(max(a.starts[b + 1], s0), top);
+  const uint32_t n = min((uint32_t)(s1 - s0), a.sq);
+  return {(uint32_t)s0, (uint32_t)s0, n, n};
+}
+
+// The keys that rows at positions p0 .. p1 see at all: the first `sinks` (as far as they lie below lo), and lo .. hi - 1.
+struct WinSpan { uint32_t lo, hi, sinks; };
+__device__ __forceinline__ WinSpan win_span(const WinArgs& a, int32_t p0, int32_t p1, uint32_t nk) {
+  WinSpan s;
+  s.hi = p1 < 0 ? 0u : min((uint32_t)p1 + 1u, nk);
+  s.lo = a.window != 0 && p0 >= 0 && (uint32_t)p0 >= a.window ? (uint32_t)p0 - a.window + 1u : 0u;
+  s.sinks = min(a.sinks, s.lo);
+  return s;
+}
+
+__device__ __forceinline__ float max_over_halves(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
+// What a wavefront's 32 rows (positions pw .. pw + 31) have to do with keys first .. first + n - 1, of which those below `end` exist.
+__device__ __forceinline__ bool win_none(const WinArgs& a, int32_t pw, uint32_t first, uint32_t n, uint32_t end) {
+  if (pw + 31 < 0 || first >= end || (int32_t)first > pw + 31) return true;
+  return a.window != 0 && (int32_t)(first + n - 1) <= pw - (int32_t)a.window && first >= a.sinks;
+}
+__device__ __forceinline__ bool win_all(const WinArgs& a, int32_t pw, uint32_t first, uint32_t n, uint32_t end) {
+  if (first + n > end || (int32_t)(first + n - 1) > pw) return false;
+  return a.window == 0 || (int32_t)first > pw + 31 - (int32_t)a.window || first + n <= a.sinks;
+}
+__device__ __forceinline__ bool win_sees(const WinArgs& a, int32_t p, uint32_t j, uint32_t end) {
+  return j < end && (int32_t)j <= p && (a.window == 0 || (int32_t)j > p - (int32_t)a.window || j < a.sinks);
+}
+
+template <int DH> constexpr int kWinKv = DH == 64 ? 128 : 64;        // keys of a tile: two buffers of K and V are 64 KB
+
+// Forward.  Four wavefronts of 32 rows: hb query heads of a key head (1, 2 or 4), 128 / hb rows each, so that the wavefronts of a
+// block have nearly the same keys and share them.
+template <int DH>
+__global__ __launch_bounds__(AT_THREADS, 2) void win_fwd_kernel(WinArgs a) {
+  constexpr int KS = DH / 16, DT = DH / 32, KV = kWinKv<DH>, NT = KV / 32;
+  __shared__ __align__(1024) bf16_t sK0[KV * DH];
+  __shared__ __align__(1024) bf16_t sV0[KV * DH];
+  __shared__ __align__(1024) bf16_t sK1[KV * DH];
+  __shared__ __align__(1024) bf16_t sV1[KV * DH];
+  const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), qi = lane & 31, h = lane >> 5;
+  const uint32_t units = a.heads / a.hb, b = blockIdx.x / units, head0 = blockIdx.x % units * a.hb, head = head0 + wave % a.hb, kvh = head0 / a.group;
+  const WinSeq sq = win_seq(a, b);
+  const uint32_t per = AT_Q / a.hb, q_blk = blockIdx.y * per;
+  if (q_blk >= sq.nq) return;
+  const uint32_t qw = q_blk + wave / a.hb * 32, q = qw + qi;
+  const int32_t off = (int32_t)sq.nk - (int32_t)sq.nq, pw = (int32_t)qw + off, p = pw + (int32_t)qi;
+  const uint32_t q_end = min(q_blk + per, sq.nq);
+  const WinSpan sp = win_span(a, (int32_t)q_blk + off, (int32_t)q_end - 1 + off, sq.nk);
+  const bf16_t* kbase = a.k + (size_t)sq.k0 * a.ld_k + kvh * DH;
+  const bf16_t* vbase = a.v + (size_t)sq.k0 * a.ld_v + kvh * DH;
+  const float c2 = a.scale * kLog2e;
+  const uint32_t sink_tiles = (sp.sinks + KV - 1) / KV, tiles = sink_tiles + (sp.hi > sp.lo ? (sp.hi - sp.lo + KV - 1) / KV : 0u);
+
+  bf16x8 fq[KS];
+  {
+    const bf16_t* qp = a.q + (size_t)(sq.q0 + (q < sq.nq ? q : sq.nq - 1)) * a.ld_q + head * DH;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) fq[ks] = *reinterpret_cast<const bf16x8*>(qp + ks * 16 + h * 8);
+  }
+  floatx16 oacc[DT];
+#pragma unroll
+  for (int d = 0; d < DT; ++d)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) oacc[d][r] = 0.f;
+  float m_run = -INFINITY, l_run = 0.f;            // l: of this lane's keys only
+
+  auto first_of = [&](uint32_t t) { return t < sink_tiles ? t * KV : sp.lo + (t - sink_tiles) * KV; };
+  auto end_of = [&](uint32_t t) { return t < sink_tiles ? sp.sinks : sp.hi; };
+  auto fetch = [&](bf16_t* sK, bf16_t* sV, uint32_t t) {
+    at_dma_rows<DH, KV>(sK, kbase, a.ld_k, first_of(t), end_of(t));
+    at_dma_rows<DH, KV>(sV, vbase, a.ld_v, first_of(t), end_of(t));
+  };
+  auto tile = [&](const bf16_t* sK, const bf16_t* sV, uint32_t t, auto edge) {
+    constexpr bool EDGE = decltype(edge)::value;
+    const uint32_t kv0 = first_of(t), end = end_of(t);
+    floatx16 sacc[NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      if (EDGE && win_none(a, pw, kv0 + n * 32, 32, end)) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) sacc[n][r] = -INFINITY;
+        continue;
+      }
+#pragma unroll
+      for (int r = 0; r < 16; ++r) sacc[n][r] = 0.f;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks)
+        sacc[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(at_frag<DH>(sK, n * 32 + qi, ks * 2 + h), fq[ks], sacc[n], 0, 0, 0);
+      if (EDGE) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const uint32_t kv = kv0 + n * 32 + (r >> 2) * 8 + h * 4 + (r & 3);
+          sacc[n][r] = win_sees(a, p, kv, end) ? sacc[n][r] : -INFINITY;
+        }
+      }
+    }
+    float mx = -INFINITY;
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) mx = fmaxf(mx, sacc[n][r]);
+    mx = max_over_halves(mx) * c2;                         // c2 > 0
+    // The running maximum follows only where scores pass it by more than 2^8 (or there was none): sums and accumulators are fp32 and
+    // the probabilities' rounding is relative, so a maximum that is a little low costs nothing, and the accumulators are seldom scaled.
+    if (__any(mx > m_run + 8.0f)) {
+      const float m_new = fmaxf(m_run, mx), m_use = m_new == -INFINITY ? 0.f : m_new;
+      const float alpha = __builtin_amdgcn_exp2f(m_run - m_use);
+      l_run *= alpha;
+#pragma unroll
+      for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) oacc[d][r] *= alpha;
+      m_run = m_new;
+    }
+    const float m_use = m_run == -INFINITY ? 0.f : m_run;
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      if (EDGE && win_none(a, pw, kv0 + n * 32, 32, end)) continue;
+      float pt[16];
+#pragma unroll
+      for (int r = 0; r < 16; ++r) { pt[r] = __builtin_amdgcn_exp2f(fmaf(sacc[n][r], c2, -m_use)); l_run += pt[r]; }
+#pragma unroll
+      for (int s2 = 0; s2 < 2; ++s2) {
+        const bf16x8 fp = at_pack8(pt, 8 * s2);
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+          oacc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(at_frag_tr<DH>(sV, d * 32, n * 32 + 16 * s2 + 4 * h), fp, oacc[d], 0, 0, 0);
+      }
+    }
+  };
+  auto turn = [&](const bf16_t* sK, const bf16_t* sV, uint32_t t) {
+    const uint32_t first = first_of(t), end = end_of(t);
+    if (win_none(a, pw, first, KV, end)) return;
+    if (win_all(a, pw, first, KV, end)) tile(sK, sV, t, std::false_type{});
+    else tile(sK, sV, t, std::true_type{});
+  };
+  if (tiles > 0) fetch(sK0, sV0, 0);
+  for (uint32_t t = 0; t < tiles; t += 2) {
+    wait_fetches();
+    __syncthreads();                                       // tile t has landed, nobody reads buffer 1 any more
+    if (t + 1 < tiles) fetch(sK1, sV1, t + 1);
+    turn(sK0, sV0, t);
+    if (t + 1 < tiles) {
+      wait_fetches();
+      __syncthreads();
+      if (t + 2 < tiles) fetch(sK0, sV0, t + 2);
+      turn(sK1, sV1, t + 1);
+    }
+  }
+  l_run += __shfl_xor(l_run, 32, 64);
+  __syncthreads();                                         // nobody reads the last tiles any more: K's buffers stage the output
+  const uint32_t rows = qw < q_end ? q_end - qw : 0u;
+  bf16_t* stage = KV == AT_KV ? sK0 + wave * (32 * DH) : (wave < 2 ? sK0 : sK1) + (wave & 1) * (32 * DH);
+  at_store_tile<DH>(stage, oacc, l_run > 0.f ? 1.0f / l_run : 0.f, a.o + (size_t)(sq.q0 + qw) * a.ld_o + head * DH, a.ld_o, rows);
+  if (qi < rows && h == 0 && a.lse != nullptr) a.lse[(size_t)head * a.rows_q + sq.q0 + q] = (m_run + __log2f(l_run)) * kLn2;
+}
+
+// Backward, dq.  Rows and wavefronts as in the forward kernel.  Also writes delta.
+template <int DH>
+__global__ __launch_bounds__(AT_THREADS, 2) void win_dq_kernel(WinArgs a) {
+  constexpr int KS = DH / 16, DT = DH / 32, KV = kWinKv<DH>;
+  __shared__ __align__(1024) bf16_t sK0[KV * DH];
+  __shared__ __align__(1024) bf16_t sV0[KV * DH];
+  __shared__ __align__(1024) bf16_t sK1[KV * DH];
+  __shared__ __align__(1024) bf16_t sV1[KV * DH];
+  const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), qi = lane & 31, h = lane >> 5;
+  const uint32_t units = a.heads / a.hb, b = blockIdx.x / units, head0 = blockIdx.x % units * a.hb, head = head0 + wave % a.hb, kvh = head0 / a.group;
+  const WinSeq sq = win_seq(a, b);
+  const uint32_t per = AT_Q / a.hb, q_blk = blockIdx.y * per;
+  if (q_blk >= sq.nq) return;
+  const uint32_t qw = q_blk + wave / a.hb * 32, q = qw + qi;
+  const int32_t off = (int32_t)sq.nk - (int32_t)sq.nq, pw = (int32_t)qw + off, p = pw + (int32_t)qi;
+  const uint32_t q_end = min(q_blk + per, sq.nq);
+  const WinSpan sp = win_span(a, (int32_t)q_blk + off, (int32_t)q_end - 1 + off, sq.nk);
+  const bf16_t* kbase = a.k + (size_t)sq.k0 * a.ld_k + kvh * DH;
+  const bf16_t* vbase = a.v + (size_t)sq.k0 * a.ld_v + kvh * DH;
+  const float c2 = a.scale * kLog2e;
+  const uint32_t sink_tiles = (sp.sinks + KV - 1) / KV, tiles = sink_tiles + (sp.hi > sp.lo ? (sp.hi - sp.lo + KV - 1) / KV : 0u);
+
+  bf16x8 fq[KS], fdo[KS];
+  float dsum = 0.f;
+  const uint32_t row = sq.q0 + (q < sq.nq ? q : sq.nq - 1);
+  {
+    const bf16_t* qp = a.q + (size_t)row * a.ld_q + head * DH;
+    const bf16_t* dop = a.d_o + (size_t)row * a.ld_do + head * DH;
+    const bf16_t* op = a.o + (size_t)row * a.ld_o + head * DH;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      fq[ks] = *reinterpret_cast<const bf16x8*>(qp + ks * 16 + h * 8);
+      const uint4 vd = *reinterpret_cast<const uint4*>(dop + ks * 16 + h * 8), vo = *reinterpret_cast<const uint4*>(op + ks * 16 + h * 8);
+      fdo[ks] = *reinterpret_cast<const bf16x8*>(&vd);
+      dsum += bflo(vd.x) * bflo(vo.x) + bfhi(vd.x) * bfhi(vo.x) + bflo(vd.y) * bflo(vo.y) + bfhi(vd.y) * bfhi(vo.y) +
+              bflo(vd.z) * bflo(vo.z) + bfhi(vd.z) * bfhi(vo.z) + bflo(vd.w) * bflo(vo.w) + bfhi(vd.w) * bfhi(vo.w);
+    }
+  }
+  dsum += __shfl_xor(dsum, 32, 64);
+  const float lq2 = a.lse[(size_t)head * a.rows_q + row] * kLog2e;
+  if (q < q_end && h == 0) a.delta[(size_t)head * a.rows_q + row] = dsum;
+
+  floatx16 dqacc[DT];
+#pragma unroll
+  for (int d = 0; d < DT; ++d)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) dqacc[d][r] = 0.f;
+
+  auto first_of = [&](uint32_t t) { return t < sink_tiles ? t * KV : sp.lo + (t - sink_tiles) * KV; };
+  auto end_of = [&](uint32_t t) { return t < sink_tiles ? sp.sinks : sp.hi; };
+  auto fetch = [&](bf16_t* sK, bf16_t* sV, uint32_t t) {
+    at_dma_rows<DH, KV>(sK, kbase, a.ld_k, first_of(t), end_of(t));
+    at_dma_rows<DH, KV>(sV, vbase, a.ld_v, first_of(t), end_of(t));
+  };
+  auto turn = [&](const bf16_t* sK, const bf16_t* sV, uint32_t t) {
+    const uint32_t kv0 = first_of(t), end = end_of(t);
+#pragma unroll
+    for (int n = 0; n < KV / 32; ++n) {
+      const uint32_t first = kv0 + n * 32;
+      if (win_none(a, pw, first, 32, end)) continue;
+      const bool need_mask = !win_all(a, pw, first, 32, end);
+      floatx16 sacc, pacc;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) { sacc[r] = 0.f; pacc[r] = 0.f; }
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        sacc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(at_frag<DH>(sK, n * 32 + qi, ks * 2 + h), fq[ks], sacc, 0, 0, 0);      // S^T
+        pacc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(at_frag<DH>(sV, n * 32 + qi, ks * 2 + h), fdo[ks], pacc, 0, 0, 0);     // dP^T
+      }
+      float ds[16];
+#pragma unroll
+      for (int r = 0; r < 16; ++r) ds[r] = __builtin_amdgcn_exp2f(fmaf(sacc[r], c2, -lq2)) * a.scale * (pacc[r] - dsum);
+      if (need_mask) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) ds[r] = win_sees(a, p, first + (r >> 2) * 8 + h * 4 + (r & 3), end) ? ds[r] : 0.f;
+      }
+#pragma unroll
+      for (int s2 = 0; s2 < 2; ++s2) {
+        const bf16x8 fds = at_pack8(ds, 8 * s2);
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+          dqacc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(at_frag_tr<DH>(sK, d * 32, n * 32 + 16 * s2 + 4 * h), fds, dqacc[d], 0, 0, 0);
+      }
+    }
+  };
+  if (tiles > 0) fetch(sK0, sV0, 0);
+  for (uint32_t t = 0; t < tiles; t += 2) {
+    wait_fetches();
+    __syncthreads();
+    if (t + 1 < tiles) fetch(sK1, sV1, t + 1);
+    turn(sK0, sV0, t);
+    if (t + 1 < tiles) {
+      wait_fetches();
+      __syncthreads();
+      if (t + 2 < tiles) fetch(sK0, sV0, t + 2);
+      turn(sK1, sV1, t + 1);
+    }
+  }
+  __syncthreads();
+  const uint32_t rows = qw < q_end ? q_end - qw : 0u;
+  bf16_t* stage = KV == AT_KV ? sK0 + wave * (32 * DH) : (wave < 2 ? sK0 : sK1) + (wave & 1) * (32 * DH);
+  at_store_tile<DH>(stage, dqacc, 1.0f, a.dq + (size_t)(sq.q0 + qw) * a.ld_dq + head * DH, a.ld_dq, rows);
+}
+
+// Backward, dk and dv.  A block is 128 keys of a key head, 32 per wavefront; the rows that see them are streamed 64 at a time, query head
+// after query head.
+template <int DH>
+__global__ __launch_bounds__(AT_THREADS, DH == 64 ? 2 : 1) void win_dkv_kernel(WinArgs a) {
+  constexpr int KS = DH / 16, DT = DH / 32;
+  __shared__ __align__(1024) bf16_t sQ0[AT_QB * DH];
+  __shared__ __align__(1024) bf16_t sDo0[AT_QB * DH];
+  __shared__ __align__(1024) bf16_t sQ1[AT_QB * DH];
+  __shared__ __align__(1024) bf16_t sDo1[AT_QB * DH];
+  __shared__ __align__(16) float sL0[AT_QB];
+  __shared__ __align__(16) float sD0[AT_QB];
+  __shared__ __align__(16) float sL1[AT_QB];
+  __shared__ __align__(16) float sD1[AT_QB];
+  const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), ki = lane & 31, h = lane >> 5;
+  const uint32_t b = blockIdx.x / a.kv_heads, kvh = blockIdx.x % a.kv_heads;
+  const WinSeq sq = win_seq(a, b);
+  const uint32_t kv_blk = blockIdx.y * AT_KV, kw = kv_blk + wave * 32, kv = kw + ki;
+  if (kv_blk >= sq.nk) return;
+  const int32_t off = (int32_t)sq.nk - (int32_t)sq.nq;
+  const float c2 = a.scale * kLog2e;
+  // rows (of the sequence) that see one of the block's keys
+  const uint32_t kv_last = min(kv_blk + AT_KV, sq.nk) - 1;
+  const int32_t row_a = max((int32_t)kv_blk - off, 0);
+  const int64_t row_z = a.window == 0 || kv_blk < a.sinks ? (int64_t)sq.nq : min((int64_t)kv_last + a.window - off, (int64_t)sq.nq);
+  const uint32_t q_first = (uint32_t)row_a, q_end = row_z > row_a ? (uint32_t)row_z : q_first;
+  const uint32_t steps = (q_end - q_first + AT_QB - 1) / AT_QB, total = steps * a.group;
+
+  bf16x8 fk[KS], fv[KS];
+  {
+    const uint32_t r = sq.k0 + min(kv, sq.nk - 1);
+    const bf16_t* kp = a.k + (size_t)r * a.ld_k + kvh * DH;
+    const bf16_t* vp = a.v + (size_t)r * a.ld_v + kvh * DH;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      fk[ks] = *reinterpret_cast<const bf16x8*>(kp + ks * 16 + h * 8);
+      fv[ks] = *reinterpret_cast<const bf16x8*>(vp + ks * 16 + h * 8);
+    }
+  }
+  floatx16 dkacc[DT], dvacc[DT];
+#pragma unroll
+  for (int d = 0; d < DT; ++d)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) { dkacc[d][r] = 0.f; dvacc[d][r] = 0.f; }
+
+  auto fetch = [&](bf16_t* sQ, bf16_t* sDo, float* sL, float* sD, uint32_t t) {
+    const uint32_t head = kvh * a.group + t / steps, q0 = q_first + t % steps * AT_QB;
+    at_dma_rows<DH, AT_QB>(sQ, a.q + (size_t)sq.q0 * a.ld_q + head * DH, a.ld_q, q0, q_end);
+    at_dma_rows<DH, AT_QB>(sDo, a.d_o + (size_t)sq.q0 * a.ld_do + head * DH, a.ld_do, q0, q_end);
+    if (threadIdx.x < AT_QB) {
+      const size_t at = (size_t)head * a.rows_q + sq.q0 + min(q0 + threadIdx.x, q_end - 1);
+      sL[threadIdx.x] = a.lse[at] * kLog2e;
+      sD[threadIdx.x] = a.delta[at];
+    }
+  };
+  auto turn = [&](const bf16_t* sQ, const bf16_t* sDo, const float* sL, const float* sD, uint32_t t) {
+    const uint32_t q0 = q_first + t % steps * AT_QB;
+#pragma unroll
+    for (int u = 0; u < AT_QB / 32; ++u) {
+      const uint32_t qu = q0 + u * 32;
+      const int32_t pw = (int32_t)qu + off;
+      if (qu >= q_end || win_none(a, pw, kw, 32, sq.nk)) continue;
+      const bool need_mask = qu + 32 > q_end || !win_all(a, pw, kw, 32, sq.nk);
+      floatx16 sacc, pacc;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) { sacc[r] = 0.f; pacc[r] = 0.f; }
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        sacc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(at_frag<DH>(sQ, u * 32 + ki, ks * 2 + h), fk[ks], sacc, 0, 0, 0);      // S  [q][kv]
+        pacc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(at_frag<DH>(sDo, u * 32 + ki, ks * 2 + h), fv[ks], pacc, 0, 0, 0);     // dP [q][kv]
+      }
+      float pr[16], ds[16];
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const float4 l4 = *reinterpret_cast<const float4*>(sL + u * 32 + g * 8 + h * 4);
+        const float4 d4 = *reinterpret_cast<const float4*>(sD + u * 32 + g * 8 + h * 4);
+        const float lv[4] = {l4.x, l4.y, l4.z, l4.w}, dv[4] = {d4.x, d4.y, d4.z, d4.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int r = g * 4 + e;
+          pr[r] = __builtin_amdgcn_exp2f(fmaf(sacc[r], c2, -lv[e]));
+          ds[r] = pr[r] * a.scale * (pacc[r] - dv[e]);
+        }
+      }
+      if (need_mask) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const uint32_t row = qu + (r >> 2) * 8 + h * 4 + (r & 3);
+          const bool ok = row < q_end && win_sees(a, (int32_t)row + off, kv, sq.nk);
+          pr[r] = ok ? pr[r] : 0.f;
+          ds[r] = ok ? ds[r] : 0.f;
+        }
+      }
+#pragma unroll
+      for (int s2 = 0; s2 < 2; ++s2) {
+        const bf16x8 fp = at_pack8(pr, 8 * s2), fds = at_pack8(ds, 8 * s2);
+        const uint32_t qb = u * 32 + 16 * s2 + 4 * h;
+#pragma unroll
+        for (int d = 0; d < DT; ++d) {
+          dvacc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(at_frag_tr<DH>(sDo, d * 32, qb), fp, dvacc[d], 0, 0, 0);      // dV^T
+          dkacc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(at_frag_tr<DH>(sQ, d * 32, qb), fds, dkacc[d], 0, 0, 0);      // dK^T
+        }
+      }
+    }
+  };
+  if (total > 0) fetch(sQ0, sDo0, sL0, sD0, 0);
+  for (uint32_t t = 0; t < total; t += 2) {
+    wait_fetches();
+    __syncthreads();
+    if (t + 1 < total) fetch(sQ1, sDo1, sL1, sD1, t + 1);
+    turn(sQ0, sDo0, sL0, sD0, t);
+    if (t + 1 < total) {
+      wait_fetches();
+      __syncthreads();
+      if (t + 2 < total) fetch(sQ0, sDo0, sL0, sD0, t + 2);
+      turn(sQ1, sDo1, sL1, sD1, t + 1);
+    }
+  }
+  __syncthreads();
+  bf16_t* stage = (wave < 2 ? sQ0 : sDo0) + (wave & 1) * (32 * DH);
+  const uint32_t rows = kw < sq.nk ? sq.nk - kw : 0u;
+  at_store_tile<DH>(stage, dkacc, 1.0f, a.dk + (size_t)(sq.k0 + kw) * a.ld_dk + kvh * DH, a.ld_dk, rows);
+  at_store_tile<DH>(stage, dvacc, 1.0f, a.dv + (size_t)(sq.k0 + kw) * a.ld_dv + kvh * DH, a.ld_dv, rows);
+}
+
+static bool al16(const void* p) { return ((uintptr_t)p & 15) == 0; }
+
+// Extents of either pass, and what the kernels are told.
+static sif_status win_plan(const char* who, const sif_window_attn_args* a, WinArgs* w) {
+  if (!a) return fail(SIF_E_INVAL, "%s: null arguments", who);
+  if (a->struct_size != sizeof(sif_window_attn_args)) return fail(SIF_E_INVAL, "%s: struct_size", who);
+  if (!a->heads || !a->kv_heads || a->heads % a->kv_heads) return fail(SIF_E_INVAL, "%s: heads must be a multiple of kv_heads", who);
+  if (a->d_head != 64 && a->d_head != 128) return fail(SIF_E_INVAL, "%s: d_head must be 64 or 128", who);
+  if (!a->batch || !a->seq_q || !a->seq_k) return fail(SIF_E_INVAL, "%s: empty extent", who);
+  if (a->heads > 1024) return fail(SIF_E_INVAL, "%s: at most 1024 heads", who);
+  if (a->seq_q > (1u << 21) || a->seq_k > (1u << 21)) return fail(SIF_E_INVAL, "%s: sequences of at most 2^21 rows", who);
+  if ((uint64_t)a->batch * a->heads > 0x7FFFFFFFull || (uint64_t)a->batch * a->seq_q > 0x7FFFFFFFull || (uint64_t)a->batch * a->seq_k > 0x7FFFFFFFull)
+    return fail(SIF_E_INVAL, "%s: rows or heads beyond 31 bits", who);
+  if (a->sinks > 128) return fail(SIF_E_INVAL, "%s: at most 128 sinks", who);
+  if (a->window > (1u << 30)) return fail(SIF_E_INVAL, "%s: a window of at most 2^30 (0: no limit)", who);
+  if (!(a->scale >= 0.f) || !std::isfinite(a->scale)) return fail(SIF_E_INVAL, "%s: scale must be finite and not negative", who);
+  if (a->starts_dev && (a->seq_q != a->seq_k || a->rows == 0 || a->rows > 0x7FFFFFFFu)) return fail(SIF_E_INVAL, "%s: with starts, seq_q = seq_k and rows in 1 .. 2^31 - 1", who);
+  if ((uintptr_t)a->starts_dev & 3) return fail(SIF_E_INVAL, "%s: misaligned starts", who);
+  w->starts = a->starts_dev;
+  w->heads = a->heads;
+  w->kv_heads = a->kv_heads;
+  w->group = a->heads / a->kv_heads;
+  w->hb = w->group % 4 == 0 ? 4 : (w->group % 2 == 0 ? 2 : 1);
+  w->batch = a->batch;
+  w->sq = a->seq_q;
+  w->sk = a->seq_k;
+  w->window = a->window;
+  w->sinks = a->window != 0 ? a->sinks : 0;
+  w->rows = a->rows;
+  w->rows_q = a->starts_dev ? a->rows : a->batch * a->seq_q;
+  w->scale = a->scale != 0.f ? a->scale : 1.0f / sqrtf((float)a->d_head);
+  w->q = (const bf16_t*)a->q_dev;
+  w->k = (const bf16_t*)a->k_dev;
+  w->v = (const bf16_t*)a->v_dev;
+  w->o = (bf16_t*)a->o_dev;
+  w->lse = a->lse_dev;
+  w->d_o = (const bf16_t*)a->do_dev;
+  w->dq = (bf16_t*)a->dq_dev;
+  w->dk = (bf16_t*)a->dk_dev;
+  w->dv = (bf16_t*)a->dv_dev;
+  w->delta = nullptr;
+  w->ld_q = a->ld_q; w->ld_k = a->ld_k; w->ld_v = a->ld_v; w->ld_o = a->ld_o;
+  w->ld_do = a->ld_do; w->ld_dq = a->ld_dq; w->ld_dk = a->ld_dk; w->ld_dv = a->ld_dv;
+  return SIF_OK;
+}
+
+static sif_status win_check(const char* who, const sif_window_attn_args* a) {
+  const uint32_t wq = a->heads * a->d_head, wk = a->kv_heads * a->d_head;
+  if (!a->q_dev || !a->k_dev || !a->v_dev || !a->o_dev) return fail(SIF_E_INVAL, "%s: null operand", who);
+  if (a->ld_q < wq || a->ld_o < wq || a->ld_k < wk || a->ld_v < wk || ((a->ld_q | a->ld_o | a->ld_k | a->ld_v) & 7)) return fail(SIF_E_INVAL, "%s: bad leading dimensions", who);
+  if (!al16(a->q_dev) || !al16(a->k_dev) || !al16(a->v_dev) || !al16(a->o_dev)) return fail(SIF_E_INVAL, "%s: pointers must be 16-byte aligned", who);
+  if ((uintptr_t)a->lse_dev & 3) return fail(SIF_E_INVAL, "%s: misaligned lse", who);
+  return SIF_OK;
+}
+
+static uint64_t win_workspace(const WinArgs& w) { return ((uint64_t)w.heads * w.rows_q * sizeof(float) + 255) / 256 * 256; }
+
+}  // namespace sif
+
+using namespace sif;
+
+extern "C" {
+
+sif_status sif_k_window_attn_fwd(const sif_window_attn_args* a, void* stream) {
+  WinArgs w;
+  if (sif_status st = win_plan("window_attn_fwd", a, &w)) return st;
+  if (sif_status st = win_check("window_attn_fwd", a)) return st;
+  hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  const uint32_t per = AT_Q / w.hb;
+  const dim3 grid(w.batch * (w.heads / w.hb), (w.sq + per - 1) / per);
+  if (a->d_head == 64) hipLaunchKernelGGL((win_fwd_kernel<64>), grid, dim3(AT_THREADS), 0, s, w);
+  else hipLaunchKernelGGL((win_fwd_kernel<128>), grid, dim3(AT_THREADS), 0, s, w);
+  return check_launch("window_attn_fwd");
+}
+
+uint64_t sif_window_attn_bwd_workspace_bytes(const sif_window_attn_args* a) {
+  WinArgs w;
+  return win_plan("window_attn_bwd_workspace_bytes", a, &w) == SIF_OK ? win_workspace(w) : 0;
+}
+
+sif_status sif_k_window_attn_bwd(const sif_window_attn_args* a, void* stream) {
+  WinArgs w;
+  if (sif_status st = win_plan("window_attn_bwd", a, &w)) return st;
+  if (sif_status st = win_check("window_attn_bwd", a)) return st;
+  const uint32_t wq = a->heads * a->d_head, wk = a->kv_heads * a->d_head;
+  if (!a->lse_dev || !a->do_dev || !a->dq_dev || !a->dk_dev || !a->dv_dev) return fail(SIF_E_INVAL, "window_attn_bwd: null operand");
+  if (a->ld_do < wq || a->ld_dq < wq || a->ld_dk < wk || a->ld_dv < wk || ((a->ld_do | a->ld_dq | a->ld_dk | a->ld_dv) & 7))
+    return fail(SIF_E_INVAL, "window_attn_bwd: bad leading dimensions");
+  if (!al16(a->do_dev) || !al16(a->dq_dev) || !al16(a->dk_dev) || !al16(a->dv_dev)) return fail(SIF_E_INVAL, "window_attn_bwd: pointers must be 16-byte aligned");
+  if (!a->workspace_dev || ((uintptr_t)a->workspace_dev & 255)) return fail(SIF_E_INVAL, "window_attn_bwd: the workspace must be 256-byte aligned");
+  if (a->workspace_bytes < win_workspace(w))
+    return fail(SIF_E_NOMEM, "window_attn_bwd: the workspace holds %llu of %llu bytes", (unsigned long long)a->workspace_bytes, (unsigned long long)win_workspace(w));
+  w.delta = (float*)a->workspace_dev;
+  hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  const uint32_t per = AT_Q / w.hb;
+  const dim3 gq(w.batch * (w.heads / w.hb), (w.sq + per - 1) / per), gk(w.batch * w.kv_heads, (w.sk + AT_KV - 1) / AT_KV);
+  if (a->d_head == 64) hipLaunchKernelGGL((win_dq_kernel<64>), gq, dim3(AT_THREADS), 0, s, w);
+  else hipLaunchKernelGGL((win_dq_kernel<128>), gq, dim3(AT_THREADS), 0, s, w);
+  if (sif_status st = check_launch("window_attn_bwd: dq")) return st;
+  if (a->d_head == 64) hipLaunchKernelGGL((win_dkv_kernel<64>), gk, dim3(AT_THREADS), 0, s, w);
+  else hipLaunchKernelGGL((win_dkv_kernel<128>), gk, dim3(AT_THREADS), 0, s, w);
+  return check_launch("window_attn_bwd: dk and dv");
+}
+
+}  // extern "C"
