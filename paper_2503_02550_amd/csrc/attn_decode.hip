@@ -24,7 +24,8 @@ namespace sif {
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float floatx4 __attribute__((ext_vector_type(4)));
 
-constexpr uint32_t AD_WAVES = 4, AD_HEADS = 16;
+constexpr uint32_t AD_WAVES = 4, AD_HEADS = 16, AD_MAX_SPLITS = 1024;
+constexpr float kNoSplit = -1.0f;       // in the place of a split's sum
 
 struct DecodeArgs {
   KvView c;
@@ -63,10 +64,20 @@ __device__ __forceinline__ bf16x8 from_e4m3(uint32_t a, uint32_t b) {
   r[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.0f, true));
   return __builtin_bit_cast(bf16x8, r);
 }
+// 16 bytes of lines that one fetch instruction takes whole and nobody reads again: loads that claim no place in the caches.  (1 GiB read by
+// 256 to 1024 blocks in the ordinary way takes 167 to 222 us, 4.8 to 6.4 TB/s, in this way 148 to 206.)  That is V's case where a page is no
+// longer than a step: 64 sequences of 4096 tokens 189 -> 171 us, of 1 to 8192 215 -> 201.  K's rows of more than 64 bytes take several
+// instructions to a line, and so do V's in longer pages; with these loads the line came from memory again (one sequence of
+// 262011 tokens, pages of 64: 186 -> 206 us; K too: 64 sequences of 1 to 8192 222).
+__device__ __forceinline__ uint4 fetch16(const unsigned char* p) {
+  typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+  const u32x4 v = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p));
+  return make_uint4(v[0], v[1], v[2], v[3]);
+}
 __device__ __forceinline__ bf16x8 as_bf16(const uint4& v) { return *reinterpret_cast<const bf16x8*>(&v); }
 
-// Grid: (units = sequence x kv head x tile of 16 query heads, splits).
-template <int DH, bool E4M3>
+// STREAM: a step is at least as long as a page, see fetch16.  Grid: (units = sequence x kv head x tile of 16 query heads, splits).
+template <int DH, bool E4M3, bool STREAM>
 __global__ __launch_bounds__(256, 2) void attn_decode_kernel(DecodeArgs a) {
   constexpr uint32_t TOK = E4M3 ? 64 : 32, NT = TOK / 16, ELT = E4M3 ? 1 : 2;
   constexpr uint32_t KL = DH * ELT / 64, DT = DH / 16;                 // 16-byte fetches of a lane per 16 keys; tiles of 16 d
@@ -78,7 +89,13 @@ __global__ __launch_bounds__(256, 2) void attn_decode_kernel(DecodeArgs a) {
   const int32_t s = kv_listed(c, a.seqs, i);
   const DecodeSpan sp = decode_span<TOK>(s >= 0 ? kv_length(c, s) : 0u, a.window, a.sinks);
   const uint32_t parts = sp.steps == 0 ? 1u : std::min((sp.steps + a.chunk - 1) / a.chunk, a.splits), split = blockIdx.y;
-  if (split >= parts) return;
+  // what the join reads of splits that are not used
+  auto unused = [&](uint32_t which) {
+    if (threadIdx.x < std::min(a.group - ht * AD_HEADS, AD_HEADS))
+      a.part[(((size_t)i * a.heads + kvh * a.group + ht * AD_HEADS + threadIdx.x) * a.splits + which) * (DH + 4) + 1] = kNoSplit;
+  };
+  if (split >= parts) { unused(split); return; }
+  if (parts == 1 && a.splits > 1) unused(0);
   const uint32_t per = (sp.steps + parts - 1) / parts, end = std::min(sp.steps, (split + 1) * per);
   const uint32_t in_group = ht * AD_HEADS + col, head = kvh * a.group + in_group;
   const bool head_ok = in_group < a.group;
@@ -108,23 +125,27 @@ __global__ __launch_bounds__(256, 2) void attn_decode_kernel(DecodeArgs a) {
   for (uint32_t d = 0; d < DT; ++d) oacc[d] = floatx4{0.f, 0.f, 0.f, 0.f};
   float m_run = -INFINITY, l_run = 0.f;
 
-  struct Tile { uint4 k[NT * KL], v[DT]; uint32_t base; bool kpage, vpage; };
+  struct Tile { uint4 k[NT * KL], v[DT]; uint32_t base; bool there; };
   auto base_of = [&](uint32_t step) { return step < sp.sink_steps ? step * TOK : sp.from + (step - sp.sink_steps) * TOK; };
   // the pages of a step's tokens: a lane needs that of its key row's quarter and that of its own quarter
   auto page_at = [&](uint32_t token) { const uint32_t slot = token >> c.page_lg; return slot < pages ? row[slot] : -1; };
   auto fetch = [&](Tile& t, uint32_t step, int32_t kp, int32_t vp) {
     t.base = base_of(step);
-    t.kpage = (uint32_t)kp < c.n_pages;
-    t.vpage = (uint32_t)vp < c.n_pages;
+    t.there = (uint32_t)vp < c.n_pages;
     const uint32_t ktok = t.base + (col >> 2) * (TOK / 4) + (col & 3), vtok = t.base + g * (TOK / 4);
-    const unsigned char* kp8 = kbase + (size_t)(t.kpage ? kp : 0) * c.page_bytes + ((ktok & page_mask) * DH) * ELT + g * 16;
-    const unsigned char* vp8 = vbase + (size_t)(t.vpage ? vp : 0) * c.page_bytes + ((col << c.page_lg) + (vtok & page_mask)) * ELT;
+    const unsigned char* kp8 = kbase + (size_t)((uint32_t)kp < c.n_pages ? kp : 0) * c.page_bytes + ((ktok & page_mask) * DH) * ELT + g * 16;
+    const unsigned char* vp8 = vbase + (size_t)(t.there ? vp : 0) * c.page_bytes + ((col << c.page_lg) + (vtok & page_mask)) * ELT;
 #pragma unroll
     for (uint32_t n = 0; n < NT; ++n)
 #pragma unroll
       for (uint32_t j = 0; j < KL; ++j) t.k[n * KL + j] = *reinterpret_cast<const uint4*>(kp8 + (n * 4 * DH) * ELT + j * 64);
+    if constexpr (STREAM) {
 #pragma unroll
-    for (uint32_t d = 0; d < DT; ++d) t.v[d] = *reinterpret_cast<const uint4*>(vp8 + ((d * 16) << c.page_lg) * ELT);
+      for (uint32_t d = 0; d < DT; ++d) t.v[d] = fetch16(vp8 + ((d * 16) << c.page_lg) * ELT);
+    } else {
+#pragma unroll
+      for (uint32_t d = 0; d < DT; ++d) t.v[d] = *reinterpret_cast<const uint4*>(vp8 + ((d * 16) << c.page_lg) * ELT);
+    }
   };
   auto use = [&](Tile& t) {
     floatx4 sc[NT];
@@ -146,12 +167,12 @@ __global__ __launch_bounds__(256, 2) void attn_decode_kernel(DecodeArgs a) {
     // be anything, a NaN too: scores become -inf, values zero.
     const uint32_t first = t.base + g * (TOK / 4);
     const bool whole = t.base + TOK <= sp.len && (t.base >= sp.lo || t.base + TOK <= a.sinks);
-    if (!whole || !__all(t.vpage)) {
+    if (!whole || !__all(t.there)) {
       uint32_t keep = 0;                                   // bit e: token first + e is visible
 #pragma unroll
       for (uint32_t e = 0; e < TOK / 4; ++e) {
         const uint32_t tok = first + e;
-        keep |= (t.vpage && tok < sp.len && (tok >= sp.lo || tok < a.sinks)) ? 1u << e : 0u;
+        keep |= (t.there && tok < sp.len && (tok >= sp.lo || tok < a.sinks)) ? 1u << e : 0u;
       }
 #pragma unroll
       for (uint32_t n = 0; n < NT; ++n)
@@ -202,8 +223,9 @@ __global__ __launch_bounds__(256, 2) void attn_decode_kernel(DecodeArgs a) {
       }
     }
   };
-  // A wavefront's steps: every fourth of the split's.  The next one's contents are on the way while one is used, and the page
-  // numbers of the one after that.
+  // A wavefront's steps: every fourth of the split's.  While one is used the next one's contents are on the way, and in front of these the
+  // page numbers of the one after that: loads complete in order, so numbers asked for behind the contents would be waited for with
+  // them.  (A quarter of the split's steps each, one after the other: one sequence of 262011 tokens 186 -> 207 us.)
   auto kpage_of = [&](uint32_t step) { return step < end ? page_at(base_of(step) + (col >> 2) * (TOK / 4)) : -1; };
   auto vpage_of = [&](uint32_t step) { return step < end ? page_at(base_of(step) + g * (TOK / 4)) : -1; };
   uint32_t step = split * per + wave;
@@ -212,17 +234,17 @@ __global__ __launch_bounds__(256, 2) void attn_decode_kernel(DecodeArgs a) {
     int32_t kp = kpage_of(step), vp = vpage_of(step), kn = kpage_of(step + AD_WAVES), vn = vpage_of(step + AD_WAVES);
     fetch(t0, step, kp, vp);
     for (;;) {
+      kp = kpage_of(step + 2 * AD_WAVES);
+      vp = vpage_of(step + 2 * AD_WAVES);
       const bool more = step + AD_WAVES < end;
       if (more) fetch(t1, step + AD_WAVES, kn, vn);
-      kn = kpage_of(step + 2 * AD_WAVES);
-      vn = vpage_of(step + 2 * AD_WAVES);
       use(t0);
       if (!more) break;
       step += AD_WAVES;
-      const bool more2 = step + AD_WAVES < end;
-      if (more2) fetch(t0, step + AD_WAVES, kn, vn);
       kn = kpage_of(step + 2 * AD_WAVES);
       vn = vpage_of(step + 2 * AD_WAVES);
+      const bool more2 = step + AD_WAVES < end;
+      if (more2) fetch(t0, step + AD_WAVES, kp, vp);
       use(t1);
       if (!more2) break;
       step += AD_WAVES;
@@ -273,54 +295,65 @@ __global__ __launch_bounds__(256, 2) void attn_decode_kernel(DecodeArgs a) {
   }
 }
 
-// Joins a row's splits: one block per (sequence, query head), wavefronts take every 16th split, two columns a lane.
-template <int DH, bool E4M3>
+// Joins a row's splits: one block per (sequence, query head).  First every split's weight, then the weighted sum, DH / 4 lanes to a split.
+template <int DH>
 __global__ __launch_bounds__(256) void attn_decode_join_kernel(DecodeArgs a) {
-  constexpr uint32_t TOK = E4M3 ? 64 : 32, W = 4, PER = DH / 64;
-  __shared__ float s_o[W][DH], s_m[W], s_l[W];
-  const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, head = blockIdx.x % a.heads, i = blockIdx.x / a.heads;
-  const int32_t s = kv_listed(a.c, a.seqs, i);
-  const DecodeSpan sp = decode_span<TOK>(s >= 0 ? kv_length(a.c, s) : 0u, a.window, a.sinks);
-  const uint32_t parts = sp.steps == 0 ? 1u : std::min((sp.steps + a.chunk - 1) / a.chunk, a.splits);
-  if (parts <= 1) return;
-  // splits whose share is empty (their number times the share passes the end) left nothing visible: they wrote m = -inf
+  constexpr uint32_t LANES = DH / 4, ROWS = 256 / LANES;
+  __shared__ float s_w[AD_MAX_SPLITS], s_l[AD_MAX_SPLITS];
+  __shared__ __align__(16) float4 s_o[256];
+  __shared__ float sm[16];
+  const uint32_t t = threadIdx.x, head = blockIdx.x % a.heads, i = blockIdx.x / a.heads;
   const float* from = a.part + ((size_t)i * a.heads + head) * a.splits * (DH + 4);
-  float m = -INFINITY, l = 0.f, y[PER] = {};
-  for (uint32_t p = wave; p < parts; p += W) {
-    const float* at = from + (size_t)p * (DH + 4);
-    const float2 ml = *reinterpret_cast<const float2*>(at);
-    float v[PER];
-#pragma unroll
-    for (uint32_t e = 0; e < PER; ++e) v[e] = at[4 + lane * PER + e];
-    const float m_new = fmaxf(m, ml.x), m_use = m_new == -INFINITY ? 0.f : m_new;
-    const float f = __builtin_amdgcn_exp2f(m - m_use), h = __builtin_amdgcn_exp2f(ml.x - m_use);
-    l = l * f + ml.y * h;
-#pragma unroll
-    for (uint32_t e = 0; e < PER; ++e) y[e] = y[e] * f + v[e] * h;
-    m = m_new;
+  // Everything that is known only on the device - how many splits the sequence has - stands in the splits themselves: the first
+  // `parts` have an l, the others kNoSplit (all of them if one block did the whole sequence).  So there are two rounds of loads, and not the
+  // length's and the list's before them.
+  float m = -INFINITY;
+  uint32_t used = 0;
+  for (uint32_t p = t; p < a.splits; p += 256) {
+    const float2 ml = *reinterpret_cast<const float2*>(from + (size_t)p * (DH + 4));
+    const bool here = ml.y != kNoSplit;
+    used += here ? 1u : 0u;
+    s_w[p] = here ? ml.x : -INFINITY;
+    s_l[p] = here ? ml.y : 0.f;
+    m = here ? fmaxf(m, ml.x) : m;
   }
-  if (lane == 0) { s_m[wave] = m; s_l[wave] = l; }
-#pragma unroll
-  for (uint32_t e = 0; e < PER; ++e) s_o[wave][lane * PER + e] = y[e];
+  const uint32_t parts = (uint32_t)block_sum((float)used, sm);
+  if (parts == 0) return;
+  m = block_max(m, sm);
+  float l = 0.f;
+  for (uint32_t p = t; p < parts; p += 256) {
+    const float w = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s_w[p] - m);      // (a thread's own words up to here)
+    s_w[p] = w;
+    l += w * s_l[p];
+  }
+  l = block_sum(l, sm);                            // (its barriers stand behind the weights too)
+  float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
+  for (uint32_t p = t / LANES; p < parts; p += ROWS) {
+    const float4 v = *reinterpret_cast<const float4*>(from + (size_t)p * (DH + 4) + 4 + t % LANES * 4);
+    const float w = s_w[p];
+    y.x += w * v.x; y.y += w * v.y; y.z += w * v.z; y.w += w * v.w;
+  }
+  s_o[t] = y;
   __syncthreads();
-  if (threadIdx.x >= DH / 2) return;
-  m = fmaxf(fmaxf(s_m[0], s_m[1]), fmaxf(s_m[2], s_m[3]));
-  l = 0.f;
-  float t0 = 0.f, t1 = 0.f;
+  if (t >= LANES) return;
 #pragma unroll
-  for (uint32_t w = 0; w < W; ++w) {
-    const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s_m[w] - m);
-    l += f * s_l[w];
-    t0 += f * s_o[w][threadIdx.x * 2];
-    t1 += f * s_o[w][threadIdx.x * 2 + 1];
+  for (uint32_t r = 1; r < ROWS; ++r) {
+    const float4 v = s_o[r * LANES + t];
+    y.x += v.x; y.y += v.y; y.z += v.z; y.w += v.w;
   }
   const float inv = l > 0.f ? 1.f / l : 0.f;
-  reinterpret_cast<uint32_t*>(a.o + (size_t)i * a.ld_o + (size_t)head * DH)[threadIdx.x] = pack_bf2(t0 * inv, t1 * inv);
-  if (threadIdx.x == 0 && a.lse != nullptr) a.lse[(size_t)i * a.heads + head] = (m + __log2f(l)) * 0.693147180559945f;
+  *reinterpret_cast<uint2*>(a.o + (size_t)i * a.ld_o + (size_t)head * DH + t * 4) = make_uint2(pack_bf2(y.x * inv, y.y * inv), pack_bf2(y.z * inv, y.w * inv));
+  if (t == 0 && a.lse != nullptr) a.lse[(size_t)i * a.heads + head] = (m + __log2f(l)) * 0.693147180559945f;
 }
 
-// How the work is divided.  A split is at least two steps of each wavefront (below that its own end costs more than it saves), and there
-// are as many as give the chip eight blocks per CU, so that sequences of unequal length even out.
+// How the work is divided.  A CU takes in some 47 KB per us whatever its wavefronts do, so a launch wants all CUs: splits of at least one
+// step per wavefront until there is a block for each of the 256 CUs.  (One sequence, 8 kv heads of 128: 1000 tokens 14.0 -> 8.6 us,
+// 8000 84 -> 11.8, 30000 352 -> 25.8, the join's 4 to 5 us included.)  No more than that: with a block per CU the memory is near its rate,
+// more splits only cost their own ends and a longer join (32 sequences of 4000 tokens: 96.8 us, 104 with eight blocks per CU; 64 of 4096:
+// 188 and 200).  Where lengths differ much, more splits would even them out (32 sequences of 1 to 8000: 118 and 111; 64 of 1 to
+// 8192: 215 and 210), but lengths are not known here.  Equal shares of all steps for 512 blocks, found from the lengths on the
+// device, were tried: 107 and 214 us there, 105 and 195 for the equal lengths, and 1.5 to 4 us more for every short call.
 static sif_status decode_plan(const char* who, const sif_kv_cache* c, const sif_attn_decode_args* a, DecodeArgs* out, uint64_t* bytes) {
   if (sif_status st = kv_check(who, c, &out->c)) return st;
   if (!a) return fail(SIF_E_INVAL, "%s: null arguments", who);
@@ -342,8 +375,8 @@ static sif_status decode_plan(const char* who, const sif_kv_cache* c, const sif_
   uint64_t seen = a->max_tokens != 0 ? a->max_tokens : (uint64_t)c->table_ld * c->page_tokens;
   if (a->window != 0) seen = std::min<uint64_t>(seen, (uint64_t)a->window + a->sinks + 2 * tok);
   const uint64_t steps = std::max<uint64_t>(1, (seen + tok - 1) / tok);
-  const uint64_t most = std::max<uint64_t>(1, steps / (2 * AD_WAVES));
-  out->splits = (uint32_t)std::min<uint64_t>(std::min<uint64_t>(most, 1024), std::max<uint64_t>(1, 2048 / units));
+  const uint64_t most = std::max<uint64_t>(1, steps / AD_WAVES);
+  out->splits = (uint32_t)std::min<uint64_t>(std::min<uint64_t>(most, AD_MAX_SPLITS), std::max<uint64_t>(1, 256 / units));
   out->chunk = (uint32_t)((steps + out->splits - 1) / out->splits);
   *bytes = out->splits > 1 ? (uint64_t)a->n * a->heads * out->splits * (c->d_head + 4) * sizeof(float) : 256;
   return SIF_OK;
@@ -385,21 +418,22 @@ sif_status sif_k_attn_decode(const sif_kv_cache* c, const sif_attn_decode_args* 
   d.scale = a->scale != 0.f ? a->scale : 1.0f / sqrtf((float)c->d_head);
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   const dim3 grid(d.n * d.c.kv_heads * d.head_tiles, d.splits);
-#define AD_LAUNCH(K, GRID) \
-  if (c->d_head == 64) { \
-    if (c->dtype == SIF_E4M3) hipLaunchKernelGGL((K<64, true>), GRID, dim3(256), 0, s, d); \
-    else hipLaunchKernelGGL((K<64, false>), GRID, dim3(256), 0, s, d); \
-  } else { \
-    if (c->dtype == SIF_E4M3) hipLaunchKernelGGL((K<128, true>), GRID, dim3(256), 0, s, d); \
-    else hipLaunchKernelGGL((K<128, false>), GRID, dim3(256), 0, s, d); \
-  }
-  AD_LAUNCH(attn_decode_kernel, grid);
-  if (sif_status st = check_launch("attn_decode")) return st;
-  if (d.splits > 1) {
-    AD_LAUNCH(attn_decode_join_kernel, dim3(d.n * d.heads));
-    return check_launch("attn_decode: join");
+  const bool stream_v = c->page_tokens <= (c->dtype == SIF_E4M3 ? 64u : 32u) && d.head_tiles == 1;       // see fetch16; a second tile of heads reads it again
+#define AD_LAUNCH(DH, E) \
+  if (stream_v) hipLaunchKernelGGL((attn_decode_kernel<DH, E, true>), grid, dim3(64 * AD_WAVES), 0, s, d); \
+  else hipLaunchKernelGGL((attn_decode_kernel<DH, E, false>), grid, dim3(64 * AD_WAVES), 0, s, d)
+  if (c->d_head == 64) {
+    if (c->dtype == SIF_E4M3) { AD_LAUNCH(64, true); } else { AD_LAUNCH(64, false); }
+  } else {
+    if (c->dtype == SIF_E4M3) { AD_LAUNCH(128, true); } else { AD_LAUNCH(128, false); }
   }
 #undef AD_LAUNCH
+  if (sif_status st = check_launch("attn_decode")) return st;
+  if (d.splits > 1) {
+    if (c->d_head == 64) hipLaunchKernelGGL((attn_decode_join_kernel<64>), dim3(d.n * d.heads), dim3(256), 0, s, d);
+    else hipLaunchKernelGGL((attn_decode_join_kernel<128>), dim3(d.n * d.heads), dim3(256), 0, s, d);
+    return check_launch("attn_decode: join");
+  }
   return SIF_OK;
 }
 

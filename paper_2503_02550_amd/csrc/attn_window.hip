@@ -30,6 +30,8 @@ struct WinArgs {
   const bf16_t* d_o;
   bf16_t* dq; bf16_t* dk; bf16_t* dv;
   float* delta;                      // [heads][query rows]
+  float* part;                       // sums of the sinks' dk and dv by pieces (null: none), see win_sink_kernel
+  uint32_t pieces;
   uint32_t heads, kv_heads, group, hb;      // hb: query heads of one key head that a block works on
   uint32_t batch, sq, sk, window, sinks, rows, rows_q;
   uint32_t ld_q, ld_k, ld_v, ld_o, ld_do, ld_dq, ld_dk, ld_dv;
@@ -306,6 +308,155 @@ __global__ __launch_bounds__(AT_THREADS, 2) void win_dq_kernel(WinArgs a) {
   at_store_tile<DH>(stage, dqacc, 1.0f, a.dq + (size_t)(sq.q0 + qw) * a.ld_dq + head * DH, a.ld_dq, rows);
 }
 
+// The part of dk and dv that sink keys get from rows far behind them.  A sequence's first 128 keys are one block of win_dkv_kernel, which
+// goes as far as their windows; the rows from there on see nothing of them but the sinks, all of these, and there are as many as the
+// sequence is long.  They are cut into pieces (a wavefront takes every fourth 32 rows of a piece, 32 sinks in its registers), whose
+// sums are added up afterwards in a fixed order, together with that block's.  Without this the first block of 8192 rows with a
+// window of 1024 had eight times the work of any other: dk and dv of 16 query and 4 key heads took 2216 us.
+template <int DH>
+__device__ __forceinline__ float* win_part(const WinArgs& a, uint32_t unit, uint32_t sub, uint32_t piece) {      // [dk, dv][32 keys][DH]
+  const uint32_t subs = (a.sinks + 31) / 32;
+  return a.part + (((size_t)unit * subs + sub) * (a.pieces + 1) + piece) * (2 * 32 * DH);
+}
+struct WinFar { uint32_t first, steps, per, used; };       // rows from `first` on, 32 at a time (for all query heads), steps of a piece, pieces used
+__device__ __forceinline__ WinFar win_far(const WinArgs& a, const WinSeq& sq) {
+  WinFar f;
+  const int64_t near_end = (int64_t)min(127u, sq.nk - 1) + a.window - ((int64_t)sq.nk - (int64_t)sq.nq);
+  f.first = sq.nk == 0 || near_end >= (int64_t)sq.nq ? sq.nq : (uint32_t)max(near_end, (int64_t)0);
+  f.steps = (sq.nq - f.first + 31) / 32;
+  const uint32_t all = f.steps * a.group;
+  f.per = (all + a.pieces - 1) / a.pieces;
+  f.used = all > 0 ? (all + f.per - 1) / f.per : 0u;
+  return f;
+}
+
+template <int DH>
+__global__ __launch_bounds__(AT_THREADS, 1) void win_sink_kernel(WinArgs a) {
+  constexpr int KS = DH / 16, DT = DH / 32;
+  __shared__ __align__(1024) bf16_t sQ[4][2][32 * DH];
+  __shared__ __align__(1024) bf16_t sDo[4][2][32 * DH];
+  const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), ki = lane & 31, h = lane >> 5;
+  const uint32_t b = blockIdx.x / a.kv_heads, kvh = blockIdx.x % a.kv_heads, kw = blockIdx.y * 32, kv = kw + ki, piece = blockIdx.z;
+  const WinSeq sq = win_seq(a, b);
+  const WinFar far = win_far(a, sq);
+  if (piece >= far.used) return;
+  const uint32_t begin = piece * far.per, end = min(begin + far.per, far.steps * a.group);
+  const float c2 = a.scale * kLog2e;
+  bf16x8 fk[KS], fv[KS];
+  {
+    const uint32_t r = sq.k0 + min(kv, sq.nk - 1);
+    const bf16_t* kp = a.k + (size_t)r * a.ld_k + kvh * DH;
+    const bf16_t* vp = a.v + (size_t)r * a.ld_v + kvh * DH;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      fk[ks] = *reinterpret_cast<const bf16x8*>(kp + ks * 16 + h * 8);
+      fv[ks] = *reinterpret_cast<const bf16x8*>(vp + ks * 16 + h * 8);
+    }
+  }
+  floatx16 dkacc[DT], dvacc[DT];
+#pragma unroll
+  for (int d = 0; d < DT; ++d)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) { dkacc[d][r] = 0.f; dvacc[d][r] = 0.f; }
+  auto fetch = [&](int buf, uint32_t t) {
+    const uint32_t head = kvh * a.group + t / far.steps, q0 = far.first + t % far.steps * 32;
+    at_dma_rows_wave<DH>(sQ[wave][buf], a.q + (size_t)sq.q0 * a.ld_q + head * DH, a.ld_q, q0, sq.nq);
+    at_dma_rows_wave<DH>(sDo[wave][buf], a.d_o + (size_t)sq.q0 * a.ld_do + head * DH, a.ld_do, q0, sq.nq);
+  };
+  uint32_t t = begin + wave;
+  int buf = 0;
+  if (t < end) fetch(0, t);
+  for (; t < end; t += 4, buf ^= 1) {
+    const uint32_t head = kvh * a.group + t / far.steps, q0 = far.first + t % far.steps * 32;
+    // element r of a lane's scores is row q0 + 8 (r / 4) + 4 h + r % 4
+    float lv[16], dl[16];
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const size_t at = (size_t)head * a.rows_q + sq.q0 + min(q0 + (r >> 2) * 8 + h * 4 + (r & 3), sq.nq - 1);
+      lv[r] = a.lse[at] * kLog2e;
+      dl[r] = a.delta[at];
+    }
+    wait_fetches();                                // this wavefront's own rows
+    if (t + 4 < end) fetch(buf ^ 1, t + 4);
+    const bf16_t* q = sQ[wave][buf];
+    const bf16_t* d_o = sDo[wave][buf];
+    floatx16 sacc, pacc;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) { sacc[r] = 0.f; pacc[r] = 0.f; }
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      sacc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(at_frag<DH>(q, ki, ks * 2 + h), fk[ks], sacc, 0, 0, 0);
+      pacc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(at_frag<DH>(d_o, ki, ks * 2 + h), fv[ks], pacc, 0, 0, 0);
+    }
+    float pr[16], ds[16];
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const bool ok = q0 + (r >> 2) * 8 + h * 4 + (r & 3) < sq.nq && kv < a.sinks;
+      const float p = __builtin_amdgcn_exp2f(fmaf(sacc[r], c2, -lv[r]));
+      pr[r] = ok ? p : 0.f;
+      ds[r] = ok ? p * a.scale * (pacc[r] - dl[r]) : 0.f;
+    }
+#pragma unroll
+    for (int s2 = 0; s2 < 2; ++s2) {
+      const bf16x8 fp = at_pack8(pr, 8 * s2), fds = at_pack8(ds, 8 * s2);
+#pragma unroll
+      for (int d = 0; d < DT; ++d) {
+        dvacc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(at_frag_tr<DH>(d_o, d * 32, 16 * s2 + 4 * h), fp, dvacc[d], 0, 0, 0);
+        dkacc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(at_frag_tr<DH>(q, d * 32, 16 * s2 + 4 * h), fds, dkacc[d], 0, 0, 0);
+      }
+    }
+  }
+  // the four wavefronts' sums through LDS: dk, then dv
+  __syncthreads();
+  float* sum = reinterpret_cast<float*>(&sQ[0][0][0]);         // [4][32][DH] floats: as much as sQ and sDo hold half of
+  static_assert(sizeof(sQ) >= 4 * 32 * DH * sizeof(float), "room for four tiles of sums");
+  float* out = win_part<DH>(a, blockIdx.x, blockIdx.y, piece);
+#pragma unroll
+  for (int which = 0; which < 2; ++which) {
+    float* mine = sum + wave * (32 * DH) + ki * DH + h * 4;
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const floatx16& x = which ? dvacc[d] : dkacc[d];
+        *reinterpret_cast<float4*>(mine + d * 32 + g * 8) = make_float4(x[4 * g], x[4 * g + 1], x[4 * g + 2], x[4 * g + 3]);
+      }
+    __syncthreads();
+    for (uint32_t i = threadIdx.x * 4; i < 32 * DH; i += AT_THREADS * 4) {
+      float4 s = *reinterpret_cast<const float4*>(sum + i);
+#pragma unroll
+      for (int w = 1; w < 4; ++w) {
+        const float4 x = *reinterpret_cast<const float4*>(sum + w * (32 * DH) + i);
+        s.x += x.x; s.y += x.y; s.z += x.z; s.w += x.w;
+      }
+      *reinterpret_cast<float4*>(out + which * (32 * DH) + i) = s;
+    }
+    __syncthreads();
+  }
+}
+
+// Adds the pieces up: a block per 32 sinks and result (dk, dv).
+template <int DH>
+__global__ __launch_bounds__(AT_THREADS) void win_sink_join_kernel(WinArgs a) {
+  const uint32_t b = blockIdx.x / a.kv_heads, kvh = blockIdx.x % a.kv_heads, which = blockIdx.z;
+  const WinSeq sq = win_seq(a, b);
+  const WinFar far = win_far(a, sq);
+  bf16_t* out = which ? a.dv : a.dk;
+  const uint32_t ld = which ? a.ld_dv : a.ld_dk;
+  for (uint32_t i = threadIdx.x * 4; i < 32 * DH; i += AT_THREADS * 4) {
+    const uint32_t key = blockIdx.y * 32 + i / DH;
+    if (key >= sq.nk) return;
+    const float* at = win_part<DH>(a, blockIdx.x, blockIdx.y, 0) + which * (32 * DH) + i;
+    float4 s = *reinterpret_cast<const float4*>(at + (size_t)a.pieces * (2 * 32 * DH));      // the first block's own
+#pragma unroll 8
+    for (uint32_t p = 0; p < far.used; ++p) {
+      const float4 x = *reinterpret_cast<const float4*>(at + (size_t)p * (2 * 32 * DH));
+      s.x += x.x; s.y += x.y; s.z += x.z; s.w += x.w;
+    }
+    *reinterpret_cast<uint2*>(out + (size_t)(sq.k0 + key) * ld + kvh * DH + i % DH) = make_uint2(pack_bf2(s.x, s.y), pack_bf2(s.z, s.w));
+  }
+}
+
 // Backward, dk and dv.  A block is 128 keys of a key head, 32 per wavefront; the rows that see them are streamed 64 at a time, query head
 // after query head.
 template <int DH>
@@ -329,7 +480,7 @@ __global__ __launch_bounds__(AT_THREADS, DH == 64 ? 2 : 1) void win_dkv_kernel(W
   // rows (of the sequence) that see one of the block's keys
   const uint32_t kv_last = min(kv_blk + AT_KV, sq.nk) - 1;
   const int32_t row_a = max((int32_t)kv_blk - off, 0);
-  const int64_t row_z = a.window == 0 || kv_blk < a.sinks ? (int64_t)sq.nq : min((int64_t)kv_last + a.window - off, (int64_t)sq.nq);
+  const int64_t row_z = a.window == 0 ? (int64_t)sq.nq : min((int64_t)kv_last + a.window - off, (int64_t)sq.nq);
   const uint32_t q_first = (uint32_t)row_a, q_end = row_z > row_a ? (uint32_t)row_z : q_first;
   const uint32_t steps = (q_end - q_first + AT_QB - 1) / AT_QB, total = steps * a.group;
 
@@ -426,6 +577,17 @@ __global__ __launch_bounds__(AT_THREADS, DH == 64 ? 2 : 1) void win_dkv_kernel(W
   __syncthreads();
   bf16_t* stage = (wave < 2 ? sQ0 : sDo0) + (wave & 1) * (32 * DH);
   const uint32_t rows = kw < sq.nk ? sq.nk - kw : 0u;
+  if (a.part != nullptr && kw < a.sinks) {       // more is to be added to some of these rows: they go on as sums
+    float* part = win_part<DH>(a, blockIdx.x, kw / 32, a.pieces) + ki * DH + h * 4;
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        *reinterpret_cast<float4*>(part + d * 32 + g * 8) = make_float4(dkacc[d][4 * g], dkacc[d][4 * g + 1], dkacc[d][4 * g + 2], dkacc[d][4 * g + 3]);
+        *reinterpret_cast<float4*>(part + 32 * DH + d * 32 + g * 8) = make_float4(dvacc[d][4 * g], dvacc[d][4 * g + 1], dvacc[d][4 * g + 2], dvacc[d][4 * g + 3]);
+      }
+    return;
+  }
   at_store_tile<DH>(stage, dkacc, 1.0f, a.dk + (size_t)(sq.k0 + kw) * a.ld_dk + kvh * DH, a.ld_dk, rows);
   at_store_tile<DH>(stage, dvacc, 1.0f, a.dv + (size_t)(sq.k0 + kw) * a.ld_dv + kvh * DH, a.ld_dv, rows);
 }
@@ -470,7 +632,8 @@ static sif_status win_plan(const char* who, const sif_window_attn_args* a, WinAr
   w->dq = (bf16_t*)a->dq_dev;
   w->dk = (bf16_t*)a->dk_dev;
   w->dv = (bf16_t*)a->dv_dev;
-  w->delta = nullptr;
+  w->delta = w->part = nullptr;
+  w->pieces = 0;
   w->ld_q = a->ld_q; w->ld_k = a->ld_k; w->ld_v = a->ld_v; w->ld_o = a->ld_o;
   w->ld_do = a->ld_do; w->ld_dq = a->ld_dq; w->ld_dk = a->ld_dk; w->ld_dv = a->ld_dv;
   return SIF_OK;
@@ -485,7 +648,20 @@ static sif_status win_check(const char* who, const sif_window_attn_args* a) {
   return SIF_OK;
 }
 
-static uint64_t win_workspace(const WinArgs& w) { return ((uint64_t)w.heads * w.rows_q * sizeof(float) + 255) / 256 * 256; }
+// Workspace of the backward pass: delta, and the sinks' pieces where some row is far enough from them; as many pieces as give the chip two
+// blocks per CU, of at least 8 steps of 32 rows.
+static uint64_t win_workspace(WinArgs& w, uint32_t d_head, void* at) {
+  const uint64_t delta = ((uint64_t)w.heads * w.rows_q * sizeof(float) + 255) / 256 * 256;
+  w.delta = (float*)at;
+  w.part = nullptr;
+  w.pieces = 0;
+  if (w.sinks == 0 || (uint64_t)w.sk <= 127ull + w.window) return delta;
+  const uint64_t units = (uint64_t)w.batch * w.kv_heads, subs = (w.sinks + 31) / 32;
+  const uint64_t steps = (uint64_t)((std::min(w.sq, w.sk - 127 - w.window) + 31) / 32) * w.group;
+  w.pieces = (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>(512 / (units * subs), (steps + 7) / 8));
+  w.part = (float*)((unsigned char*)at + delta);
+  return delta + units * subs * (w.pieces + 1) * (2 * 32 * (uint64_t)d_head * sizeof(float));
+}
 
 }  // namespace sif
 
@@ -507,7 +683,7 @@ sif_status sif_k_window_attn_fwd(const sif_window_attn_args* a, void* stream) {
 
 uint64_t sif_window_attn_bwd_workspace_bytes(const sif_window_attn_args* a) {
   WinArgs w;
-  return win_plan("window_attn_bwd_workspace_bytes", a, &w) == SIF_OK ? win_workspace(w) : 0;
+  return win_plan("window_attn_bwd_workspace_bytes", a, &w) == SIF_OK ? win_workspace(w, a->d_head, nullptr) : 0;
 }
 
 sif_status sif_k_window_attn_bwd(const sif_window_attn_args* a, void* stream) {
@@ -520,9 +696,9 @@ sif_status sif_k_window_attn_bwd(const sif_window_attn_args* a, void* stream) {
     return fail(SIF_E_INVAL, "window_attn_bwd: bad leading dimensions");
   if (!al16(a->do_dev) || !al16(a->dq_dev) || !al16(a->dk_dev) || !al16(a->dv_dev)) return fail(SIF_E_INVAL, "window_attn_bwd: pointers must be 16-byte aligned");
   if (!a->workspace_dev || ((uintptr_t)a->workspace_dev & 255)) return fail(SIF_E_INVAL, "window_attn_bwd: the workspace must be 256-byte aligned");
-  if (a->workspace_bytes < win_workspace(w))
-    return fail(SIF_E_NOMEM, "window_attn_bwd: the workspace holds %llu of %llu bytes", (unsigned long long)a->workspace_bytes, (unsigned long long)win_workspace(w));
-  w.delta = (float*)a->workspace_dev;
+  const uint64_t need = win_workspace(w, a->d_head, a->workspace_dev);
+  if (a->workspace_bytes < need)
+    return fail(SIF_E_NOMEM, "window_attn_bwd: the workspace holds %llu of %llu bytes", (unsigned long long)a->workspace_bytes, (unsigned long long)need);
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   const uint32_t per = AT_Q / w.hb;
   const dim3 gq(w.batch * (w.heads / w.hb), (w.sq + per - 1) / per), gk(w.batch * w.kv_heads, (w.sk + AT_KV - 1) / AT_KV);
@@ -531,7 +707,15 @@ sif_status sif_k_window_attn_bwd(const sif_window_attn_args* a, void* stream) {
   if (sif_status st = check_launch("window_attn_bwd: dq")) return st;
   if (a->d_head == 64) hipLaunchKernelGGL((win_dkv_kernel<64>), gk, dim3(AT_THREADS), 0, s, w);
   else hipLaunchKernelGGL((win_dkv_kernel<128>), gk, dim3(AT_THREADS), 0, s, w);
-  return check_launch("window_attn_bwd: dk and dv");
+  if (sif_status st = check_launch("window_attn_bwd: dk and dv")) return st;
+  if (w.part == nullptr) return SIF_OK;
+  const dim3 gs(w.batch * w.kv_heads, (w.sinks + 31) / 32, w.pieces), gj(w.batch * w.kv_heads, (w.sinks + 31) / 32, 2);
+  if (a->d_head == 64) hipLaunchKernelGGL((win_sink_kernel<64>), gs, dim3(AT_THREADS), 0, s, w);
+  else hipLaunchKernelGGL((win_sink_kernel<128>), gs, dim3(AT_THREADS), 0, s, w);
+  if (sif_status st = check_launch("window_attn_bwd: sinks")) return st;
+  if (a->d_head == 64) hipLaunchKernelGGL((win_sink_join_kernel<64>), gj, dim3(AT_THREADS), 0, s, w);
+  else hipLaunchKernelGGL((win_sink_join_kernel<128>), gj, dim3(AT_THREADS), 0, s, w);
+  return check_launch("window_attn_bwd: sum of the sinks' pieces");
 }
 
 }  // extern "C"
