@@ -22,6 +22,64 @@ namespace sif {
 
 constexpr float kLog2e = 1.44269504088896f, kLn2 = 0.693147180559945f;
 
+// --- LDS tiles of this file ---
+// A fetch instruction writes 1 KB of consecutive LDS: 4 rows of 128 or 8 rows of 64.  Each such group is followed by 16 bytes of nothing,
+// and within it the 16-byte chunks of a row are exchanged (by XOR) by the row's place in the group, so that neither read meets a bank
+// twice: a 16-byte read serves the lanes 0-3, 12-15, 20-27 of 32 in one cycle and the others in the next, sixteen rows that differ
+// modulo 16; the transposing read takes 64 bytes of four rows in its first 32 lanes.  Because the exchange is the same in every group, a
+// lane's addresses are few (rows 8, 16, 32 further are immediate offsets), and they are kept in registers: with attn_tiles.h's layout, free of conflicts for rows
+// of 64 only, rows of 128 need sixteen of them (or conflicts: 88 us instead of TODO for dk and dv of 2 x 16 heads, 2048 rows, window 512).
+constexpr uint32_t kWtGroup = 512 + 8;                     // elements of a group and its gap
+template <int DH, int ROWS> constexpr int kWtTile = ROWS * DH / 512 * kWtGroup;
+template <int DH> __device__ __forceinline__ uint32_t wt_row(uint32_t row) { return DH == 128 ? (row >> 2) * kWtGroup + (row & 3u) * 128 : (row >> 3) * kWtGroup + (row & 7u) * 64; }
+template <int DH> __device__ __forceinline__ uint32_t wt_key(uint32_t row) { return DH == 128 ? (row & 3u) << 2 : (row & 2u) << 1 | ((row >> 2) & 1u) << 1; }
+
+// ROWS rows from row0 on by WAVES wavefronts (this one is number `wave` of them); rows >= limit are row limit - 1 again
+template <int DH, int ROWS, int WAVES>
+__device__ __forceinline__ void wt_fetch(bf16_t* dst, const bf16_t* src, size_t ld, uint32_t row0, uint32_t limit, uint32_t wave) {
+  typedef __attribute__((address_space(3))) void* lds_void_ptr;
+  typedef __attribute__((address_space(1))) const void* global_void_ptr;
+  constexpr int CH = DH / 8, RPI = 64 / CH;
+  const uint32_t lane = threadIdx.x & 63, in_group = lane / CH, c = (lane % CH) ^ wt_key<DH>(in_group);
+#pragma unroll
+  for (int i = 0; i < ROWS / (RPI * WAVES); ++i) {
+    const uint32_t group = i * WAVES + wave, row = row0 + group * RPI + in_group, r = row < limit ? row : limit - 1;
+    __builtin_amdgcn_global_load_lds((global_void_ptr)(src + (size_t)r * ld + c * 8), (lds_void_ptr)(dst + group * kWtGroup), 16, 0, 0);
+  }
+}
+// A lane's places in a tile, in elements: for operands with row = lane % 32 (+ a multiple of 32) and 8 consecutive d, and for operands
+// with row d = lane % 32 whose k elements are tile rows.
+template <int DH> struct WtLane {
+  uint32_t row[4], col[DH / 32];
+  __device__ __forceinline__ WtLane() {
+    const uint32_t lane = threadIdx.x & 63, ki = lane & 31, h = lane >> 5, s = lane & 15;
+#pragma unroll
+    for (uint32_t j = 0; j < 4; ++j) row[j] = wt_row<DH>(ki) + (((DH == 128 ? j * 4 : j * 2) + h) ^ wt_key<DH>(ki)) * 8;
+    const uint32_t r = 4 * h + (s >> 2), d = ((lane >> 4) & 1u) * 16 + 4 * (s & 3u);
+#pragma unroll
+    for (uint32_t t = 0; t < DH / 32; ++t) col[t] = wt_row<DH>(r) + (((t * 4 + (d >> 3)) ^ wt_key<DH>(r)) * 8) + (d & 7u);
+  }
+};
+// A or B operand: rows base + lane % 32 (base a multiple of 32), d = 16 ks + 8 h ..
+template <int DH>
+__device__ __forceinline__ bf16x8 wt_frag(const bf16_t* tile, const WtLane<DH>& l, uint32_t base, int ks) {
+  const bf16_t* p = tile + wt_row<DH>(base);
+  return *reinterpret_cast<const bf16x8*>(DH == 128 ? p + l.row[ks >> 1] + (ks & 1) * 16 : p + l.row[ks]);
+}
+// A operand of a product that contracts over tile rows: operand row d = 32 t + lane % 32, k elements 0..3 the tile rows kb + 4 h .., 4..7
+// the rows kb + 8 + 4 h .. (kb a multiple of 16)
+template <int DH>
+__device__ __forceinline__ bf16x8 wt_frag_tr(const bf16_t* tile, const WtLane<DH>& l, int t, uint32_t kb) {
+  typedef short short4_lds __attribute__((ext_vector_type(4)));
+  typedef short short8_v __attribute__((ext_vector_type(8)));
+  typedef __attribute__((address_space(3))) short4_lds* lds_ptr;
+  const bf16_t* p = tile + wt_row<DH>(kb) + l.col[t];
+  const short4_lds lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)p);
+  const short4_lds hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(p + wt_row<DH>(8)));
+  const short8_v v = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+  return __builtin_bit_cast(bf16x8, v);
+}
+
 struct WinArgs {
   const bf16_t* q; const bf16_t* k; const bf16_t* v;
   bf16_t* o;
@@ -82,10 +140,10 @@ template <int DH> constexpr int kWinKv = DH == 64 ? 128 : 64;        // keys of 
 template <int DH>
 __global__ __launch_bounds__(AT_THREADS, 2) void win_fwd_kernel(WinArgs a) {
   constexpr int KS = DH / 16, DT = DH / 32, KV = kWinKv<DH>, NT = KV / 32;
-  __shared__ __align__(1024) bf16_t sK0[KV * DH];
-  __shared__ __align__(1024) bf16_t sV0[KV * DH];
-  __shared__ __align__(1024) bf16_t sK1[KV * DH];
-  __shared__ __align__(1024) bf16_t sV1[KV * DH];
+  __shared__ __align__(1024) bf16_t sK0[kWtTile<DH, KV>];
+  __shared__ __align__(1024) bf16_t sV0[kWtTile<DH, KV>];
+  __shared__ __align__(1024) bf16_t sK1[kWtTile<DH, KV>];
+  __shared__ __align__(1024) bf16_t sV1[kWtTile<DH, KV>];
   const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), qi = lane & 31, h = lane >> 5;
   const uint32_t units = a.heads / a.hb, b = blockIdx.x / units, head0 = blockIdx.x % units * a.hb, head = head0 + wave % a.hb, kvh = head0 / a.group;
   const WinSeq sq = win_seq(a, b);
@@ -98,6 +156,7 @@ __global__ __launch_bounds__(AT_THREADS, 2) void win_fwd_kernel(WinArgs a) {
   const bf16_t* kbase = a.k + (size_t)sq.k0 * a.ld_k + kvh * DH;
   const bf16_t* vbase = a.v + (size_t)sq.k0 * a.ld_v + kvh * DH;
   const float c2 = a.scale * kLog2e;
+  const WtLane<DH> at;
   const uint32_t sink_tiles = (sp.sinks + KV - 1) / KV, tiles = sink_tiles + (sp.hi > sp.lo ? (sp.hi - sp.lo + KV - 1) / KV : 0u);
 
   bf16x8 fq[KS];
@@ -116,8 +175,8 @@ __global__ __launch_bounds__(AT_THREADS, 2) void win_fwd_kernel(WinArgs a) {
   auto first_of = [&](uint32_t t) { return t < sink_tiles ? t * KV : sp.lo + (t - sink_tiles) * KV; };
   auto end_of = [&](uint32_t t) { return t < sink_tiles ? sp.sinks : sp.hi; };
   auto fetch = [&](bf16_t* sK, bf16_t* sV, uint32_t t) {
-    at_dma_rows<DH, KV>(sK, kbase, a.ld_k, first_of(t), end_of(t));
-    at_dma_rows<DH, KV>(sV, vbase, a.ld_v, first_of(t), end_of(t));
+    wt_fetch<DH, KV, 4>(sK, kbase, a.ld_k, first_of(t), end_of(t), wave);
+    wt_fetch<DH, KV, 4>(sV, vbase, a.ld_v, first_of(t), end_of(t), wave);
   };
   auto tile = [&](const bf16_t* sK, const bf16_t* sV, uint32_t t, auto edge) {
     constexpr bool EDGE = decltype(edge)::value;
@@ -134,7 +193,7 @@ __global__ __launch_bounds__(AT_THREADS, 2) void win_fwd_kernel(WinArgs a) {
       for (int r = 0; r < 16; ++r) sacc[n][r] = 0.f;
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks)
-        sacc[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(at_frag<DH>(sK, n * 32 + qi, ks * 2 + h), fq[ks], sacc[n], 0, 0, 0);
+        sacc[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wt_frag<DH>(sK, at, n * 32, ks), fq[ks], sacc[n], 0, 0, 0);
       if (EDGE) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
@@ -173,7 +232,7 @@ __global__ __launch_bounds__(AT_THREADS, 2) void win_fwd_kernel(WinArgs a) {
         const bf16x8 fp = at_pack8(pt, 8 * s2);
 #pragma unroll
         for (int d = 0; d < DT; ++d)
-          oacc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(at_frag_tr<DH>(sV, d * 32, n * 32 + 16 * s2 + 4 * h), fp, oacc[d], 0, 0, 0);
+          oacc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wt_frag_tr<DH>(sV, at, d, n * 32 + 16 * s2), fp, oacc[d], 0, 0, 0);
       }
     }
   };
@@ -208,10 +267,10 @@ __global__ __launch_bounds__(AT_THREADS, 2) void win_fwd_kernel(WinArgs a) {
 template <int DH>
 __global__ __launch_bounds__(AT_THREADS, 2) void win_dq_kernel(WinArgs a) {
   constexpr int KS = DH / 16, DT = DH / 32, KV = kWinKv<DH>;
-  __shared__ __align__(1024) bf16_t sK0[KV * DH];
-  __shared__ __align__(1024) bf16_t sV0[KV * DH];
-  __shared__ __align__(1024) bf16_t sK1[KV * DH];
-  __shared__ __align__(1024) bf16_t sV1[KV * DH];
+  __shared__ __align__(1024) bf16_t sK0[kWtTile<DH, KV>];
+  __shared__ __align__(1024) bf16_t sV0[kWtTile<DH, KV>];
+  __shared__ __align__(1024) bf16_t sK1[kWtTile<DH, KV>];
+  __shared__ __align__(1024) bf16_t sV1[kWtTile<DH, KV>];
   const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), qi = lane & 31, h = lane >> 5;
   const uint32_t units = a.heads / a.hb, b = blockIdx.x / units, head0 = blockIdx.x % units * a.hb, head = head0 + wave % a.hb, kvh = head0 / a.group;
   const WinSeq sq = win_seq(a, b);
@@ -224,6 +283,7 @@ __global__ __launch_bounds__(AT_THREADS, 2) void win_dq_kernel(WinArgs a) {
   const bf16_t* kbase = a.k + (size_t)sq.k0 * a.ld_k + kvh * DH;
   const bf16_t* vbase = a.v + (size_t)sq.k0 * a.ld_v + kvh * DH;
   const float c2 = a.scale * kLog2e;
+  const WtLane<DH> at;
   const uint32_t sink_tiles = (sp.sinks + KV - 1) / KV, tiles = sink_tiles + (sp.hi > sp.lo ? (sp.hi - sp.lo + KV - 1) / KV : 0u);
 
   bf16x8 fq[KS], fdo[KS];
@@ -255,8 +315,8 @@ __global__ __launch_bounds__(AT_THREADS, 2) void win_dq_kernel(WinArgs a) {
   auto first_of = [&](uint32_t t) { return t < sink_tiles ? t * KV : sp.lo + (t - sink_tiles) * KV; };
   auto end_of = [&](uint32_t t) { return t < sink_tiles ? sp.sinks : sp.hi; };
   auto fetch = [&](bf16_t* sK, bf16_t* sV, uint32_t t) {
-    at_dma_rows<DH, KV>(sK, kbase, a.ld_k, first_of(t), end_of(t));
-    at_dma_rows<DH, KV>(sV, vbase, a.ld_v, first_of(t), end_of(t));
+    wt_fetch<DH, KV, 4>(sK, kbase, a.ld_k, first_of(t), end_of(t), wave);
+    wt_fetch<DH, KV, 4>(sV, vbase, a.ld_v, first_of(t), end_of(t), wave);
   };
   auto turn = [&](const bf16_t* sK, const bf16_t* sV, uint32_t t) {
     const uint32_t kv0 = first_of(t), end = end_of(t);
@@ -270,8 +330,8 @@ __global__ __launch_bounds__(AT_THREADS, 2) void win_dq_kernel(WinArgs a) {
       for (int r = 0; r < 16; ++r) { sacc[r] = 0.f; pacc[r] = 0.f; }
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
-        sacc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(at_frag<DH>(sK, n * 32 + qi, ks * 2 + h), fq[ks], sacc, 0, 0, 0);      // S^T
-        pacc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(at_frag<DH>(sV, n * 32 + qi, ks * 2 + h), fdo[ks], pacc, 0, 0, 0);     // dP^T
+        sacc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wt_frag<DH>(sK, at, n * 32, ks), fq[ks], sacc, 0, 0, 0);      // S^T
+        pacc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wt_frag<DH>(sV, at, n * 32, ks), fdo[ks], pacc, 0, 0, 0);     // dP^T
       }
       float ds[16];
 #pragma unroll
@@ -285,7 +345,7 @@ __global__ __launch_bounds__(AT_THREADS, 2) void win_dq_kernel(WinArgs a) {
         const bf16x8 fds = at_pack8(ds, 8 * s2);
 #pragma unroll
         for (int d = 0; d < DT; ++d)
-          dqacc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(at_frag_tr<DH>(sK, d * 32, n * 32 + 16 * s2 + 4 * h), fds, dqacc[d], 0, 0, 0);
+          dqacc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wt_frag_tr<DH>(sK, at, d, n * 32 + 16 * s2), fds, dqacc[d], 0, 0, 0);
       }
     }
   };
@@ -310,13 +370,15 @@ __global__ __launch_bounds__(AT_THREADS, 2) void win_dq_kernel(WinArgs a) {
 
 // The part of dk and dv that sink keys get from rows far behind them.  A sequence's first 128 keys are one block of win_dkv_kernel, which
 // goes as far as their windows; the rows from there on see nothing of them but the sinks, all of these, and there are as many as the
-// sequence is long.  They are cut into pieces (a wavefront takes every fourth 32 rows of a piece, 32 sinks in its registers), whose
-// sums are added up afterwards in a fixed order, together with that block's.  Without this the first block of 8192 rows with a
-// window of 1024 had eight times the work of any other: dk and dv of 16 query and 4 key heads took 2216 us.
+// sequence is long.  They are cut into pieces (a wavefront takes every fourth 32 rows of a piece, with 16 sinks in its registers:
+// mostly there are no more than a few), whose sums are added up afterwards in a fixed order, together with that block's.  Without this
+// the first block of 8192 rows with a window of 1024 had eight times the work of any other: dk and dv of 16 query and 4 key heads
+// took 2216 us.
+typedef float floatx4 __attribute__((ext_vector_type(4)));
 template <int DH>
-__device__ __forceinline__ float* win_part(const WinArgs& a, uint32_t unit, uint32_t sub, uint32_t piece) {      // [dk, dv][32 keys][DH]
-  const uint32_t subs = (a.sinks + 31) / 32;
-  return a.part + (((size_t)unit * subs + sub) * (a.pieces + 1) + piece) * (2 * 32 * DH);
+__device__ __forceinline__ float* win_part(const WinArgs& a, uint32_t unit, uint32_t sub, uint32_t piece) {      // [dk, dv][16 keys][DH]
+  const uint32_t subs = (a.sinks + 15) / 16;
+  return a.part + (((size_t)unit * subs + sub) * (a.pieces + 1) + piece) * (2 * 16 * DH);
 }
 struct WinFar { uint32_t first, steps, per, used; };       // rows from `first` on, 32 at a time (for all query heads), steps of a piece, pieces used
 __device__ __forceinline__ WinFar win_far(const WinArgs& a, const WinSeq& sq) {
@@ -329,19 +391,39 @@ __device__ __forceinline__ WinFar win_far(const WinArgs& a, const WinSeq& sq) {
   f.used = all > 0 ? (all + f.per - 1) / f.per : 0u;
   return f;
 }
+// The same for 16x16x32 products: rows 16 n + lane % 16 with d = 32 ks + 8 g .. (g = lane / 16); and operand row d = 16 t + lane % 16, k
+// elements 0..3 the tile rows 4 g .., 4..7 the rows 16 + 4 g ..
+template <int DH>
+__device__ __forceinline__ bf16x8 win_frag16(const bf16_t* tile, int n, int ks) {
+  const uint32_t lane = threadIdx.x & 63, row = n * 16 + (lane & 15);
+  return *reinterpret_cast<const bf16x8*>(tile + wt_row<DH>(row) + (((uint32_t)ks * 4 + (lane >> 4)) ^ wt_key<DH>(row)) * 8);
+}
+template <int DH>
+__device__ __forceinline__ bf16x8 win_frag_tr16(const bf16_t* tile, int t) {
+  typedef short short4_lds __attribute__((ext_vector_type(4)));
+  typedef short short8_v __attribute__((ext_vector_type(8)));
+  typedef __attribute__((address_space(3))) short4_lds* lds_ptr;
+  const uint32_t lane = threadIdx.x & 63, s = lane & 15, row = (lane >> 4) * 4 + (s >> 2), d = t * 16 + 4 * (s & 3u);
+  const bf16_t* p = tile + wt_row<DH>(row) + (((d >> 3) ^ wt_key<DH>(row)) * 8) + (d & 7u);
+  const short4_lds lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)p);
+  const short4_lds hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(p + wt_row<DH>(16)));
+  const short8_v v = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+  return __builtin_bit_cast(bf16x8, v);
+}
 
 template <int DH>
-__global__ __launch_bounds__(AT_THREADS, 1) void win_sink_kernel(WinArgs a) {
-  constexpr int KS = DH / 16, DT = DH / 32;
-  __shared__ __align__(1024) bf16_t sQ[4][2][32 * DH];
-  __shared__ __align__(1024) bf16_t sDo[4][2][32 * DH];
-  const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), ki = lane & 31, h = lane >> 5;
-  const uint32_t b = blockIdx.x / a.kv_heads, kvh = blockIdx.x % a.kv_heads, kw = blockIdx.y * 32, kv = kw + ki, piece = blockIdx.z;
+__global__ __launch_bounds__(AT_THREADS, 2) void win_sink_kernel(WinArgs a) {
+  constexpr int KS = DH / 32, DT = DH / 16;
+  __shared__ __align__(1024) bf16_t sQ[4][kWtTile<DH, 32>];
+  __shared__ __align__(1024) bf16_t sDo[4][kWtTile<DH, 32>];
+  const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, g = lane >> 4;
+  const uint32_t b = blockIdx.x / a.kv_heads, kvh = blockIdx.x % a.kv_heads, kv = blockIdx.y * 16 + col, piece = blockIdx.z;
   const WinSeq sq = win_seq(a, b);
   const WinFar far = win_far(a, sq);
   if (piece >= far.used) return;
   const uint32_t begin = piece * far.per, end = min(begin + far.per, far.steps * a.group);
   const float c2 = a.scale * kLog2e;
+  const bool kv_ok = kv < a.sinks;
   bf16x8 fk[KS], fv[KS];
   {
     const uint32_t r = sq.k0 + min(kv, sq.nk - 1);
@@ -349,152 +431,136 @@ __global__ __launch_bounds__(AT_THREADS, 1) void win_sink_kernel(WinArgs a) {
     const bf16_t* vp = a.v + (size_t)r * a.ld_v + kvh * DH;
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
-      fk[ks] = *reinterpret_cast<const bf16x8*>(kp + ks * 16 + h * 8);
-      fv[ks] = *reinterpret_cast<const bf16x8*>(vp + ks * 16 + h * 8);
+      fk[ks] = *reinterpret_cast<const bf16x8*>(kp + ks * 32 + g * 8);
+      fv[ks] = *reinterpret_cast<const bf16x8*>(vp + ks * 32 + g * 8);
     }
   }
-  floatx16 dkacc[DT], dvacc[DT];
+  floatx4 dkacc[DT], dvacc[DT];                    // [d][key]: element e is d = 16 t + 4 g + e of key col
 #pragma unroll
-  for (int d = 0; d < DT; ++d)
-#pragma unroll
-    for (int r = 0; r < 16; ++r) { dkacc[d][r] = 0.f; dvacc[d][r] = 0.f; }
-  auto fetch = [&](int buf, uint32_t t) {
+  for (int d = 0; d < DT; ++d) dkacc[d] = dvacc[d] = floatx4{0.f, 0.f, 0.f, 0.f};
+  const bf16_t* q = sQ[wave];
+  const bf16_t* d_o = sDo[wave];
+  for (uint32_t t = begin + wave; t < end; t += 4) {
     const uint32_t head = kvh * a.group + t / far.steps, q0 = far.first + t % far.steps * 32;
-    at_dma_rows_wave<DH>(sQ[wave][buf], a.q + (size_t)sq.q0 * a.ld_q + head * DH, a.ld_q, q0, sq.nq);
-    at_dma_rows_wave<DH>(sDo[wave][buf], a.d_o + (size_t)sq.q0 * a.ld_do + head * DH, a.ld_do, q0, sq.nq);
-  };
-  uint32_t t = begin + wave;
-  int buf = 0;
-  if (t < end) fetch(0, t);
-  for (; t < end; t += 4, buf ^= 1) {
-    const uint32_t head = kvh * a.group + t / far.steps, q0 = far.first + t % far.steps * 32;
-    // element r of a lane's scores is row q0 + 8 (r / 4) + 4 h + r % 4
-    float lv[16], dl[16];
+    wt_fetch<DH, 32, 1>(sQ[wave], a.q + (size_t)sq.q0 * a.ld_q + head * DH, a.ld_q, q0, sq.nq, 0);
+    wt_fetch<DH, 32, 1>(sDo[wave], a.d_o + (size_t)sq.q0 * a.ld_do + head * DH, a.ld_do, q0, sq.nq, 0);
+    float lv[2][4], dl[2][4];                      // of rows 16 n + 4 g + e
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      const size_t at = (size_t)head * a.rows_q + sq.q0 + min(q0 + (r >> 2) * 8 + h * 4 + (r & 3), sq.nq - 1);
-      lv[r] = a.lse[at] * kLog2e;
-      dl[r] = a.delta[at];
-    }
+    for (int n = 0; n < 2; ++n)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const size_t at = (size_t)head * a.rows_q + sq.q0 + min(q0 + n * 16 + g * 4 + e, sq.nq - 1);
+        lv[n][e] = a.lse[at] * kLog2e;
+        dl[n][e] = a.delta[at];
+      }
     wait_fetches();                                // this wavefront's own rows
-    if (t + 4 < end) fetch(buf ^ 1, t + 4);
-    const bf16_t* q = sQ[wave][buf];
-    const bf16_t* d_o = sDo[wave][buf];
-    floatx16 sacc, pacc;
+    uint32_t fp[4], fds[4];
 #pragma unroll
-    for (int r = 0; r < 16; ++r) { sacc[r] = 0.f; pacc[r] = 0.f; }
+    for (int n = 0; n < 2; ++n) {
+      floatx4 s = floatx4{0.f, 0.f, 0.f, 0.f}, p = s;
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) {
-      sacc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(at_frag<DH>(q, ki, ks * 2 + h), fk[ks], sacc, 0, 0, 0);
-      pacc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(at_frag<DH>(d_o, ki, ks * 2 + h), fv[ks], pacc, 0, 0, 0);
-    }
-    float pr[16], ds[16];
-#pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      const bool ok = q0 + (r >> 2) * 8 + h * 4 + (r & 3) < sq.nq && kv < a.sinks;
-      const float p = __builtin_amdgcn_exp2f(fmaf(sacc[r], c2, -lv[r]));
-      pr[r] = ok ? p : 0.f;
-      ds[r] = ok ? p * a.scale * (pacc[r] - dl[r]) : 0.f;
-    }
-#pragma unroll
-    for (int s2 = 0; s2 < 2; ++s2) {
-      const bf16x8 fp = at_pack8(pr, 8 * s2), fds = at_pack8(ds, 8 * s2);
-#pragma unroll
-      for (int d = 0; d < DT; ++d) {
-        dvacc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(at_frag_tr<DH>(d_o, d * 32, 16 * s2 + 4 * h), fp, dvacc[d], 0, 0, 0);
-        dkacc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(at_frag_tr<DH>(q, d * 32, 16 * s2 + 4 * h), fds, dkacc[d], 0, 0, 0);
+      for (int ks = 0; ks < KS; ++ks) {
+        s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(win_frag16<DH>(q, n, ks), fk[ks], s, 0, 0, 0);
+        p = __builtin_amdgcn_mfma_f32_16x16x32_bf16(win_frag16<DH>(d_o, n, ks), fv[ks], p, 0, 0, 0);
       }
+      float pr[4], ds[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const bool ok = kv_ok && q0 + n * 16 + g * 4 + e < sq.nq;
+        const float x = __builtin_amdgcn_exp2f(fmaf(s[e], c2, -lv[n][e]));
+        pr[e] = ok ? x : 0.f;
+        ds[e] = ok ? x * a.scale * (p[e] - dl[n][e]) : 0.f;
+      }
+      fp[2 * n] = pack_bf2(pr[0], pr[1]);
+      fp[2 * n + 1] = pack_bf2(pr[2], pr[3]);
+      fds[2 * n] = pack_bf2(ds[0], ds[1]);
+      fds[2 * n + 1] = pack_bf2(ds[2], ds[3]);
+    }
+    const uint4 vp = make_uint4(fp[0], fp[1], fp[2], fp[3]), vs = make_uint4(fds[0], fds[1], fds[2], fds[3]);
+#pragma unroll
+    for (int d = 0; d < DT; ++d) {
+      dvacc[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(win_frag_tr16<DH>(d_o, d), *reinterpret_cast<const bf16x8*>(&vp), dvacc[d], 0, 0, 0);
+      dkacc[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(win_frag_tr16<DH>(q, d), *reinterpret_cast<const bf16x8*>(&vs), dkacc[d], 0, 0, 0);
     }
   }
-  // the four wavefronts' sums through LDS: dk, then dv
+  // the four wavefronts' sums through LDS: [wavefront][dk, dv][16 keys][DH]
   __syncthreads();
-  float* sum = reinterpret_cast<float*>(&sQ[0][0][0]);         // [4][32][DH] floats: as much as sQ and sDo hold half of
-  static_assert(sizeof(sQ) >= 4 * 32 * DH * sizeof(float), "room for four tiles of sums");
+  float* sum = reinterpret_cast<float*>(&sQ[0][0]);
+  static_assert(sizeof(sQ) >= 4 * 16 * DH * sizeof(float) && sizeof(sDo) >= 4 * 16 * DH * sizeof(float), "room for four wavefronts' sums of one result");
+  float* sum_v = reinterpret_cast<float*>(&sDo[0][0]);
+#pragma unroll
+  for (int d = 0; d < DT; ++d) {
+    *reinterpret_cast<floatx4*>(sum + (wave * 16 + col) * DH + d * 16 + g * 4) = dkacc[d];
+    *reinterpret_cast<floatx4*>(sum_v + (wave * 16 + col) * DH + d * 16 + g * 4) = dvacc[d];
+  }
+  __syncthreads();
   float* out = win_part<DH>(a, blockIdx.x, blockIdx.y, piece);
+  for (uint32_t i = threadIdx.x * 4; i < 2 * 16 * DH; i += AT_THREADS * 4) {
+    const float* from = (i < 16 * DH ? sum : sum_v - 16 * DH) + i;
+    floatx4 s = *reinterpret_cast<const floatx4*>(from);
 #pragma unroll
-  for (int which = 0; which < 2; ++which) {
-    float* mine = sum + wave * (32 * DH) + ki * DH + h * 4;
-#pragma unroll
-    for (int d = 0; d < DT; ++d)
-#pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const floatx16& x = which ? dvacc[d] : dkacc[d];
-        *reinterpret_cast<float4*>(mine + d * 32 + g * 8) = make_float4(x[4 * g], x[4 * g + 1], x[4 * g + 2], x[4 * g + 3]);
-      }
-    __syncthreads();
-    for (uint32_t i = threadIdx.x * 4; i < 32 * DH; i += AT_THREADS * 4) {
-      float4 s = *reinterpret_cast<const float4*>(sum + i);
-#pragma unroll
-      for (int w = 1; w < 4; ++w) {
-        const float4 x = *reinterpret_cast<const float4*>(sum + w * (32 * DH) + i);
-        s.x += x.x; s.y += x.y; s.z += x.z; s.w += x.w;
-      }
-      *reinterpret_cast<float4*>(out + which * (32 * DH) + i) = s;
-    }
-    __syncthreads();
+    for (int w = 1; w < 4; ++w) s += *reinterpret_cast<const floatx4*>(from + w * (16 * DH));
+    *reinterpret_cast<floatx4*>(out + i) = s;
   }
 }
 
-// Adds the pieces up: a block per 32 sinks and result (dk, dv).
+// Adds the pieces up: a block takes 64 vectors of a unit's 16 sinks (dk, then dv), each wavefront every fourth piece.
 template <int DH>
-__global__ __launch_bounds__(AT_THREADS) void win_sink_join_kernel(WinArgs a) {
-  const uint32_t b = blockIdx.x / a.kv_heads, kvh = blockIdx.x % a.kv_heads, which = blockIdx.z;
+__global__ __launch_bounds__(256) void win_sink_join_kernel(WinArgs a) {
+  __shared__ __align__(16) floatx4 s_sum[4][64];
+  const uint32_t b = blockIdx.x / a.kv_heads, kvh = blockIdx.x % a.kv_heads, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const WinSeq sq = win_seq(a, b);
   const WinFar far = win_far(a, sq);
-  bf16_t* out = which ? a.dv : a.dk;
-  const uint32_t ld = which ? a.ld_dv : a.ld_dk;
-  for (uint32_t i = threadIdx.x * 4; i < 32 * DH; i += AT_THREADS * 4) {
-    const uint32_t key = blockIdx.y * 32 + i / DH;
-    if (key >= sq.nk) return;
-    const float* at = win_part<DH>(a, blockIdx.x, blockIdx.y, 0) + which * (32 * DH) + i;
-    float4 s = *reinterpret_cast<const float4*>(at + (size_t)a.pieces * (2 * 32 * DH));      // the first block's own
+  const uint32_t i = (blockIdx.z * 64 + lane) * 4, which = i / (16 * DH), key = blockIdx.y * 16 + i / DH % 16;
+  const float* at = win_part<DH>(a, blockIdx.x, blockIdx.y, 0) + i;
+  floatx4 s = floatx4{0.f, 0.f, 0.f, 0.f};
+  if (blockIdx.y * 16 < sq.nk) {
+    if (wave == 0) s = *reinterpret_cast<const floatx4*>(at + (size_t)a.pieces * (2 * 16 * DH));      // the first block's own
 #pragma unroll 8
-    for (uint32_t p = 0; p < far.used; ++p) {
-      const float4 x = *reinterpret_cast<const float4*>(at + (size_t)p * (2 * 32 * DH));
-      s.x += x.x; s.y += x.y; s.z += x.z; s.w += x.w;
-    }
-    *reinterpret_cast<uint2*>(out + (size_t)(sq.k0 + key) * ld + kvh * DH + i % DH) = make_uint2(pack_bf2(s.x, s.y), pack_bf2(s.z, s.w));
+    for (uint32_t p = wave; p < far.used; p += 4) s += *reinterpret_cast<const floatx4*>(at + (size_t)p * (2 * 16 * DH));
   }
+  s_sum[wave][lane] = s;
+  __syncthreads();
+  if (wave != 0 || key >= sq.nk) return;
+  s = s_sum[0][lane] + s_sum[1][lane] + s_sum[2][lane] + s_sum[3][lane];
+  bf16_t* out = which ? a.dv : a.dk;
+  *reinterpret_cast<uint2*>(out + (size_t)(sq.k0 + key) * (which ? a.ld_dv : a.ld_dk) + kvh * DH + i % DH) = make_uint2(pack_bf2(s[0], s[1]), pack_bf2(s[2], s[3]));
 }
 
-// Backward, dk and dv.  A block is 128 keys of a key head, 32 per wavefront; the rows that see them are streamed 64 at a time, query head
-// after query head.
+// Backward, dk and dv.  A block is 128 keys of a key head; the rows that see them are streamed 64 at a time, query head after query head.
+// Eight wavefronts: 32 keys and 32 of the 64 rows each, the two with the same keys add their sums up at the end.  K and V stay in LDS as
+// well, since with them in registers (64 of heads of 128, beside 128 of sums and 32 of scores) there is room for one wavefront
+// per SIMD only, whose exponentials then hold up its products.
+constexpr int WIN_DKV_THREADS = 512;
 template <int DH>
-__global__ __launch_bounds__(AT_THREADS, DH == 64 ? 2 : 1) void win_dkv_kernel(WinArgs a) {
+__global__ __launch_bounds__(WIN_DKV_THREADS, 2) void win_dkv_kernel(WinArgs a) {
   constexpr int KS = DH / 16, DT = DH / 32;
-  __shared__ __align__(1024) bf16_t sQ0[AT_QB * DH];
-  __shared__ __align__(1024) bf16_t sDo0[AT_QB * DH];
-  __shared__ __align__(1024) bf16_t sQ1[AT_QB * DH];
-  __shared__ __align__(1024) bf16_t sDo1[AT_QB * DH];
+  __shared__ __align__(1024) bf16_t sK[kWtTile<DH, AT_KV>];
+  __shared__ __align__(1024) bf16_t sV[kWtTile<DH, AT_KV>];
+  __shared__ __align__(1024) bf16_t sQ0[kWtTile<DH, AT_QB>];
+  __shared__ __align__(1024) bf16_t sDo0[kWtTile<DH, AT_QB>];
+  __shared__ __align__(1024) bf16_t sQ1[kWtTile<DH, AT_QB>];
+  __shared__ __align__(1024) bf16_t sDo1[kWtTile<DH, AT_QB>];
   __shared__ __align__(16) float sL0[AT_QB];
   __shared__ __align__(16) float sD0[AT_QB];
   __shared__ __align__(16) float sL1[AT_QB];
   __shared__ __align__(16) float sD1[AT_QB];
   const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), ki = lane & 31, h = lane >> 5;
+  const uint32_t part = wave & 3, u = wave >> 2;           // keys 32 part .., rows 32 u .. of a step
   const uint32_t b = blockIdx.x / a.kv_heads, kvh = blockIdx.x % a.kv_heads;
   const WinSeq sq = win_seq(a, b);
-  const uint32_t kv_blk = blockIdx.y * AT_KV, kw = kv_blk + wave * 32, kv = kw + ki;
+  const uint32_t kv_blk = blockIdx.y * AT_KV, kw = kv_blk + part * 32, kv = kw + ki;
   if (kv_blk >= sq.nk) return;
   const int32_t off = (int32_t)sq.nk - (int32_t)sq.nq;
   const float c2 = a.scale * kLog2e;
-  // rows (of the sequence) that see one of the block's keys
+  const WtLane<DH> at;
+  // rows (of the sequence) that see one of the block's keys; of the sinks' only those that see its last key too, or might
   const uint32_t kv_last = min(kv_blk + AT_KV, sq.nk) - 1;
   const int32_t row_a = max((int32_t)kv_blk - off, 0);
   const int64_t row_z = a.window == 0 ? (int64_t)sq.nq : min((int64_t)kv_last + a.window - off, (int64_t)sq.nq);
   const uint32_t q_first = (uint32_t)row_a, q_end = row_z > row_a ? (uint32_t)row_z : q_first;
   const uint32_t steps = (q_end - q_first + AT_QB - 1) / AT_QB, total = steps * a.group;
 
-  bf16x8 fk[KS], fv[KS];
-  {
-    const uint32_t r = sq.k0 + min(kv, sq.nk - 1);
-    const bf16_t* kp = a.k + (size_t)r * a.ld_k + kvh * DH;
-    const bf16_t* vp = a.v + (size_t)r * a.ld_v + kvh * DH;
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks) {
-      fk[ks] = *reinterpret_cast<const bf16x8*>(kp + ks * 16 + h * 8);
-      fv[ks] = *reinterpret_cast<const bf16x8*>(vp + ks * 16 + h * 8);
-    }
-  }
   floatx16 dkacc[DT], dvacc[DT];
 #pragma unroll
   for (int d = 0; d < DT; ++d)
@@ -503,65 +569,66 @@ __global__ __launch_bounds__(AT_THREADS, DH == 64 ? 2 : 1) void win_dkv_kernel(W
 
   auto fetch = [&](bf16_t* sQ, bf16_t* sDo, float* sL, float* sD, uint32_t t) {
     const uint32_t head = kvh * a.group + t / steps, q0 = q_first + t % steps * AT_QB;
-    at_dma_rows<DH, AT_QB>(sQ, a.q + (size_t)sq.q0 * a.ld_q + head * DH, a.ld_q, q0, q_end);
-    at_dma_rows<DH, AT_QB>(sDo, a.d_o + (size_t)sq.q0 * a.ld_do + head * DH, a.ld_do, q0, q_end);
-    if (threadIdx.x < AT_QB) {
-      const size_t at = (size_t)head * a.rows_q + sq.q0 + min(q0 + threadIdx.x, q_end - 1);
-      sL[threadIdx.x] = a.lse[at] * kLog2e;
-      sD[threadIdx.x] = a.delta[at];
+    wt_fetch<DH, AT_QB, 8>(sQ, a.q + (size_t)sq.q0 * a.ld_q + head * DH, a.ld_q, q0, q_end, wave);
+    wt_fetch<DH, AT_QB, 8>(sDo, a.d_o + (size_t)sq.q0 * a.ld_do + head * DH, a.ld_do, q0, q_end, wave);
+    if (wave < 2) {                                        // log sum exp (wavefront 0) and row term (1) of the 64 rows
+      typedef __attribute__((address_space(3))) void* lds_void_ptr;
+      typedef __attribute__((address_space(1))) const void* global_void_ptr;
+      const size_t row = (size_t)head * a.rows_q + sq.q0 + min(q0 + lane, q_end - 1);
+      __builtin_amdgcn_global_load_lds((global_void_ptr)((wave == 0 ? a.lse : a.delta) + row), (lds_void_ptr)(wave == 0 ? sL : sD), 4, 0, 0);
     }
   };
   auto turn = [&](const bf16_t* sQ, const bf16_t* sDo, const float* sL, const float* sD, uint32_t t) {
-    const uint32_t q0 = q_first + t % steps * AT_QB;
+    const uint32_t qu = q_first + t % steps * AT_QB + u * 32;
+    const int32_t pw = (int32_t)qu + off;
+    if (qu >= q_end || win_none(a, pw, kw, 32, sq.nk)) return;
+    const bool need_mask = qu + 32 > q_end || !win_all(a, pw, kw, 32, sq.nk);
+    floatx16 sacc, pacc;
 #pragma unroll
-    for (int u = 0; u < AT_QB / 32; ++u) {
-      const uint32_t qu = q0 + u * 32;
-      const int32_t pw = (int32_t)qu + off;
-      if (qu >= q_end || win_none(a, pw, kw, 32, sq.nk)) continue;
-      const bool need_mask = qu + 32 > q_end || !win_all(a, pw, kw, 32, sq.nk);
-      floatx16 sacc, pacc;
+    for (int r = 0; r < 16; ++r) { sacc[r] = 0.f; pacc[r] = 0.f; }
 #pragma unroll
-      for (int r = 0; r < 16; ++r) { sacc[r] = 0.f; pacc[r] = 0.f; }
+    for (int ks = 0; ks < KS; ++ks) {
+      sacc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wt_frag<DH>(sQ, at, u * 32, ks), wt_frag<DH>(sK, at, part * 32, ks), sacc, 0, 0, 0);      // S  [q][kv]
+      pacc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wt_frag<DH>(sDo, at, u * 32, ks), wt_frag<DH>(sV, at, part * 32, ks), pacc, 0, 0, 0);     // dP [q][kv]
+    }
+    float pr[16], ds[16];
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) {
-        sacc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(at_frag<DH>(sQ, u * 32 + ki, ks * 2 + h), fk[ks], sacc, 0, 0, 0);      // S  [q][kv]
-        pacc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(at_frag<DH>(sDo, u * 32 + ki, ks * 2 + h), fv[ks], pacc, 0, 0, 0);     // dP [q][kv]
+    for (int g = 0; g < 4; ++g) {
+      const float4 l4 = *reinterpret_cast<const float4*>(sL + u * 32 + g * 8 + h * 4);
+      const float4 d4 = *reinterpret_cast<const float4*>(sD + u * 32 + g * 8 + h * 4);
+      const float lv[4] = {l4.x, l4.y, l4.z, l4.w}, dv[4] = {d4.x, d4.y, d4.z, d4.w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int r = g * 4 + e;
+        pr[r] = __builtin_amdgcn_exp2f(fmaf(sacc[r], c2, lv[e] * -kLog2e));
+        ds[r] = pr[r] * a.scale * (pacc[r] - dv[e]);
       }
-      float pr[16], ds[16];
+    }
+    if (need_mask) {
 #pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const float4 l4 = *reinterpret_cast<const float4*>(sL + u * 32 + g * 8 + h * 4);
-        const float4 d4 = *reinterpret_cast<const float4*>(sD + u * 32 + g * 8 + h * 4);
-        const float lv[4] = {l4.x, l4.y, l4.z, l4.w}, dv[4] = {d4.x, d4.y, d4.z, d4.w};
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int r = g * 4 + e;
-          pr[r] = __builtin_amdgcn_exp2f(fmaf(sacc[r], c2, -lv[e]));
-          ds[r] = pr[r] * a.scale * (pacc[r] - dv[e]);
-        }
+      for (int r = 0; r < 16; ++r) {
+        const uint32_t row = qu + (r >> 2) * 8 + h * 4 + (r & 3);
+        const bool ok = row < q_end && win_sees(a, (int32_t)row + off, kv, sq.nk);
+        pr[r] = ok ? pr[r] : 0.f;
+        ds[r] = ok ? ds[r] : 0.f;
       }
-      if (need_mask) {
+    }
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const uint32_t row = qu + (r >> 2) * 8 + h * 4 + (r & 3);
-          const bool ok = row < q_end && win_sees(a, (int32_t)row + off, kv, sq.nk);
-          pr[r] = ok ? pr[r] : 0.f;
-          ds[r] = ok ? ds[r] : 0.f;
-        }
-      }
+    for (int s2 = 0; s2 < 2; ++s2) {
+      const bf16x8 fp = at_pack8(pr, 8 * s2), fds = at_pack8(ds, 8 * s2);
+      const uint32_t qb = u * 32 + 16 * s2;
 #pragma unroll
-      for (int s2 = 0; s2 < 2; ++s2) {
-        const bf16x8 fp = at_pack8(pr, 8 * s2), fds = at_pack8(ds, 8 * s2);
-        const uint32_t qb = u * 32 + 16 * s2 + 4 * h;
-#pragma unroll
-        for (int d = 0; d < DT; ++d) {
-          dvacc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(at_frag_tr<DH>(sDo, d * 32, qb), fp, dvacc[d], 0, 0, 0);      // dV^T
-          dkacc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(at_frag_tr<DH>(sQ, d * 32, qb), fds, dkacc[d], 0, 0, 0);      // dK^T
-        }
+      for (int d = 0; d < DT; ++d) {
+        dvacc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wt_frag_tr<DH>(sDo, at, d, qb), fp, dvacc[d], 0, 0, 0);      // dV^T
+        dkacc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wt_frag_tr<DH>(sQ, at, d, qb), fds, dkacc[d], 0, 0, 0);      // dK^T
       }
     }
   };
-  if (total > 0) fetch(sQ0, sDo0, sL0, sD0, 0);
+  if (total > 0) {
+    wt_fetch<DH, AT_KV, 8>(sK, a.k + (size_t)sq.k0 * a.ld_k + kvh * DH, a.ld_k, kv_blk, sq.nk, wave);
+    wt_fetch<DH, AT_KV, 8>(sV, a.v + (size_t)sq.k0 * a.ld_v + kvh * DH, a.ld_v, kv_blk, sq.nk, wave);
+    fetch(sQ0, sDo0, sL0, sD0, 0);
+  }
   for (uint32_t t = 0; t < total; t += 2) {
     wait_fetches();
     __syncthreads();
@@ -574,20 +641,53 @@ __global__ __launch_bounds__(AT_THREADS, DH == 64 ? 2 : 1) void win_dkv_kernel(W
       turn(sQ1, sDo1, sL1, sD1, t + 1);
     }
   }
-  __syncthreads();
-  bf16_t* stage = (wave < 2 ? sQ0 : sDo0) + (wave & 1) * (32 * DH);
+  // the second four wavefronts' sums go to the first four through LDS (dk in K's and V's place, then dv), as they lie in the registers
+  float4* pass = reinterpret_cast<float4*>(part < 2 ? sK : sV) + (part & 1) * (DT * 4 * 64);
+  static_assert(sizeof(sK) >= 2 * DT * 4 * 64 * sizeof(float4), "room for two wavefronts' sums");
+#pragma unroll
+  for (int which = 0; which < 2; ++which) {
+    __syncthreads();
+    if (u == 1) {
+#pragma unroll
+      for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const floatx16& x = which ? dvacc[d] : dkacc[d];
+          pass[(d * 4 + g) * 64 + lane] = make_float4(x[4 * g], x[4 * g + 1], x[4 * g + 2], x[4 * g + 3]);
+        }
+    }
+    __syncthreads();
+    if (u == 0) {
+#pragma unroll
+      for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const float4 v = pass[(d * 4 + g) * 64 + lane];
+          floatx16& x = which ? dvacc[d] : dkacc[d];
+          x[4 * g] += v.x; x[4 * g + 1] += v.y; x[4 * g + 2] += v.z; x[4 * g + 3] += v.w;
+        }
+    }
+  }
+  if (u == 1) return;
   const uint32_t rows = kw < sq.nk ? sq.nk - kw : 0u;
   if (a.part != nullptr && kw < a.sinks) {       // more is to be added to some of these rows: they go on as sums
-    float* part = win_part<DH>(a, blockIdx.x, kw / 32, a.pieces) + ki * DH + h * 4;
 #pragma unroll
-    for (int d = 0; d < DT; ++d)
+    for (int half = 0; half < 2; ++half) {
+      if (kw + half * 16 >= a.sinks) break;
+      float* part_at = win_part<DH>(a, blockIdx.x, kw / 16 + half, a.pieces) + (ki & 15) * DH + h * 4;
+      if ((ki >> 4) == (uint32_t)half) {
 #pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        *reinterpret_cast<float4*>(part + d * 32 + g * 8) = make_float4(dkacc[d][4 * g], dkacc[d][4 * g + 1], dkacc[d][4 * g + 2], dkacc[d][4 * g + 3]);
-        *reinterpret_cast<float4*>(part + 32 * DH + d * 32 + g * 8) = make_float4(dvacc[d][4 * g], dvacc[d][4 * g + 1], dvacc[d][4 * g + 2], dvacc[d][4 * g + 3]);
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+          for (int g = 0; g < 4; ++g) {
+            *reinterpret_cast<float4*>(part_at + d * 32 + g * 8) = make_float4(dkacc[d][4 * g], dkacc[d][4 * g + 1], dkacc[d][4 * g + 2], dkacc[d][4 * g + 3]);
+            *reinterpret_cast<float4*>(part_at + 16 * DH + d * 32 + g * 8) = make_float4(dvacc[d][4 * g], dvacc[d][4 * g + 1], dvacc[d][4 * g + 2], dvacc[d][4 * g + 3]);
+          }
       }
-    return;
+    }
   }
+  // (rows that the pieces are added to are written again by the launch that adds them up)
+  bf16_t* stage = (part < 2 ? sQ0 : sDo0) + (part & 1) * (32 * DH);
   at_store_tile<DH>(stage, dkacc, 1.0f, a.dk + (size_t)(sq.k0 + kw) * a.ld_dk + kvh * DH, a.ld_dk, rows);
   at_store_tile<DH>(stage, dvacc, 1.0f, a.dv + (size_t)(sq.k0 + kw) * a.ld_dv + kvh * DH, a.ld_dv, rows);
 }
@@ -656,11 +756,11 @@ static uint64_t win_workspace(WinArgs& w, uint32_t d_head, void* at) {
   w.part = nullptr;
   w.pieces = 0;
   if (w.sinks == 0 || (uint64_t)w.sk <= 127ull + w.window) return delta;
-  const uint64_t units = (uint64_t)w.batch * w.kv_heads, subs = (w.sinks + 31) / 32;
+  const uint64_t units = (uint64_t)w.batch * w.kv_heads, subs = (w.sinks + 15) / 16;
   const uint64_t steps = (uint64_t)((std::min(w.sq, w.sk - 127 - w.window) + 31) / 32) * w.group;
   w.pieces = (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>(512 / (units * subs), (steps + 7) / 8));
   w.part = (float*)((unsigned char*)at + delta);
-  return delta + units * subs * (w.pieces + 1) * (2 * 32 * (uint64_t)d_head * sizeof(float));
+  return delta + units * subs * (w.pieces + 1) * (2 * 16 * (uint64_t)d_head * sizeof(float));
 }
 
 }  // namespace sif
@@ -705,11 +805,11 @@ sif_status sif_k_window_attn_bwd(const sif_window_attn_args* a, void* stream) {
   if (a->d_head == 64) hipLaunchKernelGGL((win_dq_kernel<64>), gq, dim3(AT_THREADS), 0, s, w);
   else hipLaunchKernelGGL((win_dq_kernel<128>), gq, dim3(AT_THREADS), 0, s, w);
   if (sif_status st = check_launch("window_attn_bwd: dq")) return st;
-  if (a->d_head == 64) hipLaunchKernelGGL((win_dkv_kernel<64>), gk, dim3(AT_THREADS), 0, s, w);
-  else hipLaunchKernelGGL((win_dkv_kernel<128>), gk, dim3(AT_THREADS), 0, s, w);
+  if (a->d_head == 64) hipLaunchKernelGGL((win_dkv_kernel<64>), gk, dim3(WIN_DKV_THREADS), 0, s, w);
+  else hipLaunchKernelGGL((win_dkv_kernel<128>), gk, dim3(WIN_DKV_THREADS), 0, s, w);
   if (sif_status st = check_launch("window_attn_bwd: dk and dv")) return st;
   if (w.part == nullptr) return SIF_OK;
-  const dim3 gs(w.batch * w.kv_heads, (w.sinks + 31) / 32, w.pieces), gj(w.batch * w.kv_heads, (w.sinks + 31) / 32, 2);
+  const dim3 gs(w.batch * w.kv_heads, (w.sinks + 15) / 16, w.pieces), gj(w.batch * w.kv_heads, (w.sinks + 15) / 16, a->d_head / 8);
   if (a->d_head == 64) hipLaunchKernelGGL((win_sink_kernel<64>), gs, dim3(AT_THREADS), 0, s, w);
   else hipLaunchKernelGGL((win_sink_kernel<128>), gs, dim3(AT_THREADS), 0, s, w);
   if (sif_status st = check_launch("window_attn_bwd: sinks")) return st;
