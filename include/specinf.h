@@ -311,11 +311,11 @@ sif_status sif_k_attn_bwd(const void* qkv_dev, const void* o_dev, const void* d_
 typedef struct sif_window_attn_args {
   uint32_t struct_size;
   uint32_t heads, kv_heads, d_head;   /* heads a multiple of kv_heads; d_head 64 or 128                              */
-  uint32_t batch, seq_q, seq_k;       /* sequence b has the query rows b*seq_q .. and the key rows b*seq_k ..; both >= 1 */
+  uint32_t batch, seq_q, seq_k;       /* sequence b has the query rows b*seq_q .. and the key rows b*seq_k ..; both 1 .. 2^20 */
   uint32_t window;                    /* 0 = no limit                                                                */
   uint32_t sinks;                     /* at most 128                                                                 */
   float scale;                        /* 0 = 1 / sqrt(d_head)                                                        */
-  uint32_t ld_q, ld_k, ld_v, ld_o;    /* elements from a row to the next, multiples of 8; head h in columns h*d_head .. */
+  uint32_t ld_q, ld_k, ld_v, ld_o;    /* elements from a row to the next, multiples of 8, below 2^27; head h in columns h*d_head .. */
   uint32_t ld_do, ld_dq, ld_dk, ld_dv;
   uint32_t rows;                      /* with starts_dev: rows of all tensors                                        */
   uint32_t reserved;

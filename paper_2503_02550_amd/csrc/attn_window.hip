@@ -20,6 +20,7 @@
 
 namespace sif {
 
+constexpr int kSchedMfma = 0x8, kSchedLds = 0x100;      // instruction classes of the scheduling groups (LDS: reads)
 constexpr float kLog2e = 1.44269504088896f, kLn2 = 0.693147180559945f;
 
 // --- LDS tiles of this file ---
@@ -27,20 +28,32 @@ constexpr float kLog2e = 1.44269504088896f, kLn2 = 0.693147180559945f;
 // and within it the 16-byte chunks of a row are exchanged (by XOR) by the row's place in the group, so that neither read meets a bank
 // twice: a 16-byte read serves the lanes 0-3, 12-15, 20-27 of 32 in one cycle and the others in the next, sixteen rows that differ
 // modulo 16; the transposing read takes 64 bytes of four rows in its first 32 lanes.  Because the exchange is the same in every group, a
-// lane's addresses are few (rows 8, 16, 32 further are immediate offsets), and they are kept in registers: with attn_tiles.h's layout, free of conflicts for rows
-// of 64 only, rows of 128 need sixteen of them (or conflicts: 88 us instead of TODO for dk and dv of 2 x 16 heads, 2048 rows, window 512).
+// lane's addresses are few (rows 8, 16, 32 further are immediate offsets) and stay in registers.  (dk and dv of 8192 rows, 16 query and 4
+// key heads of 128, window 1024: 330 us with attn_tiles.h's layout, which is free of conflicts for rows of 64 only, 477 with an exchange by
+// sixteen different keys, whose addresses do not fit the registers, 185 so.)
 constexpr uint32_t kWtGroup = 512 + 8;                     // elements of a group and its gap
 template <int DH, int ROWS> constexpr int kWtTile = ROWS * DH / 512 * kWtGroup;
 template <int DH> __device__ __forceinline__ uint32_t wt_row(uint32_t row) { return DH == 128 ? (row >> 2) * kWtGroup + (row & 3u) * 128 : (row >> 3) * kWtGroup + (row & 7u) * 64; }
 template <int DH> __device__ __forceinline__ uint32_t wt_key(uint32_t row) { return DH == 128 ? (row & 3u) << 2 : (row & 2u) << 1 | ((row >> 2) & 1u) << 1; }
 
-// ROWS rows from row0 on by WAVES wavefronts (this one is number `wave` of them); rows >= limit are row limit - 1 again
+// ROWS rows from row0 on by WAVES wavefronts (this one is number `wave` of them); rows >= limit are row limit - 1 again.  Where none is, a
+// lane's offset is the same in every tile and all else is scalar: the vector units have no address to work out.
 template <int DH, int ROWS, int WAVES>
-__device__ __forceinline__ void wt_fetch(bf16_t* dst, const bf16_t* src, size_t ld, uint32_t row0, uint32_t limit, uint32_t wave) {
+__device__ __forceinline__ void wt_fetch(bf16_t* dst, const bf16_t* src, uint32_t ld, uint32_t row0, uint32_t limit, uint32_t wave) {
   typedef __attribute__((address_space(3))) void* lds_void_ptr;
   typedef __attribute__((address_space(1))) const void* global_void_ptr;
   constexpr int CH = DH / 8, RPI = 64 / CH;
   const uint32_t lane = threadIdx.x & 63, in_group = lane / CH, c = (lane % CH) ^ wt_key<DH>(in_group);
+  if (row0 + ROWS <= limit) {
+    const uint32_t mine = (in_group * ld + c * 8) * 2;                 // bytes; ld < 2^27
+#pragma unroll
+    for (int i = 0; i < ROWS / (RPI * WAVES); ++i) {
+      const uint32_t group = i * WAVES + wave;
+      const char* base = reinterpret_cast<const char*>(src + (size_t)(row0 + group * RPI) * ld);
+      __builtin_amdgcn_global_load_lds((global_void_ptr)(base + mine), (lds_void_ptr)(dst + group * kWtGroup), 16, 0, 0);
+    }
+    return;
+  }
 #pragma unroll
   for (int i = 0; i < ROWS / (RPI * WAVES); ++i) {
     const uint32_t group = i * WAVES + wave, row = row0 + group * RPI + in_group, r = row < limit ? row : limit - 1;
@@ -88,6 +101,7 @@ struct WinArgs {
   const bf16_t* d_o;
   bf16_t* dq; bf16_t* dk; bf16_t* dv;
   float* delta;                      // [heads][query rows]
+  float* lse2;                       // [heads][query rows], minus the log sum exp in base-2 units
   float* part;                       // sums of the sinks' dk and dv by pieces (null: none), see win_sink_kernel
   uint32_t pieces;
   uint32_t heads, kv_heads, group, hb;      // hb: query heads of one key head that a block works on
@@ -140,14 +154,13 @@ template <int DH> constexpr int kWinKv = DH == 64 ? 128 : 64;        // keys of 
 template <int DH>
 __global__ __launch_bounds__(AT_THREADS, 2) void win_fwd_kernel(WinArgs a) {
   constexpr int KS = DH / 16, DT = DH / 32, KV = kWinKv<DH>, NT = KV / 32;
-  __shared__ __align__(1024) bf16_t sK0[kWtTile<DH, KV>];
-  __shared__ __align__(1024) bf16_t sV0[kWtTile<DH, KV>];
-  __shared__ __align__(1024) bf16_t sK1[kWtTile<DH, KV>];
-  __shared__ __align__(1024) bf16_t sV1[kWtTile<DH, KV>];
+  constexpr uint32_t TILE = kWtTile<DH, KV>;
+  __shared__ __align__(1024) bf16_t tiles_lds[4 * TILE];            // K, K, V, V
   const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), qi = lane & 31, h = lane >> 5;
   const uint32_t units = a.heads / a.hb, b = blockIdx.x / units, head0 = blockIdx.x % units * a.hb, head = head0 + wave % a.hb, kvh = head0 / a.group;
   const WinSeq sq = win_seq(a, b);
-  const uint32_t per = AT_Q / a.hb, q_blk = blockIdx.y * per;
+  // (the last rows see the most keys where there is no window: their blocks start first)
+  const uint32_t per = AT_Q / a.hb, q_blk = (gridDim.y - 1 - blockIdx.y) * per;
   if (q_blk >= sq.nq) return;
   const uint32_t qw = q_blk + wave / a.hb * 32, q = qw + qi;
   const int32_t off = (int32_t)sq.nk - (int32_t)sq.nq, pw = (int32_t)qw + off, p = pw + (int32_t)qi;
@@ -174,17 +187,24 @@ __global__ __launch_bounds__(AT_THREADS, 2) void win_fwd_kernel(WinArgs a) {
 
   auto first_of = [&](uint32_t t) { return t < sink_tiles ? t * KV : sp.lo + (t - sink_tiles) * KV; };
   auto end_of = [&](uint32_t t) { return t < sink_tiles ? sp.sinks : sp.hi; };
-  auto fetch = [&](bf16_t* sK, bf16_t* sV, uint32_t t) {
-    wt_fetch<DH, KV, 4>(sK, kbase, a.ld_k, first_of(t), end_of(t), wave);
-    wt_fetch<DH, KV, 4>(sV, vbase, a.ld_v, first_of(t), end_of(t), wave);
+  auto fetch = [&](uint32_t buf, uint32_t t) {
+    wt_fetch<DH, KV, 4>(tiles_lds + buf * TILE, kbase, a.ld_k, first_of(t), end_of(t), wave);
+    wt_fetch<DH, KV, 4>(tiles_lds + (2 + buf) * TILE, vbase, a.ld_v, first_of(t), end_of(t), wave);
   };
-  auto tile = [&](const bf16_t* sK, const bf16_t* sV, uint32_t t, auto edge) {
-    constexpr bool EDGE = decltype(edge)::value;
-    const uint32_t kv0 = first_of(t), end = end_of(t);
+  // (one body for both buffers and for tiles with and without a mask: of several, each had copied all sums on its way in)
+  if (tiles > 0) fetch(0, 0);
+  for (uint32_t t = 0; t < tiles; ++t) {
+    wait_fetches();
+    __syncthreads();                                       // tile t has landed, nobody reads the other buffer any more
+    const uint32_t kv0 = first_of(t), end = end_of(t), buf = t & 1;
+    if (t + 1 < tiles) fetch(buf ^ 1, t + 1);
+    if (win_none(a, pw, kv0, KV, end)) continue;
+    const bf16_t* sK = tiles_lds + buf * TILE;
+    const bf16_t* sV = sK + 2 * TILE;
     floatx16 sacc[NT];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-      if (EDGE && win_none(a, pw, kv0 + n * 32, 32, end)) {
+      if (NT > 2 && win_none(a, pw, kv0 + n * 32, 32, end)) {          // (short windows meet such parts often)
 #pragma unroll
         for (int r = 0; r < 16; ++r) sacc[n][r] = -INFINITY;
         continue;
@@ -192,15 +212,22 @@ __global__ __launch_bounds__(AT_THREADS, 2) void win_fwd_kernel(WinArgs a) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) sacc[n][r] = 0.f;
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks)
-        sacc[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wt_frag<DH>(sK, at, n * 32, ks), fq[ks], sacc[n], 0, 0, 0);
-      if (EDGE) {
+      for (int ks = 0; ks < KS; ++ks) sacc[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wt_frag<DH>(sK, at, n * 32, ks), fq[ks], sacc[n], 0, 0, 0);
+    }
+    if constexpr (NT == 2) {                               // the order of this part: operands are read eight products ahead
+      __builtin_amdgcn_sched_group_barrier(kSchedLds, KS, 0);
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const uint32_t kv = kv0 + n * 32 + (r >> 2) * 8 + h * 4 + (r & 3);
-          sacc[n][r] = win_sees(a, p, kv, end) ? sacc[n][r] : -INFINITY;
-        }
+      for (int i = 0; i < KS; ++i) {
+        __builtin_amdgcn_sched_group_barrier(kSchedMfma, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(kSchedLds, 1, 0);
       }
+      __builtin_amdgcn_sched_group_barrier(kSchedMfma, KS, 0);
+    }
+    if (!win_all(a, pw, kv0, KV, end)) {
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) sacc[n][r] = win_sees(a, p, kv0 + n * 32 + (r >> 2) * 8 + h * 4 + (r & 3), end) ? sacc[n][r] : -INFINITY;
     }
     float mx = -INFINITY;
 #pragma unroll
@@ -215,15 +242,13 @@ __global__ __launch_bounds__(AT_THREADS, 2) void win_fwd_kernel(WinArgs a) {
       const float alpha = __builtin_amdgcn_exp2f(m_run - m_use);
       l_run *= alpha;
 #pragma unroll
-      for (int d = 0; d < DT; ++d)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) oacc[d][r] *= alpha;
+      for (int d = 0; d < DT; ++d) oacc[d] *= alpha;
       m_run = m_new;
     }
     const float m_use = m_run == -INFINITY ? 0.f : m_run;
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-      if (EDGE && win_none(a, pw, kv0 + n * 32, 32, end)) continue;
+      if (NT > 2 && win_none(a, pw, kv0 + n * 32, 32, end)) continue;
       float pt[16];
 #pragma unroll
       for (int r = 0; r < 16; ++r) { pt[r] = __builtin_amdgcn_exp2f(fmaf(sacc[n][r], c2, -m_use)); l_run += pt[r]; }
@@ -231,34 +256,14 @@ __global__ __launch_bounds__(AT_THREADS, 2) void win_fwd_kernel(WinArgs a) {
       for (int s2 = 0; s2 < 2; ++s2) {
         const bf16x8 fp = at_pack8(pt, 8 * s2);
 #pragma unroll
-        for (int d = 0; d < DT; ++d)
-          oacc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wt_frag_tr<DH>(sV, at, d, n * 32 + 16 * s2), fp, oacc[d], 0, 0, 0);
+        for (int d = 0; d < DT; ++d) oacc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wt_frag_tr<DH>(sV, at, d, n * 32 + 16 * s2), fp, oacc[d], 0, 0, 0);
       }
-    }
-  };
-  auto turn = [&](const bf16_t* sK, const bf16_t* sV, uint32_t t) {
-    const uint32_t first = first_of(t), end = end_of(t);
-    if (win_none(a, pw, first, KV, end)) return;
-    if (win_all(a, pw, first, KV, end)) tile(sK, sV, t, std::false_type{});
-    else tile(sK, sV, t, std::true_type{});
-  };
-  if (tiles > 0) fetch(sK0, sV0, 0);
-  for (uint32_t t = 0; t < tiles; t += 2) {
-    wait_fetches();
-    __syncthreads();                                       // tile t has landed, nobody reads buffer 1 any more
-    if (t + 1 < tiles) fetch(sK1, sV1, t + 1);
-    turn(sK0, sV0, t);
-    if (t + 1 < tiles) {
-      wait_fetches();
-      __syncthreads();
-      if (t + 2 < tiles) fetch(sK0, sV0, t + 2);
-      turn(sK1, sV1, t + 1);
     }
   }
   l_run += __shfl_xor(l_run, 32, 64);
   __syncthreads();                                         // nobody reads the last tiles any more: K's buffers stage the output
   const uint32_t rows = qw < q_end ? q_end - qw : 0u;
-  bf16_t* stage = KV == AT_KV ? sK0 + wave * (32 * DH) : (wave < 2 ? sK0 : sK1) + (wave & 1) * (32 * DH);
+  bf16_t* stage = tiles_lds + wave * (32 * DH);
   at_store_tile<DH>(stage, oacc, l_run > 0.f ? 1.0f / l_run : 0.f, a.o + (size_t)(sq.q0 + qw) * a.ld_o + head * DH, a.ld_o, rows);
   if (qi < rows && h == 0 && a.lse != nullptr) a.lse[(size_t)head * a.rows_q + sq.q0 + q] = (m_run + __log2f(l_run)) * kLn2;
 }
@@ -267,14 +272,13 @@ __global__ __launch_bounds__(AT_THREADS, 2) void win_fwd_kernel(WinArgs a) {
 template <int DH>
 __global__ __launch_bounds__(AT_THREADS, 2) void win_dq_kernel(WinArgs a) {
   constexpr int KS = DH / 16, DT = DH / 32, KV = kWinKv<DH>;
-  __shared__ __align__(1024) bf16_t sK0[kWtTile<DH, KV>];
-  __shared__ __align__(1024) bf16_t sV0[kWtTile<DH, KV>];
-  __shared__ __align__(1024) bf16_t sK1[kWtTile<DH, KV>];
-  __shared__ __align__(1024) bf16_t sV1[kWtTile<DH, KV>];
+  constexpr uint32_t TILE = kWtTile<DH, KV>;
+  __shared__ __align__(1024) bf16_t tiles_lds[4 * TILE];            // K, K, V, V
   const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), qi = lane & 31, h = lane >> 5;
   const uint32_t units = a.heads / a.hb, b = blockIdx.x / units, head0 = blockIdx.x % units * a.hb, head = head0 + wave % a.hb, kvh = head0 / a.group;
   const WinSeq sq = win_seq(a, b);
-  const uint32_t per = AT_Q / a.hb, q_blk = blockIdx.y * per;
+  // (the last rows see the most keys where there is no window: their blocks start first)
+  const uint32_t per = AT_Q / a.hb, q_blk = (gridDim.y - 1 - blockIdx.y) * per;
   if (q_blk >= sq.nq) return;
   const uint32_t qw = q_blk + wave / a.hb * 32, q = qw + qi;
   const int32_t off = (int32_t)sq.nk - (int32_t)sq.nq, pw = (int32_t)qw + off, p = pw + (int32_t)qi;
@@ -304,7 +308,10 @@ __global__ __launch_bounds__(AT_THREADS, 2) void win_dq_kernel(WinArgs a) {
   }
   dsum += __shfl_xor(dsum, 32, 64);
   const float lq2 = a.lse[(size_t)head * a.rows_q + row] * kLog2e;
-  if (q < q_end && h == 0) a.delta[(size_t)head * a.rows_q + row] = dsum;
+  if (q < q_end && h == 0) {
+    a.delta[(size_t)head * a.rows_q + row] = dsum;
+    a.lse2[(size_t)head * a.rows_q + row] = -lq2;
+  }
 
   floatx16 dqacc[DT];
 #pragma unroll
@@ -314,17 +321,23 @@ __global__ __launch_bounds__(AT_THREADS, 2) void win_dq_kernel(WinArgs a) {
 
   auto first_of = [&](uint32_t t) { return t < sink_tiles ? t * KV : sp.lo + (t - sink_tiles) * KV; };
   auto end_of = [&](uint32_t t) { return t < sink_tiles ? sp.sinks : sp.hi; };
-  auto fetch = [&](bf16_t* sK, bf16_t* sV, uint32_t t) {
-    wt_fetch<DH, KV, 4>(sK, kbase, a.ld_k, first_of(t), end_of(t), wave);
-    wt_fetch<DH, KV, 4>(sV, vbase, a.ld_v, first_of(t), end_of(t), wave);
+  auto fetch = [&](uint32_t buf, uint32_t t) {
+    wt_fetch<DH, KV, 4>(tiles_lds + buf * TILE, kbase, a.ld_k, first_of(t), end_of(t), wave);
+    wt_fetch<DH, KV, 4>(tiles_lds + (2 + buf) * TILE, vbase, a.ld_v, first_of(t), end_of(t), wave);
   };
-  auto turn = [&](const bf16_t* sK, const bf16_t* sV, uint32_t t) {
-    const uint32_t kv0 = first_of(t), end = end_of(t);
+  if (tiles > 0) fetch(0, 0);
+  for (uint32_t t = 0; t < tiles; ++t) {
+    wait_fetches();
+    __syncthreads();                                       // tile t has landed, nobody reads the other buffer any more
+    const uint32_t kv0 = first_of(t), end = end_of(t), buf = t & 1;
+    if (t + 1 < tiles) fetch(buf ^ 1, t + 1);
+    if (win_none(a, pw, kv0, KV, end)) continue;
+    const bf16_t* sK = tiles_lds + buf * TILE;
+    const bf16_t* sV = sK + 2 * TILE;
 #pragma unroll
     for (int n = 0; n < KV / 32; ++n) {
       const uint32_t first = kv0 + n * 32;
       if (win_none(a, pw, first, 32, end)) continue;
-      const bool need_mask = !win_all(a, pw, first, 32, end);
       floatx16 sacc, pacc;
 #pragma unroll
       for (int r = 0; r < 16; ++r) { sacc[r] = 0.f; pacc[r] = 0.f; }
@@ -335,8 +348,8 @@ __global__ __launch_bounds__(AT_THREADS, 2) void win_dq_kernel(WinArgs a) {
       }
       float ds[16];
 #pragma unroll
-      for (int r = 0; r < 16; ++r) ds[r] = __builtin_amdgcn_exp2f(fmaf(sacc[r], c2, -lq2)) * a.scale * (pacc[r] - dsum);
-      if (need_mask) {
+      for (int r = 0; r < 16; ++r) ds[r] = __builtin_amdgcn_exp2f(fmaf(sacc[r], c2, -lq2)) * (pacc[r] - dsum);      // (the scale is left for the end)
+      if (!win_all(a, pw, first, 32, end)) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) ds[r] = win_sees(a, p, first + (r >> 2) * 8 + h * 4 + (r & 3), end) ? ds[r] : 0.f;
       }
@@ -344,28 +357,14 @@ __global__ __launch_bounds__(AT_THREADS, 2) void win_dq_kernel(WinArgs a) {
       for (int s2 = 0; s2 < 2; ++s2) {
         const bf16x8 fds = at_pack8(ds, 8 * s2);
 #pragma unroll
-        for (int d = 0; d < DT; ++d)
-          dqacc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wt_frag_tr<DH>(sK, at, d, n * 32 + 16 * s2), fds, dqacc[d], 0, 0, 0);
+        for (int d = 0; d < DT; ++d) dqacc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wt_frag_tr<DH>(sK, at, d, n * 32 + 16 * s2), fds, dqacc[d], 0, 0, 0);
       }
-    }
-  };
-  if (tiles > 0) fetch(sK0, sV0, 0);
-  for (uint32_t t = 0; t < tiles; t += 2) {
-    wait_fetches();
-    __syncthreads();
-    if (t + 1 < tiles) fetch(sK1, sV1, t + 1);
-    turn(sK0, sV0, t);
-    if (t + 1 < tiles) {
-      wait_fetches();
-      __syncthreads();
-      if (t + 2 < tiles) fetch(sK0, sV0, t + 2);
-      turn(sK1, sV1, t + 1);
     }
   }
   __syncthreads();
   const uint32_t rows = qw < q_end ? q_end - qw : 0u;
-  bf16_t* stage = KV == AT_KV ? sK0 + wave * (32 * DH) : (wave < 2 ? sK0 : sK1) + (wave & 1) * (32 * DH);
-  at_store_tile<DH>(stage, dqacc, 1.0f, a.dq + (size_t)(sq.q0 + qw) * a.ld_dq + head * DH, a.ld_dq, rows);
+  bf16_t* stage = tiles_lds + wave * (32 * DH);
+  at_store_tile<DH>(stage, dqacc, a.scale, a.dq + (size_t)(sq.q0 + qw) * a.ld_dq + head * DH, a.ld_dq, rows);
 }
 
 // The part of dk and dv that sink keys get from rows far behind them.  A sequence's first 128 keys are one block of win_dkv_kernel, which
@@ -450,7 +449,7 @@ __global__ __launch_bounds__(AT_THREADS, 2) void win_sink_kernel(WinArgs a) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const size_t at = (size_t)head * a.rows_q + sq.q0 + min(q0 + n * 16 + g * 4 + e, sq.nq - 1);
-        lv[n][e] = a.lse[at] * kLog2e;
+        lv[n][e] = a.lse2[at];
         dl[n][e] = a.delta[at];
       }
     wait_fetches();                                // this wavefront's own rows
@@ -467,9 +466,9 @@ __global__ __launch_bounds__(AT_THREADS, 2) void win_sink_kernel(WinArgs a) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const bool ok = kv_ok && q0 + n * 16 + g * 4 + e < sq.nq;
-        const float x = __builtin_amdgcn_exp2f(fmaf(s[e], c2, -lv[n][e]));
+        const float x = __builtin_amdgcn_exp2f(fmaf(s[e], c2, lv[n][e]));
         pr[e] = ok ? x : 0.f;
-        ds[e] = ok ? x * a.scale * (p[e] - dl[n][e]) : 0.f;
+        ds[e] = ok ? x * (p[e] - dl[n][e]) : 0.f;
       }
       fp[2 * n] = pack_bf2(pr[0], pr[1]);
       fp[2 * n + 1] = pack_bf2(pr[2], pr[3]);
@@ -522,7 +521,7 @@ __global__ __launch_bounds__(256) void win_sink_join_kernel(WinArgs a) {
   s_sum[wave][lane] = s;
   __syncthreads();
   if (wave != 0 || key >= sq.nk) return;
-  s = s_sum[0][lane] + s_sum[1][lane] + s_sum[2][lane] + s_sum[3][lane];
+  s = (s_sum[0][lane] + s_sum[1][lane] + s_sum[2][lane] + s_sum[3][lane]) * (which ? 1.0f : a.scale);
   bf16_t* out = which ? a.dv : a.dk;
   *reinterpret_cast<uint2*>(out + (size_t)(sq.k0 + key) * (which ? a.ld_dv : a.ld_dk) + kvh * DH + i % DH) = make_uint2(pack_bf2(s[0], s[1]), pack_bf2(s[2], s[3]));
 }
@@ -535,16 +534,11 @@ constexpr int WIN_DKV_THREADS = 512;
 template <int DH>
 __global__ __launch_bounds__(WIN_DKV_THREADS, 2) void win_dkv_kernel(WinArgs a) {
   constexpr int KS = DH / 16, DT = DH / 32;
+  constexpr uint32_t TILE = kWtTile<DH, AT_QB>;
+  __shared__ __align__(1024) bf16_t rows_lds[4 * TILE];             // q, q, do, do
+  __shared__ __align__(16) float vec_lds[4 * AT_QB];                // log sum exp, row term; twice
   __shared__ __align__(1024) bf16_t sK[kWtTile<DH, AT_KV>];
   __shared__ __align__(1024) bf16_t sV[kWtTile<DH, AT_KV>];
-  __shared__ __align__(1024) bf16_t sQ0[kWtTile<DH, AT_QB>];
-  __shared__ __align__(1024) bf16_t sDo0[kWtTile<DH, AT_QB>];
-  __shared__ __align__(1024) bf16_t sQ1[kWtTile<DH, AT_QB>];
-  __shared__ __align__(1024) bf16_t sDo1[kWtTile<DH, AT_QB>];
-  __shared__ __align__(16) float sL0[AT_QB];
-  __shared__ __align__(16) float sD0[AT_QB];
-  __shared__ __align__(16) float sL1[AT_QB];
-  __shared__ __align__(16) float sD1[AT_QB];
   const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), ki = lane & 31, h = lane >> 5;
   const uint32_t part = wave & 3, u = wave >> 2;           // keys 32 part .., rows 32 u .. of a step
   const uint32_t b = blockIdx.x / a.kv_heads, kvh = blockIdx.x % a.kv_heads;
@@ -567,22 +561,32 @@ __global__ __launch_bounds__(WIN_DKV_THREADS, 2) void win_dkv_kernel(WinArgs a) 
 #pragma unroll
     for (int r = 0; r < 16; ++r) { dkacc[d][r] = 0.f; dvacc[d][r] = 0.f; }
 
-  auto fetch = [&](bf16_t* sQ, bf16_t* sDo, float* sL, float* sD, uint32_t t) {
+  auto fetch = [&](uint32_t buf, uint32_t t) {
     const uint32_t head = kvh * a.group + t / steps, q0 = q_first + t % steps * AT_QB;
-    wt_fetch<DH, AT_QB, 8>(sQ, a.q + (size_t)sq.q0 * a.ld_q + head * DH, a.ld_q, q0, q_end, wave);
-    wt_fetch<DH, AT_QB, 8>(sDo, a.d_o + (size_t)sq.q0 * a.ld_do + head * DH, a.ld_do, q0, q_end, wave);
+    wt_fetch<DH, AT_QB, 8>(rows_lds + buf * TILE, a.q + (size_t)sq.q0 * a.ld_q + head * DH, a.ld_q, q0, q_end, wave);
+    wt_fetch<DH, AT_QB, 8>(rows_lds + (2 + buf) * TILE, a.d_o + (size_t)sq.q0 * a.ld_do + head * DH, a.ld_do, q0, q_end, wave);
     if (wave < 2) {                                        // log sum exp (wavefront 0) and row term (1) of the 64 rows
       typedef __attribute__((address_space(3))) void* lds_void_ptr;
       typedef __attribute__((address_space(1))) const void* global_void_ptr;
       const size_t row = (size_t)head * a.rows_q + sq.q0 + min(q0 + lane, q_end - 1);
-      __builtin_amdgcn_global_load_lds((global_void_ptr)((wave == 0 ? a.lse : a.delta) + row), (lds_void_ptr)(wave == 0 ? sL : sD), 4, 0, 0);
+      __builtin_amdgcn_global_load_lds((global_void_ptr)((wave == 0 ? a.lse2 : a.delta) + row), (lds_void_ptr)(vec_lds + (2 * buf + wave) * AT_QB), 4, 0, 0);
     }
   };
-  auto turn = [&](const bf16_t* sQ, const bf16_t* sDo, const float* sL, const float* sD, uint32_t t) {
-    const uint32_t qu = q_first + t % steps * AT_QB + u * 32;
+  if (total > 0) {
+    wt_fetch<DH, AT_KV, 8>(sK, a.k + (size_t)sq.k0 * a.ld_k + kvh * DH, a.ld_k, kv_blk, sq.nk, wave);
+    wt_fetch<DH, AT_KV, 8>(sV, a.v + (size_t)sq.k0 * a.ld_v + kvh * DH, a.ld_v, kv_blk, sq.nk, wave);
+    fetch(0, 0);
+  }
+  for (uint32_t t = 0; t < total; ++t) {
+    wait_fetches();
+    __syncthreads();                                       // step t has landed, nobody reads the other buffer any more
+    const uint32_t buf = t & 1, qu = q_first + t % steps * AT_QB + u * 32;
+    if (t + 1 < total) fetch(buf ^ 1, t + 1);
     const int32_t pw = (int32_t)qu + off;
-    if (qu >= q_end || win_none(a, pw, kw, 32, sq.nk)) return;
-    const bool need_mask = qu + 32 > q_end || !win_all(a, pw, kw, 32, sq.nk);
+    if (qu >= q_end || win_none(a, pw, kw, 32, sq.nk)) continue;
+    const bf16_t* sQ = rows_lds + buf * TILE;
+    const bf16_t* sDo = sQ + 2 * TILE;
+    const float* sL = vec_lds + 2 * buf * AT_QB + u * 32 + h * 4;
     floatx16 sacc, pacc;
 #pragma unroll
     for (int r = 0; r < 16; ++r) { sacc[r] = 0.f; pacc[r] = 0.f; }
@@ -594,17 +598,17 @@ __global__ __launch_bounds__(WIN_DKV_THREADS, 2) void win_dkv_kernel(WinArgs a) 
     float pr[16], ds[16];
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
-      const float4 l4 = *reinterpret_cast<const float4*>(sL + u * 32 + g * 8 + h * 4);
-      const float4 d4 = *reinterpret_cast<const float4*>(sD + u * 32 + g * 8 + h * 4);
+      const float4 l4 = *reinterpret_cast<const float4*>(sL + g * 8);
+      const float4 d4 = *reinterpret_cast<const float4*>(sL + AT_QB + g * 8);
       const float lv[4] = {l4.x, l4.y, l4.z, l4.w}, dv[4] = {d4.x, d4.y, d4.z, d4.w};
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const int r = g * 4 + e;
-        pr[r] = __builtin_amdgcn_exp2f(fmaf(sacc[r], c2, lv[e] * -kLog2e));
-        ds[r] = pr[r] * a.scale * (pacc[r] - dv[e]);
+        pr[r] = __builtin_amdgcn_exp2f(fmaf(sacc[r], c2, lv[e]));
+        ds[r] = pr[r] * (pacc[r] - dv[e]);
       }
     }
-    if (need_mask) {
+    if (qu + 32 > q_end || !win_all(a, pw, kw, 32, sq.nk)) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         const uint32_t row = qu + (r >> 2) * 8 + h * 4 + (r & 3);
@@ -622,23 +626,6 @@ __global__ __launch_bounds__(WIN_DKV_THREADS, 2) void win_dkv_kernel(WinArgs a) 
         dvacc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wt_frag_tr<DH>(sDo, at, d, qb), fp, dvacc[d], 0, 0, 0);      // dV^T
         dkacc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wt_frag_tr<DH>(sQ, at, d, qb), fds, dkacc[d], 0, 0, 0);      // dK^T
       }
-    }
-  };
-  if (total > 0) {
-    wt_fetch<DH, AT_KV, 8>(sK, a.k + (size_t)sq.k0 * a.ld_k + kvh * DH, a.ld_k, kv_blk, sq.nk, wave);
-    wt_fetch<DH, AT_KV, 8>(sV, a.v + (size_t)sq.k0 * a.ld_v + kvh * DH, a.ld_v, kv_blk, sq.nk, wave);
-    fetch(sQ0, sDo0, sL0, sD0, 0);
-  }
-  for (uint32_t t = 0; t < total; t += 2) {
-    wait_fetches();
-    __syncthreads();
-    if (t + 1 < total) fetch(sQ1, sDo1, sL1, sD1, t + 1);
-    turn(sQ0, sDo0, sL0, sD0, t);
-    if (t + 1 < total) {
-      wait_fetches();
-      __syncthreads();
-      if (t + 2 < total) fetch(sQ0, sDo0, sL0, sD0, t + 2);
-      turn(sQ1, sDo1, sL1, sD1, t + 1);
     }
   }
   // the second four wavefronts' sums go to the first four through LDS (dk in K's and V's place, then dv), as they lie in the registers
@@ -687,8 +674,8 @@ __global__ __launch_bounds__(WIN_DKV_THREADS, 2) void win_dkv_kernel(WinArgs a) 
     }
   }
   // (rows that the pieces are added to are written again by the launch that adds them up)
-  bf16_t* stage = (part < 2 ? sQ0 : sDo0) + (part & 1) * (32 * DH);
-  at_store_tile<DH>(stage, dkacc, 1.0f, a.dk + (size_t)(sq.k0 + kw) * a.ld_dk + kvh * DH, a.ld_dk, rows);
+  bf16_t* stage = rows_lds + part * (32 * DH);
+  at_store_tile<DH>(stage, dkacc, a.scale, a.dk + (size_t)(sq.k0 + kw) * a.ld_dk + kvh * DH, a.ld_dk, rows);
   at_store_tile<DH>(stage, dvacc, 1.0f, a.dv + (size_t)(sq.k0 + kw) * a.ld_dv + kvh * DH, a.ld_dv, rows);
 }
 
@@ -702,7 +689,7 @@ static sif_status win_plan(const char* who, const sif_window_attn_args* a, WinAr
   if (a->d_head != 64 && a->d_head != 128) return fail(SIF_E_INVAL, "%s: d_head must be 64 or 128", who);
   if (!a->batch || !a->seq_q || !a->seq_k) return fail(SIF_E_INVAL, "%s: empty extent", who);
   if (a->heads > 1024) return fail(SIF_E_INVAL, "%s: at most 1024 heads", who);
-  if (a->seq_q > (1u << 21) || a->seq_k > (1u << 21)) return fail(SIF_E_INVAL, "%s: sequences of at most 2^21 rows", who);
+  if (a->seq_q > (1u << 20) || a->seq_k > (1u << 20)) return fail(SIF_E_INVAL, "%s: sequences of at most 2^20 rows", who);
   if ((uint64_t)a->batch * a->heads > 0x7FFFFFFFull || (uint64_t)a->batch * a->seq_q > 0x7FFFFFFFull || (uint64_t)a->batch * a->seq_k > 0x7FFFFFFFull)
     return fail(SIF_E_INVAL, "%s: rows or heads beyond 31 bits", who);
   if (a->sinks > 128) return fail(SIF_E_INVAL, "%s: at most 128 sinks", who);
@@ -732,7 +719,7 @@ static sif_status win_plan(const char* who, const sif_window_attn_args* a, WinAr
   w->dq = (bf16_t*)a->dq_dev;
   w->dk = (bf16_t*)a->dk_dev;
   w->dv = (bf16_t*)a->dv_dev;
-  w->delta = w->part = nullptr;
+  w->delta = w->lse2 = w->part = nullptr;
   w->pieces = 0;
   w->ld_q = a->ld_q; w->ld_k = a->ld_k; w->ld_v = a->ld_v; w->ld_o = a->ld_o;
   w->ld_do = a->ld_do; w->ld_dq = a->ld_dq; w->ld_dk = a->ld_dk; w->ld_dv = a->ld_dv;
@@ -743,16 +730,18 @@ static sif_status win_check(const char* who, const sif_window_attn_args* a) {
   const uint32_t wq = a->heads * a->d_head, wk = a->kv_heads * a->d_head;
   if (!a->q_dev || !a->k_dev || !a->v_dev || !a->o_dev) return fail(SIF_E_INVAL, "%s: null operand", who);
   if (a->ld_q < wq || a->ld_o < wq || a->ld_k < wk || a->ld_v < wk || ((a->ld_q | a->ld_o | a->ld_k | a->ld_v) & 7)) return fail(SIF_E_INVAL, "%s: bad leading dimensions", who);
+  if ((a->ld_q | a->ld_k | a->ld_v | a->ld_do) >> 27) return fail(SIF_E_INVAL, "%s: leading dimensions below 2^27", who);
   if (!al16(a->q_dev) || !al16(a->k_dev) || !al16(a->v_dev) || !al16(a->o_dev)) return fail(SIF_E_INVAL, "%s: pointers must be 16-byte aligned", who);
   if ((uintptr_t)a->lse_dev & 3) return fail(SIF_E_INVAL, "%s: misaligned lse", who);
   return SIF_OK;
 }
 
-// Workspace of the backward pass: delta, and the sinks' pieces where some row is far enough from them; as many pieces as give the chip two
+// Workspace of the backward pass: delta and log sum exp per row, and the sinks' pieces where some row is far enough from them; as many pieces as give the chip two
 // blocks per CU, of at least 8 steps of 32 rows.
 static uint64_t win_workspace(WinArgs& w, uint32_t d_head, void* at) {
-  const uint64_t delta = ((uint64_t)w.heads * w.rows_q * sizeof(float) + 255) / 256 * 256;
+  const uint64_t rows = (uint64_t)w.heads * w.rows_q, delta = (2 * rows * sizeof(float) + 255) / 256 * 256;
   w.delta = (float*)at;
+  w.lse2 = w.delta + rows;
   w.part = nullptr;
   w.pieces = 0;
   if (w.sinks == 0 || (uint64_t)w.sk <= 127ull + w.window) return delta;

@@ -19,7 +19,7 @@ def _window(**change):
 
 
 BAD_WINDOW = [dict(struct_size=8), dict(heads=0), dict(kv_heads=0), dict(heads=3), dict(d_head=32), dict(d_head=96), dict(d_head=256), dict(batch=0), dict(seq_q=0),
-              dict(seq_k=0), dict(seq_q=(1 << 21) + 1), dict(batch=1 << 31, heads=4), dict(sinks=129), dict(window=(1 << 30) + 1), dict(scale=-1.0), dict(scale=float("nan")),
+              dict(seq_k=0), dict(seq_q=(1 << 20) + 1), dict(batch=1 << 31, heads=4), dict(sinks=129), dict(window=(1 << 30) + 1), dict(scale=-1.0), dict(scale=float("nan")),
               dict(scale=float("inf")), dict(heads=2048, kv_heads=2), dict(q_dev=None), dict(k_dev=None), dict(v_dev=None), dict(o_dev=None), dict(ld_q=248), dict(ld_k=120),
               dict(ld_v=129), dict(ld_o=260), dict(q_dev=8), dict(o_dev=4), dict(lse_dev=2), dict(starts_dev=64, rows=0), dict(starts_dev=64, rows=64, seq_q=32),
               dict(starts_dev=66, rows=64)]
