@@ -307,11 +307,14 @@ sif_status sif_k_attn_bwd(const void* qkv_dev, const void* o_dev, const void* d_
  * A query that sees no key (seq_q > seq_k) gets o = 0, lse = -inf and passes no gradient on.  What stands in keys that no query sees
  * has no influence, whatever it is.
  * Query head h reads key/value head h / (heads / kv_heads).  bf16 operands, fp32 sums and softmax; the probabilities
- * (and, backward, their gradients) are rounded to bf16 as operands of the matrix units, once. */
+ * (and, backward, their gradients) are rounded to bf16 as operands of the matrix units, once; backward takes its row term
+ * rowsum(do .* o) from o as it is stored.  Results must not overlap operands.  A NaN or an infinity in a row of k or v may
+ * reach every query of its sequence as soon as one query sees that row. */
 typedef struct sif_window_attn_args {
   uint32_t struct_size;
   uint32_t heads, kv_heads, d_head;   /* heads a multiple of kv_heads; d_head 64 or 128                              */
-  uint32_t batch, seq_q, seq_k;       /* sequence b has the query rows b*seq_q .. and the key rows b*seq_k ..; both 1 .. 2^20 */
+  uint32_t batch, seq_q, seq_k;       /* sequence b has the query rows b*seq_q .. and the key rows b*seq_k ..; both 1 .. 2^20;
+                                         batch * heads below 2^23                                                     */
   uint32_t window;                    /* 0 = no limit                                                                */
   uint32_t sinks;                     /* at most 128                                                                 */
   float scale;                        /* 0 = 1 / sqrt(d_head)                                                        */
@@ -343,7 +346,7 @@ uint64_t sif_window_attn_bwd_workspace_bytes(const sif_window_attn_args* a);    
  * refs[p] says to how many; refs[p] = 0 is a free page.  The caller owns all of it; the operations below keep it in
  * order on the device, in stream order, without a host synchronisation (they can be captured into a graph).  All of
  * them give the same result every time: pages are taken lowest number first, in the order in which sequences are listed.
- * Two operations on one cache must not overlap.
+ * Two operations on one cache must not overlap, nor one with attention over it.
  * Lists: seqs_dev names n sequences (int32; null = 0 .. n-1).  A sequence number outside 0 .. n_seqs-1, and a
  * sequence that was listed before in the same call, is left out.  status_dev (int32 [n], may be null) receives SIF_OK
  * or what was wrong with an entry; an entry in error changes nothing.  A page number outside 0 .. n_pages-1 in a table row
@@ -376,7 +379,7 @@ sif_status sif_k_kv_extend(const sif_kv_cache* c, const int32_t* seqs_dev, const
                            void* workspace_dev, uint64_t workspace_bytes, void* stream);
 /* Writes the newest tokens' keys and values (bf16 rows of kv_heads * d_head, ld_k / ld_v elements apart) of one layer.
  * Rows starts[i] .. starts[i+1] - 1 (starts_dev int32 [n+1], ascending, within 0 .. rows) are the last tokens of sequence i of the
- * list; starts_dev null: one row each, rows = n.  In SIF_E4M3 a value is divided by its scale, held at +-448 and rounded to
+ * list; starts_dev null: one row each, rows = n.  n and rows are at most 2^27.  In SIF_E4M3 a value is divided by its scale, held at +-448 and rounded to
  * nearest even (NaN stays NaN).  A token that has no page is left out. */
 sif_status sif_k_kv_write(const sif_kv_cache* c, uint32_t layer, const void* k_dev, const void* v_dev, uint32_t ld_k, uint32_t ld_v,
                           const int32_t* seqs_dev, const int32_t* starts_dev, uint32_t n, uint32_t rows, void* stream);
@@ -398,10 +401,11 @@ sif_status sif_k_kv_copy_pages(const sif_kv_cache* c, const int32_t* src_dev, co
 /* --- Attention of one new token per sequence over a paged cache ---------------------------------------------------
  * The query of sequence i of the list stands at its last position, lengths - 1 (its key and value are in the cache); mask,
  * softmax and heads as in sif_k_window_attn_fwd.  Tokens without a page, and tokens past the row of the table, are not visible.  A
- * sequence that sees nothing (empty, or a number outside the table) gets o = 0, lse = -inf.  A sequence may be listed more than once. */
+ * sequence that sees nothing (empty, or a number outside the table) gets o = 0, lse = -inf.  A sequence may be listed more than once.
+ * o must not overlap q. */
 typedef struct sif_attn_decode_args {
   uint32_t struct_size;
-  uint32_t layer, n, heads;           /* n >= 1 sequences; heads a multiple of the cache's kv_heads                    */
+  uint32_t layer, n, heads;           /* n >= 1 sequences; heads a multiple of the cache's kv_heads; n * heads below 2^23 */
   uint32_t window, sinks;             /* window 0 = no limit; any number of sinks                                    */
   uint32_t max_tokens;                /* what the longest listed sequence is expected to hold (0: a whole row of the table).  Only the
                                          division of the work depends on it: a longer sequence is computed all the same */

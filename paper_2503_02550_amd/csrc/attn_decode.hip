@@ -360,7 +360,6 @@ static sif_status decode_plan(const char* who, const sif_kv_cache* c, const sif_
   if (a->struct_size != sizeof(sif_attn_decode_args)) return fail(SIF_E_INVAL, "%s: struct_size", who);
   if (a->layer >= c->layers) return fail(SIF_E_INVAL, "%s: no layer %u", who, a->layer);
   if (!a->n || !a->heads || a->heads % c->kv_heads) return fail(SIF_E_INVAL, "%s: no sequences, or heads not a multiple of kv_heads", who);
-  if (a->n > (1u << 20) || a->heads > (1u << 14)) return fail(SIF_E_INVAL, "%s: at most 2^20 sequences and 2^14 heads", who);
   const uint32_t tok = c->dtype == SIF_E4M3 ? 64u : 32u;
   out->seqs = a->seqs_dev;
   out->layer = a->layer;
@@ -371,7 +370,7 @@ static sif_status decode_plan(const char* who, const sif_kv_cache* c, const sif_
   out->window = a->window;
   out->sinks = a->sinks;
   const uint64_t units = (uint64_t)a->n * c->kv_heads * out->head_tiles;
-  if (units > 0x7FFFFFFFull || (uint64_t)a->n * a->heads > 0x7FFFFFFFull) return fail(SIF_E_INVAL, "%s: too many sequences and heads for one launch", who);
+  if ((uint64_t)a->n * a->heads >= 1ull << 23) return fail(SIF_E_INVAL, "%s: n * heads below 2^23", who);       // threads of a grid stay below 2^32
   uint64_t seen = a->max_tokens != 0 ? a->max_tokens : (uint64_t)c->table_ld * c->page_tokens;
   if (a->window != 0) seen = std::min<uint64_t>(seen, (uint64_t)a->window + a->sinks + 2 * tok);
   const uint64_t steps = std::max<uint64_t>(1, (seen + tok - 1) / tok);

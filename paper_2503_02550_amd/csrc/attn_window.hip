@@ -10,7 +10,10 @@
 // Products, operands and LDS tiles are those of attention.hip.  A block meets only the tiles that one of its rows sees: the sinks', then
 // from the first key of its first row's window to its last row.  Those ranges begin and end exactly there and are not rounded to
 // tiles, and what a fetch would read past the end is the last row again, so that a key or query that nobody sees is never read.
-// Bound by the matrix units, beside which the exponentials take three quarters of the time with heads of 128, all of it with 64.
+// Bound by the matrix and the vector units together: forward with heads of 128 the first are busy 43 % of a SIMD's cycles (of 1.75 GHz,
+// which the chip holds under this load), the second 50 %, backward 42 and 42 (dq), 38 and 30 (dk, dv), and there is little
+// overlap between the two wavefronts of a SIMD.  8192 rows, 16 query and 4 key heads of 128, window 1024: 93, 127, 177 us, that is 690,
+// 760 and 730 TFLOP/s of the products that each kernel needs (a large matrix product reaches 1390 on this card); the sinks' two launches 21.
 #include <math.h>
 #include <algorithm>
 
@@ -150,12 +153,18 @@ __device__ __forceinline__ bool win_sees(const WinArgs& a, int32_t p, uint32_t j
 template <int DH> constexpr int kWinKv = DH == 64 ? 128 : 64;        // keys of a tile: two buffers of K and V are 64 KB
 
 // Forward.  Four wavefronts of 32 rows: hb query heads of a key head (1, 2 or 4), 128 / hb rows each, so that the wavefronts of a
-// block have nearly the same keys and share them.
+// block have nearly the same keys and share them.  (Timing variants at 8192 rows as above: without the exponentials 84 us, without the
+// fetches after the first 82, without both 71.)
 template <int DH>
 __global__ __launch_bounds__(AT_THREADS, 2) void win_fwd_kernel(WinArgs a) {
   constexpr int KS = DH / 16, DT = DH / 32, KV = kWinKv<DH>, NT = KV / 32;
   constexpr uint32_t TILE = kWtTile<DH, KV>;
-  __shared__ __align__(1024) bf16_t tiles_lds[4 * TILE];            // K, K, V, V
+  // (four objects, so that the compiler can tell the buffer that is being filled from the one that is being read: of one, its transposing
+  // reads would wait for the fetches under way)
+  __shared__ __align__(1024) bf16_t sK0[TILE];
+  __shared__ __align__(1024) bf16_t sV0[TILE];
+  __shared__ __align__(1024) bf16_t sK1[TILE];
+  __shared__ __align__(1024) bf16_t sV1[TILE];
   const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), qi = lane & 31, h = lane >> 5;
   const uint32_t units = a.heads / a.hb, b = blockIdx.x / units, head0 = blockIdx.x % units * a.hb, head = head0 + wave % a.hb, kvh = head0 / a.group;
   const WinSeq sq = win_seq(a, b);
@@ -187,20 +196,17 @@ __global__ __launch_bounds__(AT_THREADS, 2) void win_fwd_kernel(WinArgs a) {
 
   auto first_of = [&](uint32_t t) { return t < sink_tiles ? t * KV : sp.lo + (t - sink_tiles) * KV; };
   auto end_of = [&](uint32_t t) { return t < sink_tiles ? sp.sinks : sp.hi; };
-  auto fetch = [&](uint32_t buf, uint32_t t) {
-    wt_fetch<DH, KV, 4>(tiles_lds + buf * TILE, kbase, a.ld_k, first_of(t), end_of(t), wave);
-    wt_fetch<DH, KV, 4>(tiles_lds + (2 + buf) * TILE, vbase, a.ld_v, first_of(t), end_of(t), wave);
+  auto fetch = [&](bf16_t* sK, bf16_t* sV, uint32_t t) {
+    wt_fetch<DH, KV, 4>(sK, kbase, a.ld_k, first_of(t), end_of(t), wave);
+    wt_fetch<DH, KV, 4>(sV, vbase, a.ld_v, first_of(t), end_of(t), wave);
   };
-  // (one body for both buffers and for tiles with and without a mask: of several, each had copied all sums on its way in)
-  if (tiles > 0) fetch(0, 0);
-  for (uint32_t t = 0; t < tiles; ++t) {
+  // (one body for tiles with and without a mask: of two, each copied all sums on its way in)
+  auto turn = [&](const bf16_t* sK, const bf16_t* sV, bf16_t* next_k, bf16_t* next_v, uint32_t t) {
     wait_fetches();
     __syncthreads();                                       // tile t has landed, nobody reads the other buffer any more
-    const uint32_t kv0 = first_of(t), end = end_of(t), buf = t & 1;
-    if (t + 1 < tiles) fetch(buf ^ 1, t + 1);
-    if (win_none(a, pw, kv0, KV, end)) continue;
-    const bf16_t* sK = tiles_lds + buf * TILE;
-    const bf16_t* sV = sK + 2 * TILE;
+    const uint32_t kv0 = first_of(t), end = end_of(t);
+    if (t + 1 < tiles) fetch(next_k, next_v, t + 1);
+    if (win_none(a, pw, kv0, KV, end)) return;
     floatx16 sacc[NT];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
@@ -259,11 +265,17 @@ __global__ __launch_bounds__(AT_THREADS, 2) void win_fwd_kernel(WinArgs a) {
         for (int d = 0; d < DT; ++d) oacc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wt_frag_tr<DH>(sV, at, d, n * 32 + 16 * s2), fp, oacc[d], 0, 0, 0);
       }
     }
+  };
+  if (tiles > 0) fetch(sK0, sV0, 0);
+  for (uint32_t t = 0; t < tiles; t += 2) {
+    turn(sK0, sV0, sK1, sV1, t);
+    if (t + 1 == tiles) break;
+    turn(sK1, sV1, sK0, sV0, t + 1);
   }
   l_run += __shfl_xor(l_run, 32, 64);
   __syncthreads();                                         // nobody reads the last tiles any more: K's buffers stage the output
   const uint32_t rows = qw < q_end ? q_end - qw : 0u;
-  bf16_t* stage = tiles_lds + wave * (32 * DH);
+  bf16_t* stage = KV == AT_KV ? sK0 + wave * (32 * DH) : (wave < 2 ? sK0 : sK1) + (wave & 1) * (32 * DH);
   at_store_tile<DH>(stage, oacc, l_run > 0.f ? 1.0f / l_run : 0.f, a.o + (size_t)(sq.q0 + qw) * a.ld_o + head * DH, a.ld_o, rows);
   if (qi < rows && h == 0 && a.lse != nullptr) a.lse[(size_t)head * a.rows_q + sq.q0 + q] = (m_run + __log2f(l_run)) * kLn2;
 }
@@ -273,7 +285,12 @@ template <int DH>
 __global__ __launch_bounds__(AT_THREADS, 2) void win_dq_kernel(WinArgs a) {
   constexpr int KS = DH / 16, DT = DH / 32, KV = kWinKv<DH>;
   constexpr uint32_t TILE = kWtTile<DH, KV>;
-  __shared__ __align__(1024) bf16_t tiles_lds[4 * TILE];            // K, K, V, V
+  // (four objects, so that the compiler can tell the buffer that is being filled from the one that is being read: of one, its transposing
+  // reads would wait for the fetches under way)
+  __shared__ __align__(1024) bf16_t sK0[TILE];
+  __shared__ __align__(1024) bf16_t sV0[TILE];
+  __shared__ __align__(1024) bf16_t sK1[TILE];
+  __shared__ __align__(1024) bf16_t sV1[TILE];
   const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), qi = lane & 31, h = lane >> 5;
   const uint32_t units = a.heads / a.hb, b = blockIdx.x / units, head0 = blockIdx.x % units * a.hb, head = head0 + wave % a.hb, kvh = head0 / a.group;
   const WinSeq sq = win_seq(a, b);
@@ -321,19 +338,16 @@ __global__ __launch_bounds__(AT_THREADS, 2) void win_dq_kernel(WinArgs a) {
 
   auto first_of = [&](uint32_t t) { return t < sink_tiles ? t * KV : sp.lo + (t - sink_tiles) * KV; };
   auto end_of = [&](uint32_t t) { return t < sink_tiles ? sp.sinks : sp.hi; };
-  auto fetch = [&](uint32_t buf, uint32_t t) {
-    wt_fetch<DH, KV, 4>(tiles_lds + buf * TILE, kbase, a.ld_k, first_of(t), end_of(t), wave);
-    wt_fetch<DH, KV, 4>(tiles_lds + (2 + buf) * TILE, vbase, a.ld_v, first_of(t), end_of(t), wave);
+  auto fetch = [&](bf16_t* sK, bf16_t* sV, uint32_t t) {
+    wt_fetch<DH, KV, 4>(sK, kbase, a.ld_k, first_of(t), end_of(t), wave);
+    wt_fetch<DH, KV, 4>(sV, vbase, a.ld_v, first_of(t), end_of(t), wave);
   };
-  if (tiles > 0) fetch(0, 0);
-  for (uint32_t t = 0; t < tiles; ++t) {
+  auto turn = [&](const bf16_t* sK, const bf16_t* sV, bf16_t* next_k, bf16_t* next_v, uint32_t t) {
     wait_fetches();
     __syncthreads();                                       // tile t has landed, nobody reads the other buffer any more
-    const uint32_t kv0 = first_of(t), end = end_of(t), buf = t & 1;
-    if (t + 1 < tiles) fetch(buf ^ 1, t + 1);
-    if (win_none(a, pw, kv0, KV, end)) continue;
-    const bf16_t* sK = tiles_lds + buf * TILE;
-    const bf16_t* sV = sK + 2 * TILE;
+    const uint32_t kv0 = first_of(t), end = end_of(t);
+    if (t + 1 < tiles) fetch(next_k, next_v, t + 1);
+    if (win_none(a, pw, kv0, KV, end)) return;
 #pragma unroll
     for (int n = 0; n < KV / 32; ++n) {
       const uint32_t first = kv0 + n * 32;
@@ -360,10 +374,16 @@ __global__ __launch_bounds__(AT_THREADS, 2) void win_dq_kernel(WinArgs a) {
         for (int d = 0; d < DT; ++d) dqacc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wt_frag_tr<DH>(sK, at, d, n * 32 + 16 * s2), fds, dqacc[d], 0, 0, 0);
       }
     }
+  };
+  if (tiles > 0) fetch(sK0, sV0, 0);
+  for (uint32_t t = 0; t < tiles; t += 2) {
+    turn(sK0, sV0, sK1, sV1, t);
+    if (t + 1 == tiles) break;
+    turn(sK1, sV1, sK0, sV0, t + 1);
   }
   __syncthreads();
   const uint32_t rows = qw < q_end ? q_end - qw : 0u;
-  bf16_t* stage = tiles_lds + wave * (32 * DH);
+  bf16_t* stage = KV == AT_KV ? sK0 + wave * (32 * DH) : (wave < 2 ? sK0 : sK1) + (wave & 1) * (32 * DH);
   at_store_tile<DH>(stage, dqacc, a.scale, a.dq + (size_t)(sq.q0 + qw) * a.ld_dq + head * DH, a.ld_dq, rows);
 }
 
@@ -529,14 +549,18 @@ __global__ __launch_bounds__(256) void win_sink_join_kernel(WinArgs a) {
 // Backward, dk and dv.  A block is 128 keys of a key head; the rows that see them are streamed 64 at a time, query head after query head.
 // Eight wavefronts: 32 keys and 32 of the 64 rows each, the two with the same keys add their sums up at the end.  K and V stay in LDS as
 // well, since with them in registers (64 of heads of 128, beside 128 of sums and 32 of scores) there is room for one wavefront
-// per SIMD only, whose exponentials then hold up its products.
+// per SIMD only, whose exponentials then hold up its products (8192 rows as above: 290 us, so 177).
 constexpr int WIN_DKV_THREADS = 512;
 template <int DH>
 __global__ __launch_bounds__(WIN_DKV_THREADS, 2) void win_dkv_kernel(WinArgs a) {
   constexpr int KS = DH / 16, DT = DH / 32;
   constexpr uint32_t TILE = kWtTile<DH, AT_QB>;
-  __shared__ __align__(1024) bf16_t rows_lds[4 * TILE];             // q, q, do, do
-  __shared__ __align__(16) float vec_lds[4 * AT_QB];                // log sum exp, row term; twice
+  __shared__ __align__(1024) bf16_t sQ0[TILE];
+  __shared__ __align__(1024) bf16_t sDo0[TILE];
+  __shared__ __align__(1024) bf16_t sQ1[TILE];
+  __shared__ __align__(1024) bf16_t sDo1[TILE];
+  __shared__ __align__(16) float sL0[2 * AT_QB];                    // log sum exp, row term
+  __shared__ __align__(16) float sL1[2 * AT_QB];
   __shared__ __align__(1024) bf16_t sK[kWtTile<DH, AT_KV>];
   __shared__ __align__(1024) bf16_t sV[kWtTile<DH, AT_KV>];
   const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), ki = lane & 31, h = lane >> 5;
@@ -561,32 +585,30 @@ __global__ __launch_bounds__(WIN_DKV_THREADS, 2) void win_dkv_kernel(WinArgs a) 
 #pragma unroll
     for (int r = 0; r < 16; ++r) { dkacc[d][r] = 0.f; dvacc[d][r] = 0.f; }
 
-  auto fetch = [&](uint32_t buf, uint32_t t) {
+  auto fetch = [&](bf16_t* sQ, bf16_t* sDo, float* sL, uint32_t t) {
     const uint32_t head = kvh * a.group + t / steps, q0 = q_first + t % steps * AT_QB;
-    wt_fetch<DH, AT_QB, 8>(rows_lds + buf * TILE, a.q + (size_t)sq.q0 * a.ld_q + head * DH, a.ld_q, q0, q_end, wave);
-    wt_fetch<DH, AT_QB, 8>(rows_lds + (2 + buf) * TILE, a.d_o + (size_t)sq.q0 * a.ld_do + head * DH, a.ld_do, q0, q_end, wave);
+    wt_fetch<DH, AT_QB, 8>(sQ, a.q + (size_t)sq.q0 * a.ld_q + head * DH, a.ld_q, q0, q_end, wave);
+    wt_fetch<DH, AT_QB, 8>(sDo, a.d_o + (size_t)sq.q0 * a.ld_do + head * DH, a.ld_do, q0, q_end, wave);
     if (wave < 2) {                                        // log sum exp (wavefront 0) and row term (1) of the 64 rows
       typedef __attribute__((address_space(3))) void* lds_void_ptr;
       typedef __attribute__((address_space(1))) const void* global_void_ptr;
       const size_t row = (size_t)head * a.rows_q + sq.q0 + min(q0 + lane, q_end - 1);
-      __builtin_amdgcn_global_load_lds((global_void_ptr)((wave == 0 ? a.lse2 : a.delta) + row), (lds_void_ptr)(vec_lds + (2 * buf + wave) * AT_QB), 4, 0, 0);
+      __builtin_amdgcn_global_load_lds((global_void_ptr)((wave == 0 ? a.lse2 : a.delta) + row), (lds_void_ptr)(sL + wave * AT_QB), 4, 0, 0);
     }
   };
   if (total > 0) {
     wt_fetch<DH, AT_KV, 8>(sK, a.k + (size_t)sq.k0 * a.ld_k + kvh * DH, a.ld_k, kv_blk, sq.nk, wave);
     wt_fetch<DH, AT_KV, 8>(sV, a.v + (size_t)sq.k0 * a.ld_v + kvh * DH, a.ld_v, kv_blk, sq.nk, wave);
-    fetch(0, 0);
+    fetch(sQ0, sDo0, sL0, 0);
   }
-  for (uint32_t t = 0; t < total; ++t) {
+  auto turn = [&](const bf16_t* sQ, const bf16_t* sDo, const float* sLd, bf16_t* next_q, bf16_t* next_do, float* next_l, uint32_t t) {
     wait_fetches();
     __syncthreads();                                       // step t has landed, nobody reads the other buffer any more
-    const uint32_t buf = t & 1, qu = q_first + t % steps * AT_QB + u * 32;
-    if (t + 1 < total) fetch(buf ^ 1, t + 1);
+    const uint32_t qu = q_first + t % steps * AT_QB + u * 32;
+    if (t + 1 < total) fetch(next_q, next_do, next_l, t + 1);
     const int32_t pw = (int32_t)qu + off;
-    if (qu >= q_end || win_none(a, pw, kw, 32, sq.nk)) continue;
-    const bf16_t* sQ = rows_lds + buf * TILE;
-    const bf16_t* sDo = sQ + 2 * TILE;
-    const float* sL = vec_lds + 2 * buf * AT_QB + u * 32 + h * 4;
+    if (qu >= q_end || win_none(a, pw, kw, 32, sq.nk)) return;
+    const float* sL = sLd + u * 32 + h * 4;
     floatx16 sacc, pacc;
 #pragma unroll
     for (int r = 0; r < 16; ++r) { sacc[r] = 0.f; pacc[r] = 0.f; }
@@ -627,6 +649,11 @@ __global__ __launch_bounds__(WIN_DKV_THREADS, 2) void win_dkv_kernel(WinArgs a) 
         dkacc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wt_frag_tr<DH>(sQ, at, d, qb), fds, dkacc[d], 0, 0, 0);      // dK^T
       }
     }
+  };
+  for (uint32_t t = 0; t < total; t += 2) {
+    turn(sQ0, sDo0, sL0, sQ1, sDo1, sL1, t);
+    if (t + 1 == total) break;
+    turn(sQ1, sDo1, sL1, sQ0, sDo0, sL0, t + 1);
   }
   // the second four wavefronts' sums go to the first four through LDS (dk in K's and V's place, then dv), as they lie in the registers
   float4* pass = reinterpret_cast<float4*>(part < 2 ? sK : sV) + (part & 1) * (DT * 4 * 64);
@@ -674,7 +701,7 @@ __global__ __launch_bounds__(WIN_DKV_THREADS, 2) void win_dkv_kernel(WinArgs a) 
     }
   }
   // (rows that the pieces are added to are written again by the launch that adds them up)
-  bf16_t* stage = rows_lds + part * (32 * DH);
+  bf16_t* stage = (part < 2 ? sQ0 : sDo0) + (part & 1) * (32 * DH);
   at_store_tile<DH>(stage, dkacc, a.scale, a.dk + (size_t)(sq.k0 + kw) * a.ld_dk + kvh * DH, a.ld_dk, rows);
   at_store_tile<DH>(stage, dvacc, 1.0f, a.dv + (size_t)(sq.k0 + kw) * a.ld_dv + kvh * DH, a.ld_dv, rows);
 }
@@ -690,8 +717,8 @@ static sif_status win_plan(const char* who, const sif_window_attn_args* a, WinAr
   if (!a->batch || !a->seq_q || !a->seq_k) return fail(SIF_E_INVAL, "%s: empty extent", who);
   if (a->heads > 1024) return fail(SIF_E_INVAL, "%s: at most 1024 heads", who);
   if (a->seq_q > (1u << 20) || a->seq_k > (1u << 20)) return fail(SIF_E_INVAL, "%s: sequences of at most 2^20 rows", who);
-  if ((uint64_t)a->batch * a->heads > 0x7FFFFFFFull || (uint64_t)a->batch * a->seq_q > 0x7FFFFFFFull || (uint64_t)a->batch * a->seq_k > 0x7FFFFFFFull)
-    return fail(SIF_E_INVAL, "%s: rows or heads beyond 31 bits", who);
+  if ((uint64_t)a->batch * a->heads >= 1ull << 23) return fail(SIF_E_INVAL, "%s: batch * heads below 2^23", who);       // threads of a grid stay below 2^32
+  if ((uint64_t)a->batch * a->seq_q > 0x7FFFFFFFull || (uint64_t)a->batch * a->seq_k > 0x7FFFFFFFull) return fail(SIF_E_INVAL, "%s: rows beyond 31 bits", who);
   if (a->sinks > 128) return fail(SIF_E_INVAL, "%s: at most 128 sinks", who);
   if (a->window > (1u << 30)) return fail(SIF_E_INVAL, "%s: a window of at most 2^30 (0: no limit)", who);
   if (!(a->scale >= 0.f) || !std::isfinite(a->scale)) return fail(SIF_E_INVAL, "%s: scale must be finite and not negative", who);

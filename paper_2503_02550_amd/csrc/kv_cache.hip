@@ -497,7 +497,7 @@ sif_status sif_k_kv_write(const sif_kv_cache* c, uint32_t layer, const void* k, 
   if (sif_status st = kv_check("kv_write", c, &w)) return st;
   if (layer >= w.layers) return fail(SIF_E_INVAL, "kv_write: no layer %u", layer);
   if (!k || !v || (((uintptr_t)k | (uintptr_t)v) & 15)) return fail(SIF_E_INVAL, "kv_write: k and v must be 16-byte aligned");
-  if (n == 0 || rows == 0 || n > 0x7FFFFFFEu || rows > 0x7FFFFFFFu) return fail(SIF_E_INVAL, "kv_write: entries or rows outside 1 .. 2^31 - 2");
+  if (n == 0 || rows == 0 || n > (1u << 27) || rows > (1u << 27)) return fail(SIF_E_INVAL, "kv_write: entries or rows outside 1 .. 2^27");
   if (starts == nullptr && rows != n) return fail(SIF_E_INVAL, "kv_write: without starts there is one row per entry");
   const uint32_t width = w.kv_heads * w.d_head;
   if (ld_k < width || ld_v < width || ((ld_k | ld_v) & 7)) return fail(SIF_E_INVAL, "kv_write: bad leading dimensions");

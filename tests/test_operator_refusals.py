@@ -19,9 +19,9 @@ def _window(**change):
 
 
 BAD_WINDOW = [dict(struct_size=8), dict(heads=0), dict(kv_heads=0), dict(heads=3), dict(d_head=32), dict(d_head=96), dict(d_head=256), dict(batch=0), dict(seq_q=0),
-              dict(seq_k=0), dict(seq_q=(1 << 20) + 1), dict(batch=1 << 31, heads=4), dict(sinks=129), dict(window=(1 << 30) + 1), dict(scale=-1.0), dict(scale=float("nan")),
+              dict(seq_k=0), dict(seq_q=(1 << 20) + 1), dict(batch=1 << 21), dict(sinks=129), dict(window=(1 << 30) + 1), dict(scale=-1.0), dict(scale=float("nan")),
               dict(scale=float("inf")), dict(heads=2048, kv_heads=2), dict(q_dev=None), dict(k_dev=None), dict(v_dev=None), dict(o_dev=None), dict(ld_q=248), dict(ld_k=120),
-              dict(ld_v=129), dict(ld_o=260), dict(q_dev=8), dict(o_dev=4), dict(lse_dev=2), dict(starts_dev=64, rows=0), dict(starts_dev=64, rows=64, seq_q=32),
+              dict(ld_v=129), dict(ld_o=260), dict(ld_k=1 << 27), dict(q_dev=8), dict(o_dev=4), dict(lse_dev=2), dict(starts_dev=64, rows=0), dict(starts_dev=64, rows=64, seq_q=32),
               dict(starts_dev=66, rows=64)]
 BAD_BACKWARD = [dict(lse_dev=None), dict(do_dev=None), dict(dq_dev=None), dict(dk_dev=None), dict(dv_dev=None), dict(ld_do=8), dict(ld_dq=252), dict(ld_dk=120), dict(ld_dv=124),
                 dict(do_dev=8), dict(dv_dev=8), dict(workspace_dev=None), dict(workspace_dev=(1 << 20) + 16)]
@@ -124,15 +124,14 @@ def test_page_operations_refuse_bad_lists_and_workspaces():
         assert lib.sif_k_kv_compact(p, work, size, None) == status
 
 
-@pytest.mark.parametrize("change", [dict(layer=2), dict(k=None), dict(v=None), dict(k=8), dict(ld_k=120), dict(ld_v=129), dict(n=0, rows=0), dict(rows=0), dict(rows=3)], ids=str)
+@pytest.mark.parametrize("change", [dict(layer=2), dict(k=None), dict(v=None), dict(k=8), dict(ld_k=120), dict(ld_v=129), dict(n=0, rows=0), dict(rows=0), dict(rows=3), dict(n=(1 << 27) + 1, rows=(1 << 27) + 1)], ids=str)
 def test_write_refuses(change):
     x = dict(dict(layer=0, k=1 << 20, v=1 << 20, ld_k=128, ld_v=128, n=2, rows=2), **change)
     assert S.lib.sif_k_kv_write(C.byref(_cache()), x["layer"], x["k"], x["v"], x["ld_k"], x["ld_v"], None, None, x["n"], x["rows"], None) == S.SIF_E_INVAL
 
 
 @pytest.mark.parametrize("change", [dict(struct_size=4), dict(layer=2), dict(n=0), dict(heads=0), dict(heads=3), dict(q_dev=None), dict(o_dev=None), dict(q_dev=8), dict(o_dev=2),
-                                    dict(lse_dev=2), dict(seqs_dev=1), dict(ld_q=248), dict(ld_o=260), dict(scale=-0.5), dict(scale=float("nan")), dict(n=(1 << 20) + 1),
-                                    dict(heads=(1 << 14) + 2)], ids=str)
+                                    dict(lse_dev=2), dict(seqs_dev=1), dict(ld_q=248), dict(ld_o=260), dict(scale=-0.5), dict(scale=float("nan")), dict(n=1 << 21)], ids=str)
 def test_decode_refuses(change):
     assert S.lib.sif_k_attn_decode(C.byref(_cache()), C.byref(_decode(**change)), None) == S.SIF_E_INVAL
 
