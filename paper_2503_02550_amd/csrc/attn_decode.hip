@@ -24,7 +24,7 @@ namespace sif {
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float floatx4 __attribute__((ext_vector_type(4)));
 
-constexpr uint32_t AD_WAVES = 4, AD_HEADS = 16, AD_MAX_SPLITS = 1024;
+constexpr uint32_t AD_WAVES = 4, AD_HEADS = 16, AD_BLOCKS = 256;      // AD_BLOCKS: a block for each CU, and so the most splits
 constexpr float kNoSplit = -1.0f;       // in the place of a split's sum
 
 struct DecodeArgs {
@@ -33,7 +33,7 @@ struct DecodeArgs {
   const bf16_t* q;
   bf16_t* o;
   float* lse;
-  float* part;                       // [unit][split][16 rows][DH + 2]
+  float* part;                       // [sequence][query head][split][DH + 4]: m, l, -, -, O
   uint32_t layer, n, heads, group, head_tiles, window, sinks, splits, chunk, ld_q, ld_o;      // chunk: steps of a split
   float scale;
 };
@@ -299,7 +299,8 @@ __global__ __launch_bounds__(256, 2) void attn_decode_kernel(DecodeArgs a) {
 template <int DH>
 __global__ __launch_bounds__(256) void attn_decode_join_kernel(DecodeArgs a) {
   constexpr uint32_t LANES = DH / 4, ROWS = 256 / LANES;
-  __shared__ float s_w[AD_MAX_SPLITS], s_l[AD_MAX_SPLITS];
+  static_assert(AD_BLOCKS == 256, "a thread per split");
+  __shared__ float s_w[AD_BLOCKS];
   __shared__ __align__(16) float4 s_o[256];
   __shared__ float sm[16];
   const uint32_t t = threadIdx.x, head = blockIdx.x % a.heads, i = blockIdx.x / a.heads;
@@ -307,32 +308,20 @@ __global__ __launch_bounds__(256) void attn_decode_join_kernel(DecodeArgs a) {
   // Everything that is known only on the device - how many splits the sequence has - stands in the splits themselves: the first
   // `parts` have an l, the others kNoSplit (all of them if one block did the whole sequence).  So there are two rounds of loads, and not the
   // length's and the list's before them.
-  float m = -INFINITY;
-  uint32_t used = 0;
-  for (uint32_t p = t; p < a.splits; p += 256) {
-    const float2 ml = *reinterpret_cast<const float2*>(from + (size_t)p * (DH + 4));
-    const bool here = ml.y != kNoSplit;
-    used += here ? 1u : 0u;
-    s_w[p] = here ? ml.x : -INFINITY;
-    s_l[p] = here ? ml.y : 0.f;
-    m = here ? fmaxf(m, ml.x) : m;
-  }
-  const uint32_t parts = (uint32_t)block_sum((float)used, sm);
+  float2 ml = make_float2(-INFINITY, kNoSplit);
+  if (t < a.splits) ml = *reinterpret_cast<const float2*>(from + (size_t)t * (DH + 4));
+  const bool here = ml.y != kNoSplit;
+  const uint32_t parts = (uint32_t)block_sum(here ? 1.f : 0.f, sm);
   if (parts == 0) return;
-  m = block_max(m, sm);
-  float l = 0.f;
-  for (uint32_t p = t; p < parts; p += 256) {
-    const float w = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s_w[p] - m);      // (a thread's own words up to here)
-    s_w[p] = w;
-    l += w * s_l[p];
-  }
-  l = block_sum(l, sm);                            // (its barriers stand behind the weights too)
+  const float m = block_max(here ? ml.x : -INFINITY, sm), w = here && m != -INFINITY ? __builtin_amdgcn_exp2f(ml.x - m) : 0.f;
+  s_w[t] = w;
+  const float l = block_sum(here ? w * ml.y : 0.f, sm);      // (its barriers stand behind the weights too)
   float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 8
   for (uint32_t p = t / LANES; p < parts; p += ROWS) {
     const float4 v = *reinterpret_cast<const float4*>(from + (size_t)p * (DH + 4) + 4 + t % LANES * 4);
-    const float w = s_w[p];
-    y.x += w * v.x; y.y += w * v.y; y.z += w * v.z; y.w += w * v.w;
+    const float f = s_w[p];
+    y.x += f * v.x; y.y += f * v.y; y.z += f * v.z; y.w += f * v.w;
   }
   s_o[t] = y;
   __syncthreads();
@@ -375,7 +364,7 @@ static sif_status decode_plan(const char* who, const sif_kv_cache* c, const sif_
   if (a->window != 0) seen = std::min<uint64_t>(seen, (uint64_t)a->window + a->sinks + 2 * tok);
   const uint64_t steps = std::max<uint64_t>(1, (seen + tok - 1) / tok);
   const uint64_t most = std::max<uint64_t>(1, steps / AD_WAVES);
-  out->splits = (uint32_t)std::min<uint64_t>(std::min<uint64_t>(most, AD_MAX_SPLITS), std::max<uint64_t>(1, 256 / units));
+  out->splits = (uint32_t)std::min<uint64_t>(most, std::max<uint64_t>(1, AD_BLOCKS / units));
   out->chunk = (uint32_t)((steps + out->splits - 1) / out->splits);
   *bytes = out->splits > 1 ? (uint64_t)a->n * a->heads * out->splits * (c->d_head + 4) * sizeof(float) : 256;
   return SIF_OK;
