@@ -62,10 +62,11 @@ def _check(run, q, k, v, do, heads, kv_heads, d, parts, window, sinks, backward=
     """parts: (first query row, queries, first key row, keys) of each sequence."""
     got = run.results()
     scale = 1.0 / math.sqrt(d) if scale is None else scale
+    exact = run.args.seq_k <= 256 or 0 < window <= 256 - sinks
     for i, (a, m, b, n) in enumerate(parts):
         rq, rk = slice(a, a + m), slice(b, b + n)
         val, tol = heads_attention(q[rq].double(), k[rk].double(), v[rk].double(), heads, kv_heads, d, visible(m, n, window, sinks), scale,
-                                   do[rq].double() if backward else None)
+                                   do[rq].double() if backward else None, exact)
         for name in val:
             if name == "lse":
                 if run.lse is not None:
