@@ -162,6 +162,7 @@ __global__ __launch_bounds__(256, 2) void attn_decode_kernel(DecodeArgs a) {
           sc[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16(kv), fq[j], sc[n], 0, 0, 0);
         }
       }
+      sc[n] *= c2;                                         // (in front of the mask: a scale of the cache may be 0 or negative)
     }
     // masks: only steps that hold the end, the border of the window or of the sinks, or a quarter without a page.  What is held there may
     // be anything, a NaN too: scores become -inf, values zero.
@@ -193,7 +194,7 @@ __global__ __launch_bounds__(256, 2) void attn_decode_kernel(DecodeArgs a) {
 #pragma unroll
     for (uint32_t n = 0; n < NT; ++n)
 #pragma unroll
-      for (uint32_t e = 0; e < 4; ++e) { sc[n][e] *= c2; mx = fmaxf(mx, sc[n][e]); }
+      for (uint32_t e = 0; e < 4; ++e) mx = fmaxf(mx, sc[n][e]);
     mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
     mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
     const float m_new = fmaxf(m_run, mx), m_use = m_new == -INFINITY ? 0.f : m_new;

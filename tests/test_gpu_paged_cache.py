@@ -438,6 +438,17 @@ def test_decode_lists_holes_and_garbage(e4m3):
     pool.attend(_rows(22, len(seqs), 4 * d), 4, 0, seqs, 0, 0)
 
 
+@pytest.mark.parametrize("window,sinks", [(0, 0), (70, 5)])
+def test_decode_with_scales_of_zero_and_below(window, sinks):
+    """A key is what is held times its scale, whatever that is: a kv head whose keys are all zero (a scale of 0), and negative ones, in
+    lengths that end inside a step."""
+    lens, d = [77, 300, 9], 64
+    pool = _filled(31, lens, 32, kv_heads=3, d=d, e4m3=True)
+    pool.ks[1].copy_(torch.tensor([0.0, -0.02, 0.03]))
+    pool.vs[1].copy_(torch.tensor([-0.02, 0.01, 0.0]))
+    pool.attend(_rows(32, 3, 6 * d), 6, 1, None, window, sinks)
+
+
 @pytest.mark.parametrize("e4m3", [False, True])
 def test_decode_of_a_long_sequence_beside_short_ones(e4m3):
     lens = [20011, 1, 300]
