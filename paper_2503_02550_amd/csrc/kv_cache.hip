@@ -44,8 +44,9 @@ sif_status kv_check(const char* who, const sif_kv_cache* c, KvView* out) {
   return SIF_OK;
 }
 
-static sif_status kv_check_list(const char* who, uint32_t n) {
+static sif_status kv_check_list(const char* who, uint32_t n, const int32_t* x, const int32_t* y = nullptr, const int32_t* status = nullptr) {
   if (n == 0 || n > kKvMaxListed) return fail(SIF_E_INVAL, "%s: 1 to %u entries", who, kKvMaxListed);
+  if (((uintptr_t)x | (uintptr_t)y | (uintptr_t)status) & 3) return fail(SIF_E_INVAL, "%s: misaligned list", who);
   return SIF_OK;
 }
 
@@ -482,7 +483,7 @@ sif_status sif_k_kv_extend(const sif_kv_cache* c, const int32_t* seqs, const int
                            uint64_t workspace_bytes, void* stream) {
   KvView v;
   if (sif_status st = kv_check("kv_extend", c, &v)) return st;
-  if (sif_status st = kv_check_list("kv_extend", n)) return st;
+  if (sif_status st = kv_check_list("kv_extend", n, seqs, counts, status)) return st;
   if (sif_status st = kv_check_work("kv_extend", v, workspace, workspace_bytes)) return st;
   const KvWork w = kv_work(v, workspace);
   hipLaunchKernelGGL(kv_extend_kernel, dim3(1), dim3(1024), 0, S(stream), v, seqs, counts, n, status, w);
@@ -498,6 +499,7 @@ sif_status sif_k_kv_write(const sif_kv_cache* c, uint32_t layer, const void* k, 
   if (layer >= w.layers) return fail(SIF_E_INVAL, "kv_write: no layer %u", layer);
   if (!k || !v || (((uintptr_t)k | (uintptr_t)v) & 15)) return fail(SIF_E_INVAL, "kv_write: k and v must be 16-byte aligned");
   if (n == 0 || rows == 0 || n > (1u << 27) || rows > (1u << 27)) return fail(SIF_E_INVAL, "kv_write: entries or rows outside 1 .. 2^27");
+  if (((uintptr_t)seqs | (uintptr_t)starts) & 3) return fail(SIF_E_INVAL, "kv_write: misaligned list");
   if (starts == nullptr && rows != n) return fail(SIF_E_INVAL, "kv_write: without starts there is one row per entry");
   const uint32_t width = w.kv_heads * w.d_head;
   if (ld_k < width || ld_v < width || ((ld_k | ld_v) & 7)) return fail(SIF_E_INVAL, "kv_write: bad leading dimensions");
@@ -513,7 +515,7 @@ sif_status sif_k_kv_write(const sif_kv_cache* c, uint32_t layer, const void* k, 
 sif_status sif_k_kv_fork(const sif_kv_cache* c, const int32_t* src, const int32_t* dst, uint32_t n, int32_t* status, void* stream) {
   KvView v;
   if (sif_status st = kv_check("kv_fork", c, &v)) return st;
-  if (sif_status st = kv_check_list("kv_fork", n)) return st;
+  if (sif_status st = kv_check_list("kv_fork", n, src, dst, status)) return st;
   if (!src || !dst) return fail(SIF_E_INVAL, "kv_fork: null list");
   hipLaunchKernelGGL(kv_fork_kernel, dim3(n), dim3(256), 0, S(stream), v, src, dst, n, status);
   return check_launch("kv_fork");
@@ -522,7 +524,7 @@ sif_status sif_k_kv_fork(const sif_kv_cache* c, const int32_t* src, const int32_
 static sif_status kv_release(const char* who, const sif_kv_cache* c, const int32_t* seqs, uint32_t n, uint32_t window, uint32_t sinks, void* stream) {
   KvView v;
   if (sif_status st = kv_check(who, c, &v)) return st;
-  if (sif_status st = kv_check_list(who, n)) return st;
+  if (sif_status st = kv_check_list(who, n, seqs)) return st;
   hipLaunchKernelGGL(kv_release_kernel, dim3(n), dim3(256), 0, S(stream), v, seqs, window, sinks);
   return check_launch(who);
 }
@@ -550,7 +552,7 @@ sif_status sif_k_kv_compact(const sif_kv_cache* c, void* workspace, uint64_t wor
 sif_status sif_k_kv_copy_pages(const sif_kv_cache* c, const int32_t* src, const int32_t* dst, uint32_t n, int32_t* status, void* stream) {
   KvView v;
   if (sif_status st = kv_check("kv_copy_pages", c, &v)) return st;
-  if (sif_status st = kv_check_list("kv_copy_pages", n)) return st;
+  if (sif_status st = kv_check_list("kv_copy_pages", n, src, dst, status)) return st;
   if (!src || !dst) return fail(SIF_E_INVAL, "kv_copy_pages: null list");
   hipLaunchKernelGGL(kv_copy_listed_kernel, dim3(n, 2 * v.layers), dim3(256), 0, S(stream), v, src, dst, n, status);
   return check_launch("kv_copy_pages");

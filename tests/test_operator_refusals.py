@@ -124,6 +124,19 @@ def test_page_operations_refuse_bad_lists_and_workspaces():
         assert lib.sif_k_kv_compact(p, work, size, None) == status
 
 
+def test_page_operations_refuse_misaligned_lists():
+    c, lib, at, big = _cache(), S.lib, 1 << 20, 1 << 40
+    p, off = C.byref(c), at + 2
+    for x, y, status in ((off, at, None), (at, off, None), (at, at, off)):
+        assert lib.sif_k_kv_extend(p, x, y, 2, status, at, big, None) == S.SIF_E_INVAL
+        assert lib.sif_k_kv_fork(p, x, y, 2, status, None) == S.SIF_E_INVAL
+        assert lib.sif_k_kv_copy_pages(p, x, y, 2, status, None) == S.SIF_E_INVAL
+    assert lib.sif_k_kv_free(p, off, 2, None) == S.SIF_E_INVAL
+    assert lib.sif_k_kv_trim(p, off, 2, 4, 0, None) == S.SIF_E_INVAL
+    for seqs, starts in ((off, None), (at, off)):
+        assert lib.sif_k_kv_write(p, 0, at, at, 128, 128, seqs, starts, 2, 2, None) == S.SIF_E_INVAL
+
+
 @pytest.mark.parametrize("change", [dict(layer=2), dict(k=None), dict(v=None), dict(k=8), dict(ld_k=120), dict(ld_v=129), dict(n=0, rows=0), dict(rows=0), dict(rows=3), dict(n=(1 << 27) + 1, rows=(1 << 27) + 1)], ids=str)
 def test_write_refuses(change):
     x = dict(dict(layer=0, k=1 << 20, v=1 << 20, ld_k=128, ld_v=128, n=2, rows=2), **change)
