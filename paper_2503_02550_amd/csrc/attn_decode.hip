@@ -24,7 +24,7 @@ namespace sif {
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float floatx4 __attribute__((ext_vector_type(4)));
 
-constexpr uint32_t AD_WAVES = 4, AD_HEADS = 16, AD_BLOCKS = 256;      // AD_BLOCKS: a block for each CU, and so the most splits
+constexpr uint32_t AD_WAVES = 4, AD_HEADS = 16, AD_BLOCKS = 256;      // AD_BLOCKS: a block for each CU, and the most splits
 constexpr float kNoSplit = -1.0f;       // in the place of a split's sum
 
 struct DecodeArgs {
@@ -338,12 +338,14 @@ __global__ __launch_bounds__(256) void attn_decode_join_kernel(DecodeArgs a) {
 }
 
 // How the work is divided.  A CU takes in some 47 KB per us whatever its wavefronts do, so a launch wants all CUs: splits of at least one
-// step per wavefront until there is a block for each of the 256 CUs.  (One sequence, 8 kv heads of 128: 1000 tokens 14.0 -> 8.6 us,
-// 8000 84 -> 11.8, 30000 352 -> 25.8, the join's 4 to 5 us included.)  No more than that: with a block per CU the memory is near its rate,
-// more splits only cost their own ends and a longer join (32 sequences of 4000 tokens: 96.8 us, 104 with eight blocks per CU; 64 of 4096:
-// 188 and 200).  Where lengths differ much, more splits would even them out (32 sequences of 1 to 8000: 118 and 111; 64 of 1 to
-// 8192: 215 and 210), but lengths are not known here.  Equal shares of all steps for 512 blocks, found from the lengths on the
-// device, were tried: 107 and 214 us there, 105 and 195 for the equal lengths, and 1.5 to 4 us more for every short call.
+// step per wavefront until there is a block for each of the 256 CUs.  (One sequence, 8 kv heads of 128: 1000 tokens 14.0 -> 8.5 us,
+// 8000 87 -> 11.5, 30000 325 -> 26.5, the join's 4 to 5 us included.)  Past that, up to eight blocks per CU, only where there are several
+// sequences, and in splits of 2048 tokens or more: where lengths differ, which is not known here, the long sequences' ends are then shared
+// (pages of 16: 32 sequences of 1 to 8000 tokens 112 -> 89 us, 64 of 1 to 8192 200 -> 193, 128 of 1 to 8000 389 -> 350, three of 100 to
+// 262011 375 -> 280; pages of 64: 139 -> 112, 237 -> 220, 451 -> 404, 463 -> 318), where they do not, that costs the splits' own ends and
+// the join (64 of 4096 170 -> 177, of 64-token pages 188 -> 197; 16 of 8000 85 -> 89 and 99 -> 112; 32 of 4000 the same; one of 262011
+// 189 -> 198 in pages of 64).  Splits that may be as short as a step cost more (128 of 500 13 -> 21), of 1024 tokens too (64 of 4096 182),
+// of 4096 leave 32 of 1 to 8000 at 111.
 static sif_status decode_plan(const char* who, const sif_kv_cache* c, const sif_attn_decode_args* a, DecodeArgs* out, uint64_t* bytes) {
   if (sif_status st = kv_check(who, c, &out->c)) return st;
   if (!a) return fail(SIF_E_INVAL, "%s: null arguments", who);
@@ -365,7 +367,8 @@ static sif_status decode_plan(const char* who, const sif_kv_cache* c, const sif_
   if (a->window != 0) seen = std::min<uint64_t>(seen, (uint64_t)a->window + a->sinks + 2 * tok);
   const uint64_t steps = std::max<uint64_t>(1, (seen + tok - 1) / tok);
   const uint64_t most = std::max<uint64_t>(1, steps / AD_WAVES);
-  out->splits = (uint32_t)std::min<uint64_t>(most, std::max<uint64_t>(1, AD_BLOCKS / units));
+  const uint64_t one = std::min<uint64_t>(most, AD_BLOCKS / units), eight = a->n > 1 ? std::min<uint64_t>(seen / 2048, 8 * AD_BLOCKS / units) : 0;
+  out->splits = (uint32_t)std::min<uint64_t>(AD_BLOCKS, std::max<uint64_t>(1, std::max(one, eight)));
   out->chunk = (uint32_t)((steps + out->splits - 1) / out->splits);
   *bytes = out->splits > 1 ? (uint64_t)a->n * a->heads * out->splits * (c->d_head + 4) * sizeof(float) : 256;
   return SIF_OK;
