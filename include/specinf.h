@@ -308,7 +308,7 @@ sif_status sif_k_attn_bwd(const void* qkv_dev, const void* o_dev, const void* d_
  * has no influence, whatever it is.
  * Query head h reads key/value head h / (heads / kv_heads).  bf16 operands, fp32 sums and softmax; the probabilities
  * (and, backward, their gradients) are rounded to bf16 as operands of the matrix units, once; backward takes its row term
- * rowsum(do .* o) from o as it is stored where rows see more than 256 keys (seq_k and window + sinks above), from the scores else.  Results must not overlap operands.  A NaN or an infinity in a row of k or v may
+ * rowsum(do .* o) from o as it is stored, but from the scores in blocks of rows none of which sees more than 256 keys.  Results must not overlap operands.  A NaN or an infinity in a row of k or v may
  * reach every query of its sequence as soon as one query sees that row. */
 typedef struct sif_window_attn_args {
   uint32_t struct_size;

@@ -109,7 +109,6 @@ struct WinArgs {
   uint32_t pieces;
   uint32_t heads, kv_heads, group, hb;      // hb: query heads of one key head that a block works on
   uint32_t batch, sq, sk, window, sinks, rows, rows_q;
-  uint32_t exact;                    // backward: the row term from the scores, see win_dq_kernel
   uint32_t ld_q, ld_k, ld_v, ld_o, ld_do, ld_dq, ld_dk, ld_dv;
   float scale;
 };
@@ -284,9 +283,10 @@ __global__ __launch_bounds__(AT_THREADS, 2) void win_fwd_kernel(WinArgs a) {
 // Backward, dq.  Rows and wavefronts as in the forward kernel.  Also writes delta.
 // delta = rowsum(do .* o) is taken from o as it is stored, whose two roundings to bf16 (of the probabilities and of o itself) it inherits.
 // Beside the sums of many keys that is little, but where a row sees some tens, o is as large as v and dq and dk were 2.6e-3 off in the norm (16
-// keys), 2.5e-3 (100), for the 2.4e-3 that the roundings of P and dS make.  There (`exact`: rows that see at most 256 keys) it is
+// keys), 2.5e-3 (100), for the 2.4e-3 that the roundings of P and dS make.  There it is
 // taken as the sum of P dP, which is the same in exact arithmetic, in a sweep of its own over the tiles: 2.4e-3, for 26 us instead of 17 (nine
-// sequences of 1 to 611 rows, 12 heads of 64, window 100).
+// sequences of 1 to 611 rows, 12 heads of 64, window 100).  Each block decides by what its own rows see at most (256 keys): how near a sequence's
+// gradients are does not depend on the others in the call (16 rows beside 611, no window: dq 3.0e-3, so 2.4e-3).
 template <int DH>
 __global__ __launch_bounds__(AT_THREADS, 2) void win_dq_kernel(WinArgs a) {
   constexpr int KS = DH / 16, DT = DH / 32, KV = kWinKv<DH>;
@@ -366,7 +366,8 @@ __global__ __launch_bounds__(AT_THREADS, 2) void win_dq_kernel(WinArgs a) {
       turn(sK1, sV1, sK0, sV0, t + 1);
     }
   };
-  if (a.exact != 0) {
+  const bool exact = (a.window != 0 ? min(sp.hi, a.window + a.sinks) : sp.hi) <= 256;
+  if (exact) {
     dsum = 0.f;
     sweep([&](const bf16_t* sK, const bf16_t* sV, int n, uint32_t first, uint32_t end) {
       floatx16 sacc, pacc;
@@ -763,7 +764,6 @@ static sif_status win_plan(const char* who, const sif_window_attn_args* a, WinAr
   w->sk = a->seq_k;
   w->window = a->window;
   w->sinks = a->window != 0 ? a->sinks : 0;
-  w->exact = a->seq_k <= 256 || (a->window != 0 && a->window + w->sinks <= 256) ? 1 : 0;
   w->rows = a->rows;
   w->rows_q = a->starts_dev ? a->rows : a->batch * a->seq_q;
   w->scale = a->scale != 0.f ? a->scale : 1.0f / sqrtf((float)a->d_head);
