@@ -379,7 +379,8 @@ sif_status sif_k_kv_extend(const sif_kv_cache* c, const int32_t* seqs_dev, const
                            void* workspace_dev, uint64_t workspace_bytes, void* stream);
 /* Writes the newest tokens' keys and values (bf16 rows of kv_heads * d_head, ld_k / ld_v elements apart) of one layer.
  * Rows starts[i] .. starts[i+1] - 1 (starts_dev int32 [n+1], ascending, within 0 .. rows) are the last tokens of sequence i of the
- * list; starts_dev null: one row each, rows = n.  n and rows are at most 2^27.  In SIF_E4M3 a value is divided by its scale, held at +-448 and rounded to
+ * list; starts_dev null: one row each, rows = n.  n and rows are at most 2^27, a list has at most 16384
+ * entries.  In SIF_E4M3 a value is divided by its scale, held at +-448 and rounded to
  * nearest even (NaN stays NaN).  A token that has no page is left out. */
 sif_status sif_k_kv_write(const sif_kv_cache* c, uint32_t layer, const void* k_dev, const void* v_dev, uint32_t ld_k, uint32_t ld_v,
                           const int32_t* seqs_dev, const int32_t* starts_dev, uint32_t n, uint32_t rows, void* stream);

@@ -19,7 +19,7 @@ struct KvView {
   uint32_t page_bytes;               // of K or V in one layer
 };
 
-constexpr uint32_t kKvMaxListed = 1024, kKvMaxPages = 1u << 21;
+constexpr uint32_t kKvMaxListed = 1024, kKvMaxWritten = 1u << 14, kKvMaxPages = 1u << 21;      // entries of a list (kKvMaxWritten: of tokens that are written)
 
 // Checks a cache and fills in the view; `who` begins the error's text.
 sif_status kv_check(const char* who, const sif_kv_cache* c, KvView* out);

@@ -499,6 +499,9 @@ sif_status sif_k_kv_write(const sif_kv_cache* c, uint32_t layer, const void* k, 
   if (layer >= w.layers) return fail(SIF_E_INVAL, "kv_write: no layer %u", layer);
   if (!k || !v || (((uintptr_t)k | (uintptr_t)v) & 15)) return fail(SIF_E_INVAL, "kv_write: k and v must be 16-byte aligned");
   if (n == 0 || rows == 0 || n > (1u << 27) || rows > (1u << 27)) return fail(SIF_E_INVAL, "kv_write: entries or rows outside 1 .. 2^27");
+  // every row looks through the list in front of its entry, for each kv head: the work grows with rows times entries (at 2^27 of each it
+  // would not end in any useful time; 2^14 entries are 64 KB of list, and 2^10 reads a row and thread)
+  if (seqs != nullptr && n > kKvMaxWritten) return fail(SIF_E_INVAL, "kv_write: at most %u listed sequences", kKvMaxWritten);
   if (((uintptr_t)seqs | (uintptr_t)starts) & 3) return fail(SIF_E_INVAL, "kv_write: misaligned list");
   if (starts == nullptr && rows != n) return fail(SIF_E_INVAL, "kv_write: without starts there is one row per entry");
   const uint32_t width = w.kv_heads * w.d_head;

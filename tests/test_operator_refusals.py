@@ -143,6 +143,14 @@ def test_write_refuses(change):
     assert S.lib.sif_k_kv_write(C.byref(_cache()), x["layer"], x["k"], x["v"], x["ld_k"], x["ld_v"], None, None, x["n"], x["rows"], None) == S.SIF_E_INVAL
 
 
+def test_write_refuses_a_long_list_of_sequences():
+    """Each row looks through the list in front of its own entry, so the list's length is limited; entries 0 .. n-1 without a list are not."""
+    most, at = 1 << 14, 1 << 20
+    p = C.byref(_cache())
+    assert S.lib.sif_k_kv_write(p, 0, at, at, 128, 128, at, None, most + 1, most + 1, None) == S.SIF_E_INVAL and "16384" in S.last_error()
+    assert S.lib.sif_k_kv_write(p, 0, at, at, 128, 128, at, at, 1 << 27, 1, None) == S.SIF_E_INVAL
+
+
 @pytest.mark.parametrize("change", [dict(struct_size=4), dict(layer=2), dict(n=0), dict(heads=0), dict(heads=3), dict(q_dev=None), dict(o_dev=None), dict(q_dev=8), dict(o_dev=2),
                                     dict(lse_dev=2), dict(seqs_dev=1), dict(ld_q=248), dict(ld_o=260), dict(scale=-0.5), dict(scale=float("nan")), dict(n=1 << 21)], ids=str)
 def test_decode_refuses(change):
