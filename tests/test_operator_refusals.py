@@ -179,3 +179,50 @@ def test_the_binding_refuses_tensors_that_do_not_fit():
         x = dict(dict(k=k, v=v, table=table, lengths=lengths, refs=refs, dtype=S.SIF_BF16, page_tokens=16), **bad)
         with pytest.raises(S.SifError):
             S.kv_cache(**x)
+
+
+def _i32(*x):
+    return torch.tensor(x, dtype=torch.int32)
+
+
+def _refused(call):
+    with pytest.raises(S.SifError) as e:
+        call()
+    assert e.value.status == S.SIF_E_INVAL
+    return str(e.value)
+
+
+BAD_LISTS = [torch.arange(4), torch.zeros(4), _i32(0), _i32(*range(8))[::2]]      # 64 bits (what torch counts in), not whole, too short, not in a row
+
+
+@pytest.mark.parametrize("bad", BAD_LISTS, ids=["int64", "float", "short", "strided"])
+def test_the_binding_refuses_lists_that_the_kernels_would_read_wrongly(bad):
+    """The library takes a list as an address: one of 64-bit numbers would be read as twice as many of 32 bits, a short one past its end."""
+    c, good, at, big, x = _cache(), _i32(0, 1, 2, 3, 4), 1 << 20, 1 << 40, torch.zeros(4, 128, dtype=torch.bfloat16)
+    for call in (lambda: S.sif_k_kv_extend(c, bad, None, 4, at, big), lambda: S.sif_k_kv_extend(c, None, bad, 4, at, big), lambda: S.sif_k_kv_extend(c, None, None, 4, at, big, status=bad),
+                 lambda: S.sif_k_kv_write(c, 0, x, x, bad, 4), lambda: S.sif_k_kv_write(c, 0, x, x, None, 3, starts=bad, rows=4),
+                 lambda: S.sif_k_kv_fork(c, bad, good, 4), lambda: S.sif_k_kv_fork(c, good, bad, 4), lambda: S.sif_k_kv_fork(c, good, good, 4, status=bad),
+                 lambda: S.sif_k_kv_free(c, bad, 4), lambda: S.sif_k_kv_trim(c, bad, 4, 16, 0),
+                 lambda: S.sif_k_kv_copy_pages(c, bad, good, 4), lambda: S.sif_k_kv_copy_pages(c, good, bad, 4), lambda: S.sif_k_kv_copy_pages(c, good, good, 4, status=bad)):
+        assert "int32" in _refused(call)
+    z = torch.zeros(4, 256, dtype=torch.bfloat16)
+    assert "int32" in _refused(lambda: S.attn_decode_args(z, z, 4, 4, seqs=bad))
+    assert "int32" in _refused(lambda: S.window_attn_args(z, z, z, z, 4, 4, 64, 3, 4, 4, 0, 0, starts=bad, rows=4))
+
+
+def test_the_binding_refuses_rows_of_another_type_or_order():
+    z, f = torch.zeros(64, 256, dtype=torch.bfloat16), torch.zeros(256)
+    turned = torch.zeros(256, 64, dtype=torch.bfloat16).t()
+    names = ("q", "k", "v", "o", "d_o", "dq", "dk", "dv")
+    S.window_attn_args(**dict.fromkeys(names, z), lse=f, heads=4, kv_heads=4, d_head=64, batch=1, seq_q=64, seq_k=64, window=0, sinks=0)
+    for bad in (z.float(), z.half(), turned):
+        for name in names:
+            x = dict(dict.fromkeys(names, z), **{name: bad})
+            _refused(lambda: S.window_attn_args(**x, lse=f, heads=4, kv_heads=4, d_head=64, batch=1, seq_q=64, seq_k=64, window=0, sinks=0))
+        _refused(lambda: S.attn_decode_args(bad, z, 64, 4))
+        _refused(lambda: S.attn_decode_args(z, bad, 64, 4))
+        _refused(lambda: S.sif_k_kv_write(_cache(), 0, bad[:4, :128], z[:4, :128], None, 4))
+        _refused(lambda: S.sif_k_kv_write(_cache(), 0, z[:4, :128], bad[:4, :128], None, 4))
+    for lse in (f.double(), f.to(torch.bfloat16), torch.zeros(512)[::2]):
+        _refused(lambda: S.attn_decode_args(z, z, 64, 4, lse=lse))
+        _refused(lambda: S.window_attn_args(z, z, z, z, 4, 4, 64, 1, 64, 64, 0, 0, lse=lse))
