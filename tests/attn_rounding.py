@@ -13,14 +13,33 @@ import torch
 
 GRADIENTS, FORWARD = 1.1, 1.37
 
+CASES = [
+    # batch, queries, keys, heads, kv heads, d, window, sinks
+    (1, 300, 300, 2, 1, 64, 0, 0),
+    (2, 129, 129, 6, 2, 64, 31, 5),
+    (1, 257, 257, 8, 1, 128, 33, 4),
+    (2, 70, 31, 4, 2, 64, 12, 2),                 # rows that see nothing
+    (1, 100, 517, 4, 1, 128, 130, 7),
+    (1, 700, 700, 6, 2, 64, 200, 70),             # from here on also rows that see nothing of a sequence's first keys but the sinks
+    (1, 700, 700, 4, 4, 128, 129, 33),
+    (3, 391, 391, 4, 2, 64, 100, 100),
+    (1, 1500, 1500, 4, 1, 128, 256, 4),           # these rows in eighteen pieces
+]
+
+
+def inputs(seed, rq, rk, n_heads, kv_heads, d):
+    g = torch.Generator().manual_seed(seed)
+    r = lambda n, w: torch.randn(n, w, generator=g).to(torch.bfloat16)      # noqa: E731
+    return r(rq, n_heads * d), r(rk, kv_heads * d), r(rk, kv_heads * d), r(rq, n_heads * d)
+
 
 def bf16(x):
     return x.to(torch.bfloat16).double()
 
 
-def head(q, k, v, seen, scale, do=None, o=None):
+def head(q, k, v, seen, scale, do=None, o=None, change=None, lost=None):
     """One head as the kernels round it: o, and given do also dq, dk, dv.  o: the stored result that the row term is taken from (None: it is
-    taken from the scores)."""
+    taken from the scores).  change, lost: mistakes that a test of the bounds plants, the latter the pairs (row, key) that dk leaves out."""
     s = (q @ k.t() * scale).masked_fill(~seen, -math.inf)
     lse = torch.logsumexp(s, 1)
     p = torch.where(seen, torch.exp(s - torch.where(lse > -math.inf, lse, 0.0)[:, None]), 0.0)
@@ -29,11 +48,14 @@ def head(q, k, v, seen, scale, do=None, o=None):
         dp = do @ v.t()
         delta = (p * dp).sum(1, keepdim=True) if o is None else (do * o).sum(1, keepdim=True)
         ds = bf16(p * (dp - delta))
-        got |= {"dq": bf16(ds @ k * scale), "dk": (ds.t() @ q) * scale, "dv": bf16(p).t() @ do}
+        if change == "no row term":
+            ds = bf16(p * dp)
+        left = torch.where(lost, 0.0, ds) if lost is not None else ds
+        got |= {"dq": bf16(ds @ k * scale), "dk": (left.t() @ q) * scale, "dv": bf16(p).t() @ do}
     return got
 
 
-def heads(q, k, v, n_heads, kv_heads, d, seen, scale, do=None, o=None):
+def heads(q, k, v, n_heads, kv_heads, d, seen, scale, do=None, o=None, change=None, lost=None):
     """All heads of one sequence, laid out as attn_reference.heads_attention's."""
     group = n_heads // kv_heads
     out = {"o": torch.zeros(q.shape[0], n_heads * d, dtype=torch.float64)}
@@ -41,7 +63,8 @@ def heads(q, k, v, n_heads, kv_heads, d, seen, scale, do=None, o=None):
         out |= {"dq": torch.zeros_like(out["o"]), "dk": torch.zeros(k.shape[0], kv_heads * d, dtype=torch.float64), "dv": torch.zeros(k.shape[0], kv_heads * d, dtype=torch.float64)}
     for h in range(n_heads):
         cq, ck = slice(h * d, h * d + d), slice(h // group * d, h // group * d + d)
-        a = head(q[:, cq], k[:, ck], v[:, ck], seen, scale, None if do is None else do[:, cq], None if o is None else o[:, cq])
+        a = head(q[:, cq], k[:, ck], v[:, ck], seen, scale, None if do is None else do[:, cq], None if o is None else o[:, cq], change,
+                 None if lost is None else lost(h))
         for name, x in a.items():
             out[name][:, cq if name in ("o", "dq") else ck] += x
     for name in ("dk", "dv"):
