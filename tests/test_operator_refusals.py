@@ -169,6 +169,14 @@ def test_decode_needs_its_workspace_where_it_splits():
     assert S.lib.sif_attn_decode_workspace_bytes(C.byref(c), None) == 0
 
 
+def test_a_workspace_planned_for_shorter_sequences_is_refused():
+    """Its size goes by max_tokens, so a call with another asks for its own."""
+    c = _cache(table_ld=100000)
+    short, long = (S.sif_attn_decode_workspace_bytes(c, _decode(max_tokens=m)) for m in (1000, 100000))
+    assert short < long
+    assert S.lib.sif_k_attn_decode(C.byref(c), C.byref(_decode(max_tokens=100000, workspace_bytes=short)), None) == S.SIF_E_NOMEM
+
+
 def test_the_binding_refuses_tensors_that_do_not_fit():
     k, v = torch.zeros(1, 3, 2, 16, 64, dtype=torch.bfloat16), torch.zeros(1, 3, 2, 64, 16, dtype=torch.bfloat16)
     table, lengths, refs = torch.zeros(2, 2, dtype=torch.int32), torch.zeros(2, dtype=torch.int32), torch.zeros(3, dtype=torch.int32)
