@@ -317,7 +317,7 @@ typedef struct sif_window_attn_args {
                                          batch * heads below 2^23                                                     */
   uint32_t window;                    /* 0 = no limit                                                                */
   uint32_t sinks;                     /* at most 128                                                                 */
-  float scale;                        /* 0 = 1 / sqrt(d_head)                                                        */
+  float scale;                        /* 0 = 1 / sqrt(d_head); not negative, scale * log2(e) finite                   */
   uint32_t ld_q, ld_k, ld_v, ld_o;    /* elements from a row to the next, multiples of 8, below 2^27; head h in columns h*d_head .. */
   uint32_t ld_do, ld_dq, ld_dk, ld_dv;
   uint32_t rows;                      /* with starts_dev: rows of all tensors                                        */
@@ -410,7 +410,7 @@ typedef struct sif_attn_decode_args {
   uint32_t window, sinks;             /* window 0 = no limit; any number of sinks                                    */
   uint32_t max_tokens;                /* what the longest listed sequence is expected to hold (0: a whole row of the table).  Only the
                                          division of the work depends on it: a longer sequence is computed all the same */
-  float scale;                        /* 0 = 1 / sqrt(d_head)                                                        */
+  float scale;                        /* 0 = 1 / sqrt(d_head); not negative, scale * log2(e) finite                   */
   uint32_t ld_q, ld_o;                /* elements from a sequence's row to the next, multiples of 8; rows of heads * d_head */
   const int32_t* seqs_dev;            /* [n], or null = 0 .. n-1                                                     */
   const void* q_dev;                  /* bf16                                                                        */

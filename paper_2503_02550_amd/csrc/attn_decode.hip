@@ -352,6 +352,7 @@ static sif_status decode_plan(const char* who, const sif_kv_cache* c, const sif_
   if (a->struct_size != sizeof(sif_attn_decode_args)) return fail(SIF_E_INVAL, "%s: struct_size", who);
   if (a->layer >= c->layers) return fail(SIF_E_INVAL, "%s: no layer %u", who, a->layer);
   if (!a->n || !a->heads || a->heads % c->kv_heads) return fail(SIF_E_INVAL, "%s: no sequences, or heads not a multiple of kv_heads", who);
+  if (!(a->scale >= 0.f) || !std::isfinite(a->scale * 1.44269504088896f)) return fail(SIF_E_INVAL, "%s: scale must be finite (in base 2 too) and not negative", who);
   const uint32_t tok = c->dtype == SIF_E4M3 ? 64u : 32u;
   out->seqs = a->seqs_dev;
   out->layer = a->layer;
@@ -395,7 +396,6 @@ sif_status sif_k_attn_decode(const sif_kv_cache* c, const sif_attn_decode_args* 
   if (((uintptr_t)a->q_dev | (uintptr_t)a->o_dev) & 15) return fail(SIF_E_INVAL, "attn_decode: q and o must be 16-byte aligned");
   if (((uintptr_t)a->lse_dev | (uintptr_t)a->seqs_dev) & 3) return fail(SIF_E_INVAL, "attn_decode: misaligned operand");
   if (a->ld_q < width || a->ld_o < width || ((a->ld_q | a->ld_o) & 7)) return fail(SIF_E_INVAL, "attn_decode: bad leading dimensions");
-  if (!(a->scale >= 0.f) || !std::isfinite(a->scale)) return fail(SIF_E_INVAL, "attn_decode: scale must be finite and not negative");
   if (d.splits > 1) {
     if (!a->workspace_dev || ((uintptr_t)a->workspace_dev & 255)) return fail(SIF_E_INVAL, "attn_decode: the workspace must be 256-byte aligned");
     if (a->workspace_bytes < bytes)

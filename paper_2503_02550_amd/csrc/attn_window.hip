@@ -751,7 +751,7 @@ static sif_status win_plan(const char* who, const sif_window_attn_args* a, WinAr
   if ((uint64_t)a->batch * a->seq_q > 0x7FFFFFFFull || (uint64_t)a->batch * a->seq_k > 0x7FFFFFFFull) return fail(SIF_E_INVAL, "%s: rows beyond 31 bits", who);
   if (a->sinks > 128) return fail(SIF_E_INVAL, "%s: at most 128 sinks", who);
   if (a->window > (1u << 30)) return fail(SIF_E_INVAL, "%s: a window of at most 2^30 (0: no limit)", who);
-  if (!(a->scale >= 0.f) || !std::isfinite(a->scale)) return fail(SIF_E_INVAL, "%s: scale must be finite and not negative", who);
+  if (!(a->scale >= 0.f) || !std::isfinite(a->scale * kLog2e)) return fail(SIF_E_INVAL, "%s: scale must be finite (in base 2 too) and not negative", who);
   if (a->starts_dev && (a->seq_q != a->seq_k || a->rows == 0 || a->rows > 0x7FFFFFFFu)) return fail(SIF_E_INVAL, "%s: with starts, seq_q = seq_k and rows in 1 .. 2^31 - 1", who);
   if ((uintptr_t)a->starts_dev & 3) return fail(SIF_E_INVAL, "%s: misaligned starts", who);
   w->starts = a->starts_dev;

@@ -1,5 +1,6 @@
 """What the attention operators and the cache's page operations refuse: checked on the host before anything is launched, so without a GPU."""
 import ctypes as C
+import math
 
 import pytest
 import torch
@@ -175,6 +176,16 @@ def test_a_workspace_planned_for_shorter_sequences_is_refused():
     short, long = (S.sif_attn_decode_workspace_bytes(c, _decode(max_tokens=m)) for m in (1000, 100000))
     assert short < long
     assert S.lib.sif_k_attn_decode(C.byref(c), C.byref(_decode(max_tokens=100000, workspace_bytes=short)), None) == S.SIF_E_NOMEM
+
+
+def test_a_scale_whose_base_2_form_is_infinite_is_refused():
+    """Exponentials are taken in base 2: past this a score of zero would become NaN."""
+    most = 3.4028235e38 * math.log(2.0)
+    for scale, refused in ((1.001 * most, True), (0.999 * most, False)):
+        assert (S.lib.sif_window_attn_bwd_workspace_bytes(C.byref(_window(scale=scale))) == 0) == refused
+        assert (S.lib.sif_attn_decode_workspace_bytes(C.byref(_cache()), C.byref(_decode(scale=scale))) == 0) == refused
+        for call in (lambda: S.lib.sif_k_window_attn_fwd(C.byref(_window(scale=scale, q_dev=None)), None), lambda: S.lib.sif_k_attn_decode(C.byref(_cache()), C.byref(_decode(scale=scale, ld_q=0)), None)):
+            assert call() == S.SIF_E_INVAL and ("scale" in S.last_error()) == refused
 
 
 def test_the_binding_refuses_tensors_that_do_not_fit():
