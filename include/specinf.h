@@ -309,12 +309,13 @@ sif_status sif_k_attn_bwd(const void* qkv_dev, const void* o_dev, const void* d_
  * Query head h reads key/value head h / (heads / kv_heads).  bf16 operands, fp32 sums and softmax; the probabilities
  * (and, backward, their gradients) are rounded to bf16 as operands of the matrix units, once; backward takes its row term
  * rowsum(do .* o) from o as it is stored, but from the scores in blocks of rows none of which sees more than 256 keys.  Results must not overlap operands.  A NaN or an infinity in a row of k or v may
- * reach every query of its sequence as soon as one query sees that row. */
+ * reach every query of its sequence as soon as one query sees that row; backward, one in q, do, o or lse of a query that sees some key may reach
+ * dk and dv of every key of its sequence. */
 typedef struct sif_window_attn_args {
   uint32_t struct_size;
   uint32_t heads, kv_heads, d_head;   /* heads a multiple of kv_heads; d_head 64 or 128                              */
   uint32_t batch, seq_q, seq_k;       /* sequence b has the query rows b*seq_q .. and the key rows b*seq_k ..; both 1 .. 2^20;
-                                         batch * heads below 2^23                                                     */
+                                         batch * heads below 2^23, batch * seq_q and batch * seq_k below 2^31          */
   uint32_t window;                    /* 0 = no limit                                                                */
   uint32_t sinks;                     /* at most 128                                                                 */
   float scale;                        /* 0 = 1 / sqrt(d_head); not negative, scale * log2(e) finite                   */
@@ -381,7 +382,8 @@ sif_status sif_k_kv_extend(const sif_kv_cache* c, const int32_t* seqs_dev, const
  * Rows starts[i] .. starts[i+1] - 1 (starts_dev int32 [n+1], ascending, within 0 .. rows) are the last tokens of sequence i of the
  * list; starts_dev null: one row each, rows = n.  n and rows are at most 2^27, a list has at most 16384
  * entries.  In SIF_E4M3 a value is divided by its scale, held at +-448 and rounded to
- * nearest even (NaN stays NaN).  A token that has no page is left out. */
+ * nearest even (NaN stays NaN).  A token that has no page is left out; a page is written to whoever else holds it (extending
+ * by the tokens before they are written leaves them in pages of the sequence's own). */
 sif_status sif_k_kv_write(const sif_kv_cache* c, uint32_t layer, const void* k_dev, const void* v_dev, uint32_t ld_k, uint32_t ld_v,
                           const int32_t* seqs_dev, const int32_t* starts_dev, uint32_t n, uint32_t rows, void* stream);
 /* Sequence dst[i] becomes a copy of src[i] and shares its pages.  Status SIF_E_INVAL: a number outside the table, a dst that is

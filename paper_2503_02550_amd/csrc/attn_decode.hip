@@ -1,4 +1,5 @@
-// Attention of one new token per sequence over a paged cache (Sec. 5.1's generating workloads: one such launch per layer and token).
+// Attention of one new token per sequence over a paged cache: one launch, or two, per layer and token of a program that generates (no
+// registered model does).
 //
 //   o = sum_j p_j v_j / sum_j p_j,   p_j = exp(scale k_scale q k_j - m),   over the visible tokens j
 //
@@ -64,7 +65,8 @@ __device__ __forceinline__ bf16x8 from_e4m3(uint32_t a, uint32_t b) {
   r[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.0f, true));
   return __builtin_bit_cast(bf16x8, r);
 }
-// 16 bytes of lines that one fetch instruction takes whole and nobody reads again: loads that claim no place in the caches.  (1 GiB read by
+// 16 bytes of lines that one fetch instruction takes whole and that this sequence does not read again: loads that claim no place in the
+// caches.  (Sequences that share pages after a fork read them once each; that case has not been timed both ways.)  (1 GiB read by
 // 256 to 1024 blocks in the ordinary way takes 167 to 222 us, 4.8 to 6.4 TB/s, in this way 148 to 206.)  That is V's case where a page is no
 // longer than a step: 64 sequences of 4096 tokens 189 -> 171 us, of 1 to 8192 215 -> 201.  K's rows of more than 64 bytes take several
 // instructions to a line, and so do V's in longer pages; with these loads the line came from memory again (one sequence of

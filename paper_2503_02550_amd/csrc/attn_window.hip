@@ -1,5 +1,5 @@
 // Attention with a sliding window of recent keys and a few first keys (sinks) that stay visible, forward and backward, with fewer key
-// heads than query heads if wanted (Sec. 5.1's transformer training on long sequences; prompts).
+// heads than query heads if wanted.  Single launches: no registered model contains them, so they carry no monitor record.
 //
 //   key j is visible to the query at position p  iff  j <= p  and  (window = 0  or  p - j < window  or  j < sinks)
 //   forward    o = softmax(scale q k^T | visible) v,  lse = log sum exp
@@ -10,10 +10,12 @@
 // Products, operands and LDS tiles are those of attention.hip.  A block meets only the tiles that one of its rows sees: the sinks', then
 // from the first key of its first row's window to its last row.  Those ranges begin and end exactly there and are not rounded to
 // tiles, and what a fetch would read past the end is the last row again, so that a key or query that nobody sees is never read.
-// Bound by the matrix and the vector units together: forward with heads of 128 the first are busy 43 % of a SIMD's cycles (of 1.75 GHz,
-// which the chip holds under this load), the second 50 %, backward 42 and 42 (dq), 38 and 30 (dk, dv), and there is little
-// overlap between the two wavefronts of a SIMD.  8192 rows, 16 query and 4 key heads of 128, window 1024: 93, 127, 177 us, that is 690,
-// 760 and 730 TFLOP/s of the products that each kernel needs (a large matrix product reaches 1390 on this card); the sinks' two launches 21.
+// Bound by the matrix and the vector units together: forward with heads of 128 the first are busy 43 % of a SIMD's cycles,
+// the second 50 %, backward 42 and 42 (dq), 38 and 30 (dk, dv), and there is little
+// overlap between the two wavefronts of a SIMD.  8192 rows, 16 query and 4 key heads of 128, window 1024: 84, 114, 150 us, that is 770,
+// 850 and 860 TFLOP/s of the products that each kernel needs (a large matrix product reaches 1390 on this card); the sinks' two launches 22.
+// (So once passes have followed one another for a while; the first dozen run at a lower clock and take 99, 134 and 189 us.  What is compared
+// below, one form of a kernel with another, was measured in such short runs, both sides alike.)
 #include <math.h>
 #include <algorithm>
 
@@ -153,8 +155,8 @@ __device__ __forceinline__ bool win_sees(const WinArgs& a, int32_t p, uint32_t j
 template <int DH> constexpr int kWinKv = DH == 64 ? 128 : 64;        // keys of a tile: two buffers of K and V are 64 KB
 
 // Forward.  Four wavefronts of 32 rows: hb query heads of a key head (1, 2 or 4), 128 / hb rows each, so that the wavefronts of a
-// block have nearly the same keys and share them.  (Timing variants at 8192 rows as above: without the exponentials 84 us, without the
-// fetches after the first 82, without both 71.)
+// block have nearly the same keys and share them.  (Timing variants at 8192 rows as above, where the whole took 93 us: without the
+// exponentials 84, without the fetches after the first 82, without both 71.)
 template <int DH>
 __global__ __launch_bounds__(AT_THREADS, 2) void win_fwd_kernel(WinArgs a) {
   constexpr int KS = DH / 16, DT = DH / 32, KV = kWinKv<DH>, NT = KV / 32;
@@ -282,11 +284,11 @@ __global__ __launch_bounds__(AT_THREADS, 2) void win_fwd_kernel(WinArgs a) {
 
 // Backward, dq.  Rows and wavefronts as in the forward kernel.  Also writes delta.
 // delta = rowsum(do .* o) is taken from o as it is stored, whose two roundings to bf16 (of the probabilities and of o itself) it inherits.
-// Beside the sums of many keys that is little, but where a row sees some tens, o is as large as v and dq and dk were 2.6e-3 off in the norm (16
-// keys), 2.5e-3 (100), for the 2.4e-3 that the roundings of P and dS make.  There it is
-// taken as the sum of P dP, which is the same in exact arithmetic, in a sweep of its own over the tiles: 2.4e-3, for 26 us instead of 17 (nine
+// Beside the sums of many keys that is little (dq 2.5e-3 off in the norm for windows of 256 and more, where the roundings of dS and dq
+// alone make 2.35e-3), but where a row sees some tens, o is as large as v: 2.6e-3 (100 keys), 2.7e-3 (16), 3.0e-3 (sequences of 16).  There it is
+// taken as the sum of P dP, which is the same in exact arithmetic, in a sweep of its own over the tiles: 2.35e-3, for 26 us instead of 17 (nine
 // sequences of 1 to 611 rows, 12 heads of 64, window 100).  Each block decides by what its own rows see at most (256 keys): how near a sequence's
-// gradients are does not depend on the others in the call (16 rows beside 611, no window: dq 3.0e-3, so 2.4e-3).
+// gradients are does not depend on the others in the call.
 template <int DH>
 __global__ __launch_bounds__(AT_THREADS, 2) void win_dq_kernel(WinArgs a) {
   constexpr int KS = DH / 16, DT = DH / 32, KV = kWinKv<DH>;

@@ -1,5 +1,4 @@
-// Page operations of a paged key-value cache (the inference instances' side of Sec. 3.3: they are queued on a stream like every other
-// kernel and ask the host nothing).  Bookkeeping is integers: what it costs is launches and dependent loads, so each operation is one
+// Page operations of a paged key-value cache: queued on a stream like every other kernel, they ask the host nothing.  Bookkeeping is integers: what it costs is launches and dependent loads, so each operation is one
 // launch for the bookkeeping and, where contents move, one that moves them at the memory's rate.  Results do not depend on the
 // order of blocks: reference counts are sums, and who gets which page follows from a rank in the list of free pages.
 #include "common.h"
