@@ -48,7 +48,8 @@ enum {
   SIF_E_DEVICE = -6     /* a HIP call failed; text in sif_last_error() */
 };
 
-enum { SIF_F32 = 0, SIF_BF16 = 1, SIF_E4M3 = 2 /* 8 bits: 4 of exponent, 3 of mantissa, finite up to 448, no infinities */ };
+enum { SIF_F32 = 0, SIF_BF16 = 1, SIF_E4M3 = 2 /* 8 bits: 4 of exponent, 3 of mantissa, finite up to 448, no infinities */,
+       SIF_E2M1 = 3 /* 4 bits: 2 of exponent, 1 of mantissa (0, .5, 1, 1.5, 2, 3, 4, 6 and their negatives), a power of two for every 32 */ };
 enum { SIF_STATUS_BUSY = 0, SIF_STATUS_IDLE = 1 };
 
 const char* sif_last_error(void);
@@ -340,9 +341,59 @@ sif_status sif_k_window_attn_fwd(const sif_window_attn_args* a, void* stream);
 sif_status sif_k_window_attn_bwd(const sif_window_attn_args* a, void* stream);
 uint64_t sif_window_attn_bwd_workspace_bytes(const sif_window_attn_args* a);    /* 0: refused, see sif_last_error() */
 
+/* --- Rotary positions --------------------------------------------------------------------------------------------
+ * The first rot_dim elements of a head are pairs, (i, i + rot_dim / 2) or (2i, 2i + 1); a token at position p turns pair i by the angle
+ * a = p f_i and scales it by m:
+ *   y_first = m (x_first cos a - x_second sin a),   y_second = m (x_second cos a + x_first sin a),   f_i = base^(-2i / rot_dim)
+ * The other elements stay as they are.  For contexts longer than the trained one the frequencies f are scaled:
+ *   SIF_ROPE_LINEAR  f / factor
+ *   SIF_ROPE_BASE    with base * factor^(rot_dim / (rot_dim - 2)) in the place of base: the lowest one becomes f / factor, the highest one stays
+ *   SIF_ROPE_PARTS   g f + (1 - g) f / factor, g = (r - low_turns) / (high_turns - low_turns) held to 0 .. 1, where r = trained_tokens f / 2 pi is
+ *                    how often the pair turns within the trained length (arXiv 2309.00071) */
+enum { SIF_ROPE_HALF = 0, SIF_ROPE_INTERLEAVED = 1 };
+enum { SIF_ROPE_PLAIN = 0, SIF_ROPE_LINEAR = 1, SIF_ROPE_BASE = 2, SIF_ROPE_PARTS = 3 };
+
+typedef struct sif_rope_desc {
+  uint32_t struct_size;
+  uint32_t layout;                    /* SIF_ROPE_HALF or SIF_ROPE_INTERLEAVED                                        */
+  uint32_t rot_dim;                   /* a multiple of 16, at most 256                                               */
+  uint32_t scaling;                   /* SIF_ROPE_PLAIN and so on; what a scaling does not name is not looked at      */
+  double base, factor;                /* base at least 1, factor above 0                                             */
+  double low_turns, high_turns, trained_tokens;    /* SIF_ROPE_PARTS: low_turns < high_turns                          */
+  double magnitude;                   /* m                                                                           */
+} sif_rope_desc;
+
+/* The table that the launches take (by value: it may be changed or dropped when they have returned).  A program may fill in frequencies of its own. */
+typedef struct sif_rope {
+  uint32_t struct_size;
+  uint32_t layout, rot_dim, reserved;
+  double magnitude;
+  double turns[128];                  /* [rot_dim / 2] f_i / 2 pi, whole turns per token, between -1 and 1                */
+} sif_rope;
+
+/* A pure host function. */
+sif_status sif_rope_plan(const sif_rope_desc* d, sif_rope* out);
+
+/* Turns rows of query heads and, if there are any, of key heads.  bf16, fp32 products, each result rounded once; angles are reduced in 64 bits, so they
+ * are as right at the last position as at the first.  inverse = 1 turns back and scales by m all the same: dx of the forward pass from dy.  Results may take their operands' place (q_out =
+ * q with the same leading dimension, so too k), and must not overlap them otherwise. */
+typedef struct sif_rope_args {
+  uint32_t struct_size;
+  uint32_t rows, heads, kv_heads, d_head;   /* d_head a multiple of 8, rot_dim to 256; kv_heads 0: no keys               */
+  uint32_t seq;                       /* without positions_dev: row r stands at first + r % seq                       */
+  int32_t first;
+  uint32_t inverse;
+  uint32_t ld_q, ld_q_out, ld_k, ld_k_out;  /* elements from a row to the next, multiples of 8, below 2^27               */
+  const int32_t* positions_dev;       /* [rows], any numbers, or null                                                */
+  const void* q_dev; void* q_out_dev; /* head h in columns h*d_head ..                                               */
+  const void* k_dev; void* k_out_dev;
+} sif_rope_args;
+
+sif_status sif_k_rope(const sif_rope* r, const sif_rope_args* a, void* stream);
+
 /* --- A paged key-value cache -------------------------------------------------------------------------------------
  * Pages of page_tokens tokens, for all layers at once: page p of layer l holds keys as [kv_head][token][d_head] and
- * values as [kv_head][d_head][token], so that the matrix units take both as they lie.  Sequence s holds the pages
+ * values as [kv_head][d_head][token], so that the matrix units take both as they lie (in SIF_E2M1 as told below).  Sequence s holds the pages
  * table[s][0 .. ceil(lengths[s] / page_tokens) - 1], every other entry of its row is -1; a page may belong to several sequences,
  * refs[p] says to how many; refs[p] = 0 is a free page.  The caller owns all of it; the operations below keep it in
  * order on the device, in stream order, without a host synchronisation (they can be captured into a graph).  All of
@@ -351,10 +402,17 @@ uint64_t sif_window_attn_bwd_workspace_bytes(const sif_window_attn_args* a);    
  * Lists: seqs_dev names n sequences (int32; null = 0 .. n-1).  A sequence number outside 0 .. n_seqs-1, and a
  * sequence that was listed before in the same call, is left out.  status_dev (int32 [n], may be null) receives SIF_OK
  * or what was wrong with an entry; an entry in error changes nothing.  A page number outside 0 .. n_pages-1 in a table row
- * stands for no page.  The page operations take n from 1 to 1024. */
+ * stands for no page.  The page operations take n from 1 to 1024.
+ * In SIF_E2M1 32 consecutive elements of a token's head are held as x / 2^e in 4 bits each and one byte e + 127 (255: all of them are NaN); a kv head's
+ * part of a page has page_tokens * d_head * 17 / 32 bytes:
+ *   keys    [token][d_head / 2], element 2i in the lower half of byte i, 2i + 1 in the upper one;    then [d_head / 32][token] bytes e + 127
+ *   values  [d_head / 32][16][token], element 32b + c in the lower half of byte (b, c), 32b + c + 16 in the upper one;    then [token][d_head / 32] bytes
+ * Written there, e is the smallest from -127 to 127 with |x| <= 7 2^e for all 32, and each x / 2^e goes to the nearest of the values, from the middle to
+ * the one with an even mantissa, so that no element is more than half a step off (-0 stays -0); infinities count as the largest number in bf16 and are held as +-6 2^e, one NaN makes
+ * NaN of its 32. */
 typedef struct sif_kv_cache {
   uint32_t struct_size;
-  uint32_t dtype;                     /* SIF_BF16 or SIF_E4M3                                                        */
+  uint32_t dtype;                     /* SIF_BF16, SIF_E4M3 or SIF_E2M1                                              */
   uint32_t layers, kv_heads, d_head;  /* d_head 64 or 128                                                            */
   uint32_t page_tokens;               /* 16, 32, 64, 128 or 256                                                      */
   uint32_t n_pages, n_seqs, table_ld; /* n_pages at most 2^21; table_ld: pages that a row of the table holds           */
@@ -386,6 +444,29 @@ sif_status sif_k_kv_extend(const sif_kv_cache* c, const int32_t* seqs_dev, const
  * by the tokens before they are written leaves them in pages of the sequence's own). */
 sif_status sif_k_kv_write(const sif_kv_cache* c, uint32_t layer, const void* k_dev, const void* v_dev, uint32_t ld_k, uint32_t ld_v,
                           const int32_t* seqs_dev, const int32_t* starts_dev, uint32_t n, uint32_t rows, void* stream);
+/* sif_k_kv_write with the rotation on the way: a token's position is its place in its sequence, from 0.  Keys are turned and then written as above, rounded once (to 8 and 4 bits from products in 64 bits: next to
+ * a border between two of their values a last bit decides about a whole step); values are written as they are.  With heads > 0 the same rows of q
+ * are turned into q_out, also those of a sequence that was listed before and of tokens without a page; rows of no sequence stay as they were.  q_out may be q (with the same leading dimension). */
+typedef struct sif_kv_append_args {
+  uint32_t struct_size;
+  uint32_t layer, n, rows;            /* as sif_k_kv_write                                                           */
+  uint32_t heads;                     /* of q: any number, at most 1024; 0 = no q                                    */
+  uint32_t ld_q, ld_q_out, ld_k, ld_v;
+  uint32_t reserved;
+  const int32_t* seqs_dev;
+  const int32_t* starts_dev;
+  const void* k_dev; const void* v_dev;
+  const void* q_dev; void* q_out_dev;
+} sif_kv_append_args;
+
+/* rope->rot_dim at most d_head */
+sif_status sif_k_kv_append(const sif_kv_cache* c, const sif_rope* r, const sif_kv_append_args* a, void* stream);
+/* Reads rows back: rows starts[i] .. starts[i+1] - 1 of k and v (bf16) become the keys and values that the cache holds of the last tokens of sequence i of
+ * the list, in SIF_E4M3 times their scales, rounded to bf16.  With starts as far apart as the sequences are long, whole sequences: what sif_k_window_attn_fwd takes as
+ * k and v of a prompt's next piece.  Tokens in front of the sequence's first one, and tokens without a page, give zeros; rows of no sequence stay as they were.
+ * A sequence may be listed more than once.  Arguments as sif_k_kv_write. */
+sif_status sif_k_kv_read(const sif_kv_cache* c, uint32_t layer, void* k_dev, void* v_dev, uint32_t ld_k, uint32_t ld_v,
+                         const int32_t* seqs_dev, const int32_t* starts_dev, uint32_t n, uint32_t rows, void* stream);
 /* Sequence dst[i] becomes a copy of src[i] and shares its pages.  Status SIF_E_INVAL: a number outside the table, a dst that is
  * not empty or was listed before, a src that is listed as a dst. */
 sif_status sif_k_kv_fork(const sif_kv_cache* c, const int32_t* src_dev, const int32_t* dst_dev, uint32_t n, int32_t* status_dev, void* stream);
@@ -439,6 +520,38 @@ sif_status sif_k_embed_bwd(const int32_t* ids_dev, const void* dx_dev, void* dwt
  * vocab..ld-1 set to zero. */
 sif_status sif_k_xent_fwd_bwd(void* logits_dev, const int32_t* targets_dev, float* loss_dev, uint32_t tokens,
                               uint32_t vocab, uint32_t ld, void* stream);
+/* --- A token for every row of logits -------------------------------------------------------------------------------
+ * Of a row's tokens (a logit of -inf or NaN is none) these are left, in this order:
+ *   top_k > 0      the top_k with the largest logits, of equal ones those with the lowest numbers
+ *   top_p < 1      of these the fewest, most probable first (equal ones as before), whose probabilities exp(l / temperature) make up at least top_p of
+ *                  the sum of what top_k left; at least one
+ *   min_p > 0      those at least min_p (held to 1) times as probable as the most probable one
+ * and the token is the first, in the order of their numbers, at which the sum of the probabilities exceeds random (held to 0 .. 1 - 2^-24, NaN counts as 0) times that of all that are
+ * left.  A temperature that is not above 0: the largest logit's token, of equal ones the lowest number.  Logits of +inf leave no probability to others.
+ * Probabilities are taken in 64 bits and added as integers of at least 2^-44 of the largest one, so the answer does not depend on the order of additions.  A row without a token gets -1.
+ * kept: how many tokens were left (1 where the temperature is not above 0); logprob: the log of the token's share of their sum (-inf for no token). */
+typedef struct sif_sample_args {
+  uint32_t struct_size;
+  uint32_t dtype;                     /* SIF_F32 or SIF_BF16                                                         */
+  uint32_t n, vocab, ld;              /* rows (at most 2^20), tokens (at most 2^18), elements from a row to the next (a multiple of 8) */
+  float temperature;                  /* for rows whose list is null, so too the next three; 0 = greedy, not negative, not NaN */
+  int32_t top_k;                      /* not above 0: no limit                                                        */
+  float top_p;                        /* 1 or more, or NaN: no limit                                                 */
+  float min_p;                        /* not above 0: no limit                                                        */
+  uint32_t reserved;
+  const float* temperature_dev;       /* [n] or null, so too the next three                                          */
+  const int32_t* top_k_dev;
+  const float* top_p_dev;
+  const float* min_p_dev;
+  const void* logits_dev;             /* [n][ld], 16-byte aligned                                                    */
+  const float* random_dev;            /* [n], in [0, 1); null only with temperature = 0 for all rows                  */
+  int32_t* token_dev;                 /* [n]                                                                         */
+  float* logprob_dev;                 /* [n] or null                                                                 */
+  int32_t* kept_dev;                  /* [n] or null                                                                 */
+} sif_sample_args;
+
+sif_status sif_k_sample(const sif_sample_args* a, void* stream);
+
 /* out[0] = scale * sum x[0..n)  fixed order, one block (fp32) */
 sif_status sif_k_reduce_sum(const float* x_dev, float* out_dev, uint32_t n, float scale, void* stream);
 

@@ -21,7 +21,9 @@ u32, u64, i32, i64, f32, vp = C.c_uint32, C.c_uint64, C.c_int32, C.c_int64, C.c_
 # status codes / enums (mirrors of the header)
 SIF_OK, SIF_W_SLO_RISK = 0, 1
 SIF_E_INVAL, SIF_E_NOMEM, SIF_E_AGAIN, SIF_E_CANCELLED, SIF_E_TIMEOUT, SIF_E_DEVICE = -1, -2, -3, -4, -5, -6
-SIF_F32, SIF_BF16, SIF_E4M3 = 0, 1, 2
+SIF_F32, SIF_BF16, SIF_E4M3, SIF_E2M1 = 0, 1, 2, 3
+SIF_ROPE_HALF, SIF_ROPE_INTERLEAVED = 0, 1
+SIF_ROPE_PLAIN, SIF_ROPE_LINEAR, SIF_ROPE_BASE, SIF_ROPE_PARTS = 0, 1, 2, 3
 SIF_STATUS_BUSY, SIF_STATUS_IDLE = 0, 1
 SIF_A_ROW_K, SIF_A_ROW_M = 0, 1
 SIF_B_ROW_K, SIF_B_ROW_N = 0, 1
@@ -614,6 +616,37 @@ class sif_attn_decode_args(C.Structure):
                 ("workspace_dev", vp), ("workspace_bytes", u64)]
 
 
+class sif_rope_desc(C.Structure):
+    _fields_ = [("struct_size", u32), ("layout", u32), ("rot_dim", u32), ("scaling", u32), ("base", C.c_double), ("factor", C.c_double),
+                ("low_turns", C.c_double), ("high_turns", C.c_double), ("trained_tokens", C.c_double), ("magnitude", C.c_double)]
+
+
+class sif_rope(C.Structure):
+    _fields_ = [("struct_size", u32), ("layout", u32), ("rot_dim", u32), ("reserved", u32), ("magnitude", C.c_double), ("turns", C.c_double * 128)]
+
+
+class sif_rope_args(C.Structure):
+    _fields_ = [("struct_size", u32), ("rows", u32), ("heads", u32), ("kv_heads", u32), ("d_head", u32), ("seq", u32), ("first", i32), ("inverse", u32),
+                ("ld_q", u32), ("ld_q_out", u32), ("ld_k", u32), ("ld_k_out", u32), ("positions_dev", vp), ("q_dev", vp), ("q_out_dev", vp),
+                ("k_dev", vp), ("k_out_dev", vp)]
+
+
+class sif_kv_append_args(C.Structure):
+    _fields_ = [("struct_size", u32), ("layer", u32), ("n", u32), ("rows", u32), ("heads", u32), ("ld_q", u32), ("ld_q_out", u32), ("ld_k", u32),
+                ("ld_v", u32), ("reserved", u32), ("seqs_dev", vp), ("starts_dev", vp), ("k_dev", vp), ("v_dev", vp), ("q_dev", vp), ("q_out_dev", vp)]
+
+
+class sif_sample_args(C.Structure):
+    _fields_ = [("struct_size", u32), ("dtype", u32), ("n", u32), ("vocab", u32), ("ld", u32), ("temperature", f32), ("top_k", i32), ("top_p", f32),
+                ("min_p", f32), ("reserved", u32), ("temperature_dev", vp), ("top_k_dev", vp), ("top_p_dev", vp), ("min_p_dev", vp), ("logits_dev", vp),
+                ("random_dev", vp), ("token_dev", vp), ("logprob_dev", vp), ("kept_dev", vp)]
+
+
+_sig("sif_rope_plan", i32, P(sif_rope_desc), P(sif_rope))
+_sig("sif_k_rope", i32, P(sif_rope), P(sif_rope_args), vp)
+_sig("sif_k_kv_append", i32, P(sif_kv_cache), P(sif_rope), P(sif_kv_append_args), vp)
+_sig("sif_k_kv_read", i32, P(sif_kv_cache), u32, vp, vp, u32, u32, vp, vp, u32, u32, vp)
+_sig("sif_k_sample", i32, P(sif_sample_args), vp)
 _sig("sif_k_window_attn_fwd", i32, P(sif_window_attn_args), vp)
 _sig("sif_k_window_attn_bwd", i32, P(sif_window_attn_args), vp)
 _sig("sif_window_attn_bwd_workspace_bytes", u64, P(sif_window_attn_args))
@@ -704,14 +737,19 @@ def sif_k_window_attn_bwd(a, stream=None):
 
 
 def kv_cache(k, v, table, lengths, refs, dtype, page_tokens, k_scale=None, v_scale=None):
-    """A filled sif_kv_cache for k [layers][pages][kv_heads][page_tokens][d_head], v [layers][pages][kv_heads][d_head][page_tokens],
-    table [sequences][pages of a row], lengths [sequences] and refs [pages] (the tensors stay the caller's to keep)."""
+    """A filled sif_kv_cache for k [layers][pages][kv_heads][page_tokens][d_head], v [layers][pages][kv_heads][d_head][page_tokens] (in SIF_E2M1 both
+    uint8 [layers][pages][kv_heads][page_tokens * d_head * 17 / 32], layouts as the header tells), table [sequences][pages of a row], lengths [sequences] and refs [pages] (the tensors stay the caller's to keep)."""
     c = sif_kv_cache()
     c.struct_size = C.sizeof(sif_kv_cache)
-    layers, n_pages, kv_heads, d_head = k.shape[0], k.shape[1], k.shape[2], k.shape[4]
-    size = {SIF_BF16: 2, SIF_E4M3: 1}.get(dtype)
-    ok = tuple(k.shape) == (layers, n_pages, kv_heads, page_tokens, d_head) and tuple(v.shape) == (layers, n_pages, kv_heads, d_head, page_tokens)
-    ok = ok and size == k.element_size() == v.element_size() and all(t.is_contiguous() for t in (k, v, table, lengths, refs))
+    layers, n_pages, kv_heads = k.shape[0], k.shape[1], k.shape[2]
+    if dtype == SIF_E2M1:
+        d_head = k.shape[-1] * 32 // (17 * max(page_tokens, 1))
+        ok = tuple(k.shape) == tuple(v.shape) == (layers, n_pages, kv_heads, page_tokens * d_head * 17 // 32) and k.dtype == v.dtype == torch.uint8
+    else:
+        size, d_head = {SIF_BF16: 2, SIF_E4M3: 1}.get(dtype), k.shape[-1]
+        ok = tuple(k.shape) == (layers, n_pages, kv_heads, page_tokens, d_head) and tuple(v.shape) == (layers, n_pages, kv_heads, d_head, page_tokens)
+        ok = ok and size == k.element_size() == v.element_size()
+    ok = ok and all(t.is_contiguous() for t in (k, v, table, lengths, refs))
     ok = ok and lengths.shape[0] == table.shape[0] and refs.shape[0] == n_pages and all(t.dtype == torch.int32 for t in (table, lengths, refs))
     ok = ok and all(t is None or (t.dtype == torch.float32 and t.is_contiguous() and tuple(t.shape) == (layers, kv_heads)) for t in (k_scale, v_scale))
     if not ok:
@@ -743,6 +781,29 @@ def sif_k_kv_write(c, layer, k, v, seqs, n, starts=None, rows=None, ld_k=None, l
     width = c.kv_heads * c.d_head
     return check(lib.sif_k_kv_write(c, layer, _rows(k, "k"), _rows(v, "v"), _ld(k, ld_k, width), _ld(v, ld_v, width), _list(seqs, n, "seqs"),
                                     _list(starts, n + 1, "starts"), n, n if rows is None else rows, stream_ptr(stream)))
+
+
+def kv_append_args(k, v, n, rows=None, layer=0, seqs=None, starts=None, q=None, q_out=None, heads=0, ld_q=None, ld_q_out=None, ld_k=None, ld_v=None):
+    """A filled sif_kv_append_args (the tensors stay the caller's to keep).  q_out None: in q's place."""
+    a = sif_kv_append_args()
+    a.struct_size = C.sizeof(sif_kv_append_args)
+    if q_out is None:
+        q_out, ld_q_out = q, ld_q
+    a.layer, a.n, a.rows, a.heads = layer, n, n if rows is None else rows, heads
+    a.ld_q, a.ld_q_out, a.ld_k, a.ld_v = _ld(q, ld_q, 0), _ld(q_out, ld_q_out, 0), _ld(k, ld_k, 0), _ld(v, ld_v, 0)
+    a.seqs_dev, a.starts_dev = _list(seqs, n, "seqs"), _list(starts, n + 1, "starts")
+    a.k_dev, a.v_dev, a.q_dev, a.q_out_dev = _rows(k, "k"), _rows(v, "v"), _rows(q, "q"), _rows(q_out, "q_out")
+    return a
+
+
+def sif_k_kv_append(c, rope, a, stream=None):
+    return check(lib.sif_k_kv_append(c, rope, a, stream_ptr(stream)))
+
+
+def sif_k_kv_read(c, layer, k, v, seqs, n, starts=None, rows=None, ld_k=None, ld_v=None, stream=None):
+    width = c.kv_heads * c.d_head
+    return check(lib.sif_k_kv_read(c, layer, _rows(k, "k"), _rows(v, "v"), _ld(k, ld_k, width), _ld(v, ld_v, width), _list(seqs, n, "seqs"),
+                                   _list(starts, n + 1, "starts"), n, n if rows is None else rows, stream_ptr(stream)))
 
 
 def sif_k_kv_fork(c, src, dst, n, status=None, stream=None):
@@ -786,3 +847,57 @@ def sif_attn_decode_workspace_bytes(c, a):
 
 def sif_k_attn_decode(c, a, stream=None):
     return check(lib.sif_k_attn_decode(c, a, stream_ptr(stream)))
+
+
+# ---- rotary positions; a token for every row of logits -----------------------------------------------------------------
+def rope_plan(rot_dim, layout=SIF_ROPE_HALF, base=10000.0, scaling=SIF_ROPE_PLAIN, factor=1.0, low_turns=1.0, high_turns=32.0, trained_tokens=0.0, magnitude=1.0):
+    """The table of a rotation that sif_k_rope and sif_k_kv_append take."""
+    d, r = sif_rope_desc(), sif_rope()
+    d.struct_size = C.sizeof(sif_rope_desc)
+    d.layout, d.rot_dim, d.scaling, d.base, d.factor, d.magnitude = layout, rot_dim, scaling, base, factor, magnitude
+    d.low_turns, d.high_turns, d.trained_tokens = low_turns, high_turns, trained_tokens
+    check(lib.sif_rope_plan(d, r))
+    return r
+
+
+def rope_args(q, q_out, rows, heads, d_head, k=None, k_out=None, kv_heads=0, positions=None, seq=0, first=0, inverse=False, ld_q=None, ld_q_out=None, ld_k=None, ld_k_out=None):
+    """A filled sif_rope_args (the tensors stay the caller's to keep)."""
+    a = sif_rope_args()
+    a.struct_size = C.sizeof(sif_rope_args)
+    wq, wk = heads * d_head, kv_heads * d_head
+    a.rows, a.heads, a.kv_heads, a.d_head, a.seq, a.first, a.inverse = rows, heads, kv_heads, d_head, seq, first, 1 if inverse else 0
+    a.ld_q, a.ld_q_out, a.ld_k, a.ld_k_out = _ld(q, ld_q, wq), _ld(q_out, ld_q_out, wq), _ld(k, ld_k, wk), _ld(k_out, ld_k_out, wk)
+    a.positions_dev = _list(positions, rows, "positions")
+    a.q_dev, a.q_out_dev, a.k_dev, a.k_out_dev = _rows(q, "q"), _rows(q_out, "q_out"), _rows(k, "k"), _rows(k_out, "k_out")
+    return a
+
+
+def sif_k_rope(rope, a, stream=None):
+    return check(lib.sif_k_rope(rope, a, stream_ptr(stream)))
+
+
+def sample_args(logits, token, n, vocab, random=None, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, logprob=None, kept=None, ld=None):
+    """A filled sif_sample_args (the tensors stay the caller's to keep).  temperature, top_k, top_p and min_p are numbers, or tensors with one for each row."""
+    if not isinstance(logits, _Tensor) or logits.dtype not in (_BF16, _FP32) or not (logits.is_contiguous() or logits.dim() == 2 and (logits.stride(1) == 1 or logits.shape[1] == 1)):
+        raise SifError(SIF_E_INVAL, "logits must be bfloat16 or float32, a row's side by side")
+
+    def numbers(t, what):
+        if isinstance(t, _Tensor) and not (t.dtype is _FP32 and t.is_contiguous() and t.numel() >= n):
+            raise SifError(SIF_E_INVAL, f"{what} must be a contiguous float32 tensor of {n} numbers")
+        return ptr(t)
+    a = sif_sample_args()
+    a.struct_size = C.sizeof(sif_sample_args)
+    a.dtype, a.n, a.vocab, a.ld = SIF_F32 if logits.dtype is _FP32 else SIF_BF16, n, vocab, _ld(logits, ld, vocab)
+    for name, x in (("temperature", temperature), ("top_p", top_p), ("min_p", min_p)):
+        setattr(a, name + "_dev" if isinstance(x, _Tensor) else name, numbers(x, name) if isinstance(x, _Tensor) else x)
+    if isinstance(top_k, _Tensor):
+        a.top_k_dev = _list(top_k, n, "top_k")
+    else:
+        a.top_k = top_k
+    a.logits_dev, a.random_dev, a.logprob_dev = ptr(logits), numbers(random, "random"), numbers(logprob, "logprob")
+    a.token_dev, a.kept_dev = _list(token, n, "token"), _list(kept, n, "kept")
+    return a
+
+
+def sif_k_sample(a, stream=None):
+    return check(lib.sif_k_sample(a, stream_ptr(stream)))

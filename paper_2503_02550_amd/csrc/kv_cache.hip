@@ -3,13 +3,14 @@
 // order of blocks: reference counts are sums, and who gets which page follows from a rank in the list of free pages.
 #include "common.h"
 #include "kv_cache.h"
+#include "kv_rows.h"
 
 namespace sif {
 
 sif_status kv_check(const char* who, const sif_kv_cache* c, KvView* out) {
   if (!c) return fail(SIF_E_INVAL, "%s: null cache", who);
   if (c->struct_size != sizeof(sif_kv_cache)) return fail(SIF_E_INVAL, "%s: struct_size of the cache", who);
-  if (c->dtype != SIF_BF16 && c->dtype != SIF_E4M3) return fail(SIF_E_INVAL, "%s: dtype must be SIF_BF16 or SIF_E4M3", who);
+  if (c->dtype != SIF_BF16 && c->dtype != SIF_E4M3 && c->dtype != SIF_E2M1) return fail(SIF_E_INVAL, "%s: dtype must be SIF_BF16, SIF_E4M3 or SIF_E2M1", who);
   if (!c->layers || !c->kv_heads || !c->n_pages || !c->n_seqs || !c->table_ld) return fail(SIF_E_INVAL, "%s: empty extent", who);
   if (c->d_head != 64 && c->d_head != 128) return fail(SIF_E_INVAL, "%s: d_head must be 64 or 128", who);
   const uint32_t pt = c->page_tokens;
@@ -18,7 +19,7 @@ sif_status kv_check(const char* who, const sif_kv_cache* c, KvView* out) {
   if (((uintptr_t)c->k_dev | (uintptr_t)c->v_dev | (uintptr_t)c->refs_dev) & 15) return fail(SIF_E_INVAL, "%s: k, v and refs must be 16-byte aligned", who);
   if (((uintptr_t)c->table_dev | (uintptr_t)c->lengths_dev | (uintptr_t)c->k_scale_dev | (uintptr_t)c->v_scale_dev) & 3)
     return fail(SIF_E_INVAL, "%s: misaligned operand", who);
-  if (c->dtype == SIF_BF16 && (c->k_scale_dev || c->v_scale_dev)) return fail(SIF_E_INVAL, "%s: scales belong to SIF_E4M3", who);
+  if (c->dtype != SIF_E4M3 && (c->k_scale_dev || c->v_scale_dev)) return fail(SIF_E_INVAL, "%s: scales belong to SIF_E4M3", who);
   if (c->layers > 1024 || c->kv_heads > 1024) return fail(SIF_E_INVAL, "%s: at most 1024 layers and 1024 kv_heads", who);
   if ((uint64_t)c->table_ld * pt > 0x7FFFFF00ull || c->n_seqs > 0x7FFFFF00u)
     return fail(SIF_E_INVAL, "%s: tokens of a row or sequences beyond 31 bits", who);
@@ -38,7 +39,8 @@ sif_status kv_check(const char* who, const sif_kv_cache* c, KvView* out) {
   v.n_pages = c->n_pages;
   v.n_seqs = c->n_seqs;
   v.table_ld = c->table_ld;
-  v.page_bytes = c->kv_heads * pt * c->d_head * (c->dtype == SIF_BF16 ? 2u : 1u);      // at most 64 MB
+  const uint32_t values = c->kv_heads * pt * c->d_head;
+  v.page_bytes = c->dtype == SIF_BF16 ? 2 * values : c->dtype == SIF_E4M3 ? values : values / 32 * 17;      // at most 64 MB, multiples of 16
   *out = v;
   return SIF_OK;
 }
@@ -268,7 +270,7 @@ __device__ __forceinline__ void kv_copy_page(const KvView& c, uint32_t part, int
   typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
   const u32x4* a = reinterpret_cast<const u32x4*>(pool + (size_t)from * c.page_bytes);
   u32x4* b = reinterpret_cast<u32x4*>(pool + (size_t)to * c.page_bytes);
-  const uint32_t m = c.page_bytes / 16;          // a page has at least 1 KB
+  const uint32_t m = c.page_bytes / 16;          // a page has at least 544 bytes
   for (uint32_t base = threadIdx.x; base < m; base += 256 * 8) {
     u32x4 v[8];
 #pragma unroll
@@ -361,13 +363,6 @@ __global__ __launch_bounds__(256) void kv_move_kernel(KvView c, KvWork w) {
     const uint32_t r = (uint32_t)(i / parts);
     kv_copy_page<true>(c, (uint32_t)(i % parts), w.high[r], w.low[r]);
   }
-}
-
-// float -> e4m3, held at +-448, NaN kept; two at a time into the low half of a word
-__device__ __forceinline__ uint32_t kv_e4m3x2(float a, float b) {
-  a = a != a ? a : fminf(fmaxf(a, -448.f), 448.f);
-  b = b != b ? b : fminf(fmaxf(b, -448.f), 448.f);
-  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false) & 0xFFFFu;
 }
 
 // Write: a block takes 16 rows of one kv head.  Keys go out as the 16-byte vectors they come in as; values pass through LDS, so that
@@ -505,6 +500,7 @@ sif_status sif_k_kv_write(const sif_kv_cache* c, uint32_t layer, const void* k, 
   if (starts == nullptr && rows != n) return fail(SIF_E_INVAL, "kv_write: without starts there is one row per entry");
   const uint32_t width = w.kv_heads * w.d_head;
   if (ld_k < width || ld_v < width || ((ld_k | ld_v) & 7)) return fail(SIF_E_INVAL, "kv_write: bad leading dimensions");
+  if (c->dtype == SIF_E2M1) return kv_write_4bit(w, w.d_head, layer, k, v, ld_k, ld_v, KvRowList{seqs, starts, n, rows}, S(stream));
   const dim3 grid((rows + 15) / 16, w.kv_heads);
 #define KV_LAUNCH(DH, E) hipLaunchKernelGGL((kv_write_kernel<DH, E>), grid, dim3(256), 0, S(stream), w, layer, (const bf16_t*)k, (const bf16_t*)v, ld_k, ld_v, \
                                             seqs, starts, n, rows)

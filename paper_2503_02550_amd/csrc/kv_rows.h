@@ -1,0 +1,60 @@
+// Which token a row of new or read-back keys and values is, for the kernels that take rows by the list of a paged cache's sequences.
+#pragma once
+#include "common.h"
+#include "kv_cache.h"
+
+namespace sif {
+
+constexpr uint32_t kKvRows = 16;         // rows of a block, sixteen threads each
+
+// Rows row0 .. row0 + 15 of lists as in sif_k_kv_write: pos the row's place in its sequence (kNoRow: the row is no sequence's; kBefore: it lies in
+// front of the sequence's first token), page its page or -1.  With `once` a sequence that stands in the list before has no page either.
+constexpr uint32_t kNoRow = 0xFFFFFFFFu, kBefore = 0xFFFFFFFEu;
+struct KvRowList { const int32_t* seqs; const int32_t* starts; uint32_t n, rows; };
+__device__ __forceinline__ void kv_find_rows(const KvView& c, const KvRowList& l, uint32_t row0, bool once, uint32_t* s_pos, int32_t* s_page) {
+  const uint32_t t = threadIdx.x, r = t >> 4, row = row0 + r;
+  uint32_t i = row, pos = kNoRow;
+  int32_t s = -1;
+  if (row < l.rows) {
+    uint32_t from = row, to = row + 1;
+    if (l.starts != nullptr) {
+      uint32_t lo = 0, hi = l.n;                 // the last entry that begins at or before the row
+      while (lo < hi) {
+        const uint32_t mid = (lo + hi) >> 1;
+        if (l.starts[mid] <= (int32_t)row) lo = mid + 1; else hi = mid;
+      }
+      i = lo - 1;
+      from = lo > 0 ? (uint32_t)l.starts[i] : 0u;
+      to = lo > 0 ? (uint32_t)l.starts[i + 1] : 0u;
+    }
+    if (i < l.n && from <= row && row < to) {
+      s = kv_listed(c, l.seqs, i);
+      if (s >= 0) {
+        const uint32_t len = kv_length(c, s), back = to - row;
+        pos = back <= len ? len - back : kBefore;
+      }
+    }
+  }
+  bool again = false;
+  if (once && s >= 0 && l.seqs != nullptr)
+    for (uint32_t j = t & 15; j < i; j += 16) again |= l.seqs[j] == s;
+  const uint64_t votes = __ballot(again);
+  if ((t & 15) == 0) {
+    int32_t p = -1;
+    if (pos < kBefore && ((votes >> (t & 63)) & 0xFFFFull) == 0) p = c.table[(size_t)s * c.table_ld + (pos >> c.page_lg)];
+    s_page[r] = (uint32_t)p < c.n_pages ? p : -1;
+    s_pos[r] = pos;
+  }
+}
+
+// float -> e4m3, held at +-448, NaN kept; two at a time into the low half of a word
+__device__ __forceinline__ uint32_t kv_e4m3x2(float a, float b) {
+  a = a != a ? a : fminf(fmaxf(a, -448.f), 448.f);
+  b = b != b ? b : fminf(fmaxf(b, -448.f), 448.f);
+  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false) & 0xFFFFu;
+}
+
+// What sif_k_kv_write does for a cache in 4 bits (kv_rows.hip); arguments as checked there.
+sif_status kv_write_4bit(const KvView& c, uint32_t d_head, uint32_t layer, const void* k, const void* v, uint32_t ld_k, uint32_t ld_v, const KvRowList& l, hipStream_t s);
+
+}  // namespace sif

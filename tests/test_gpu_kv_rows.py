@@ -1,0 +1,223 @@
+"""New tokens into a paged cache of every format with the rotation on the way, and back out of it, byte by byte."""
+import math
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+from rows_reference import HALF, Rows, frequencies, turned
+
+if torch.cuda.is_available():
+    import paper_2503_02550_amd as S
+    from gpu_util import DEV
+
+FORMATS = ["bf16", "e4m3", "e2m1"]
+
+
+def _x(seed, rows, width):
+    return torch.randn(rows, width, generator=torch.Generator().manual_seed(seed)).to(torch.bfloat16)
+
+
+def _i32(x):
+    return None if x is None else torch.tensor(list(x), dtype=torch.int32, device=DEV)
+
+
+def _wide(x, pad=8, fill=math.nan):
+    w = torch.full((x.shape[0], x.shape[1] + pad), fill, dtype=torch.bfloat16, device=DEV)
+    w[:, :x.shape[1]] = x.to(DEV)
+    return w
+
+
+def _rows_of(rows, seqs, starts, n, count):
+    """(row, sequence, position, whether the sequence was listed before) of the rows that are a sequence's."""
+    got, before = [], set()
+    for i in range(n):
+        s = i if seqs is None else seqs[i]
+        a, b = (i, i + 1) if starts is None else (starts[i], starts[i + 1])
+        ok, again = 0 <= s < len(rows.lens), s in before
+        before.add(s)
+        for r in range(max(a, 0), min(b, count)):
+            if ok:
+                got.append((r, s, rows.lens[s] - (b - r), again))
+    return got
+
+
+def _append(rows, layer, heads, seqs, starts, n, count, rot, inter=False, m=1.0, there=False, seed=1, k=None, v=None):
+    """One call, and what it must leave behind."""
+    h, d = rows.h, rows.d
+    q = _x(seed, count, max(heads, 1) * d)
+    k, v = _x(seed + 1, count, h * d) if k is None else k, _x(seed + 2, count, h * d) if v is None else v
+    f = frequencies(rot)
+    rope = S.rope_plan(rot, layout=S.SIF_ROPE_INTERLEAVED if inter else S.SIF_ROPE_HALF, magnitude=m)
+    cache = rows.on(S, DEV)
+    wq, wk, wv = _wide(q, fill=7.0), _wide(k), _wide(v, 16)
+    out = wq if there else _wide(torch.full_like(q, 7.0), 16, 7.0)
+    a = S.kv_append_args(wk, wv, n, rows=count, layer=layer, seqs=_i32(seqs), starts=_i32(starts), q=wq if heads else None, q_out=out if heads else None, heads=heads)
+    S.sif_k_kv_append(cache, rope, a)
+    torch.cuda.synchronize()
+    want_q, off_q = q.double() if there else torch.full_like(q, 7.0).double(), torch.zeros(q.shape, dtype=torch.float64)
+    slack = {}
+    for r, s, pos, again in _rows_of(rows, seqs, starts, n, count):
+        if pos < 0:
+            continue
+        p = torch.tensor([pos])
+        if heads:
+            val, off = turned(q[r].double().view(1, heads, d), p, f, inter, m)
+            want_q[r], off_q[r] = val.flatten(), HALF * val.flatten().abs() + (1 + HALF) * off.flatten() + 1e-38
+            off_q[r].view(heads, d)[:, rot:] = 0
+        if not again:
+            val, off = turned(k[r].double().view(1, h, d), p, f, inter, m)
+            rows.put("k", layer, s, pos, val[0])
+            rows.put("v", layer, s, pos, v[r].double().view(h, d))
+            if rows.place(s, pos) >= 0:
+                slack[(rows.place(s, pos), pos % rows.page)] = (val[0], HALF * val[0].abs() + (1 + HALF) * off[0] + 1e-38)
+    assert torch.all((out[:, :q.shape[1]].cpu().double() - want_q).abs() <= off_q)
+    assert bool((out[:, q.shape[1]:] == 7.0).all())
+    if rows.dtype == "bf16":
+        # turned keys are rounded to bf16 from fp32: within half a step and what that is off, no more, and everything else is equal
+        got = rows.t["k"].cpu()
+        for (page, t), (val, off) in slack.items():
+            y = got[layer, page, :, t].double()
+            assert torch.all((y == val) | ((y - val).abs() <= off) | (y.isnan() & val.isnan()))      # (infinities are equal, their difference is none)
+            rows.code["k"][layer, page, :, t] = got[layer, page, :, t]
+    rows.check()
+
+
+@pytest.mark.parametrize("dtype", FORMATS)
+@pytest.mark.parametrize("d,kv,heads,rot,page", [(64, 2, 6, 64, 16), (64, 3, 3, 32, 32), (128, 1, 4, 128, 64), (128, 2, 2, 48, 16), (64, 1, 0, 16, 256), (128, 5, 40, 112, 128)])
+def test_one_token_each(dtype, d, kv, heads, rot, page):
+    lens = [1, page, page + 1, 77, 2, 3 * page, 40]
+    for inter in (False, True):
+        rows = Rows(dtype, lens, page, kv, d, seed=rot)
+        _append(rows, 1, heads, None, None, len(lens), len(lens), rot, inter, there=inter)
+        _append(rows, 0, heads, [5, 0, 3], None, 3, 3, rot, inter, m=1.3, seed=9)
+
+
+@pytest.mark.parametrize("dtype", FORMATS)
+@pytest.mark.parametrize("inter", [False, True])
+def test_prompts_of_unequal_length(dtype, inter):
+    lens = [100, 0, 31, 64, 5, 200]
+    rows = Rows(dtype, lens, 16, 3, 64, seed=2)
+    starts = [2, 47, 47, 78, 80, 85, 140]                 # rows 0, 1 and 140 .. belong to nobody, one sequence gets nothing, one its whole length
+    _append(rows, 1, 6, None, starts, 6, 145, 64, inter)
+    rows = Rows(dtype, lens, 64, 2, 128, seed=3)
+    _append(rows, 0, 2, [5, 2, 0, 3], [0, 199, 230, 300, 301], 4, 301, 96, inter, there=True)
+
+
+@pytest.mark.parametrize("dtype", FORMATS)
+def test_lists_that_leave_rows_out(dtype):
+    """Unknown numbers, sequences that are listed twice, tokens in front of the first one and without a page."""
+    rows = Rows(dtype, [20, 40, 9, 70], 16, 2, 64, seed=4, spare=4)
+    rows.table[1][1], rows.table[3][2] = -1, 10 ** 6
+    _append(rows, 1, 4, [1, 9, 1, -1, 0, 3, 0, 2], [0, 40, 43, 50, 52, 60, 100, 103, 120], 8, 120, 64)
+
+
+@pytest.mark.parametrize("dtype", FORMATS)
+def test_special_values(dtype):
+    rows = Rows(dtype, [37, 5], 32, 2, 128, seed=5)
+    k, v = _x(6, 6, 256), _x(7, 6, 256)
+    k[0, 3], v[0, 200], k[1, 40:72], v[2, 0] = math.nan, math.nan, 0.0, -math.inf
+    v[3, :64], k[4, 128:] = -0.0, 0.0
+    k[2, 100], v[4, 5] = math.inf, 3.3895313892515355e38
+    v[5, 0:32], v[5, 32:64] = 2.0 ** -120, 1.2e-38                 # powers near their least
+    _append(rows, 0, 0, None, [0, 5, 6], 2, 6, 16, k=k, v=v)      # (what is not finite lies behind the rotated elements)
+
+
+def test_values_next_to_a_border():
+    """Turned keys whose 4-bit codes hang on the last bits: at position 0 nothing is turned, so elements stand on borders exactly, a bf16 step to either side of them, and scaled by a
+    magnitude that is no power of two."""
+    ties = torch.tensor([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, 7.0])
+    rowsv = []
+    for up in (1.0, 1 + 2.0 ** -7, 1 - 2.0 ** -8):
+        x = torch.cat([ties * up, -ties * up, ties, torch.tensor([7.0, 6.0, 0, 0, 1, 2, 3, 4])]).repeat(2)
+        rowsv.append(x)
+    for m in (1.0, 1 / 3, 0.7, 2.0 ** 0.5):
+        for i, x in enumerate(rowsv):
+            rows = Rows("e2m1", [1], 16, 1, 64, layers=1, seed=i)
+            _append(rows, 0, 0, None, None, 1, 1, 64, m=m, k=x[None].to(torch.bfloat16), v=x[None].to(torch.bfloat16) * 1.5)
+
+
+@pytest.mark.parametrize("page,d,kv", [(16, 64, 3), (64, 128, 2), (256, 64, 1)])
+def test_writing_into_4_bits_without_a_rotation(page, d, kv):
+    lens = [50, 300, 0, 17]
+    rows = Rows("e2m1", lens, page, kv, d, seed=8)
+    cache = rows.on(S, DEV)
+    starts = [0, 50, 50, 53, 69]
+    seqs = [0, 0, 3, 1]                                    # listed twice: the second entry has no rows and changes nothing
+    k, v = _x(1, 70, kv * d), _x(2, 70, kv * d)
+    S.sif_k_kv_write(cache, 1, _wide(k), _wide(v), _i32(seqs), 4, starts=_i32(starts), rows=70)
+    torch.cuda.synchronize()
+    for r, s, pos, again in _rows_of(rows, seqs, starts, 4, 70):
+        if not again and pos >= 0:
+            rows.put("k", 1, s, pos, k[r].double().view(kv, d))
+            rows.put("v", 1, s, pos, v[r].double().view(kv, d))
+    rows.check()
+
+
+@pytest.mark.parametrize("dtype", FORMATS)
+@pytest.mark.parametrize("d,kv,page", [(64, 3, 16), (128, 2, 64), (64, 1, 256)])
+def test_reading_back(dtype, d, kv, page):
+    lens = [45, 0, page, 7, 130]
+    rows = Rows(dtype, lens, page, kv, d, seed=9, spare=2)
+    if lens[4] > page:
+        rows.table[4][0] = -1                              # a page that was given up
+    cache = rows.on(S, DEV)
+    for layer, seqs, starts, count in ((0, None, [0, 45, 45, 45 + page, 52 + page, 182 + page], 182 + page), (1, [4, 0, 9, 4, 3], [1, 4, 60, 62, 70, 79], 90), (1, None, None, 5)):
+        k, v = _wide(torch.full((count, kv * d), 5.0), 8, 5.0), _wide(torch.full((count, kv * d), 5.0), 24, 5.0)
+        n = 5
+        S.sif_k_kv_read(cache, layer, k, v, _i32(seqs), n, starts=_i32(starts), rows=count)
+        torch.cuda.synchronize()
+        want = {x: torch.full((count, kv * d), 5.0, dtype=torch.float64) for x in "kv"}
+        for r, s, pos, _ in _rows_of(rows, seqs, starts, n, count):
+            for x in "kv":
+                y = rows.get(x, layer, s, pos)
+                want[x][r] = 0.0 if y is None else y.flatten()
+        for x, got in (("k", k), ("v", v)):
+            y = got[:, :kv * d].cpu().double()
+            if dtype == "e4m3":      # a product in fp32, then one rounding
+                assert torch.all((y - want[x]).abs() <= (HALF + 2.0 ** -23) * want[x].abs() + 2.0 ** -134)
+            else:
+                assert torch.equal(y, want[x]), (x, layer)
+            assert bool((got[:, kv * d:] == 5.0).all())
+        rows.check("untouched")
+
+
+def test_4_bit_pages_are_copied_whole():
+    """Forking, extending, copying and compacting move powers along with what they belong to."""
+    rows = Rows("e2m1", [20, 70, 0, 0], 32, 3, 64, layers=2, seed=10, spare=5, wider=2)
+    cache = rows.on(S, DEV)
+    size = S.sif_kv_workspace_bytes(cache)
+    work = torch.empty(size, dtype=torch.uint8, device=DEV)
+    S.sif_k_kv_fork(cache, _i32([0, 1]), _i32([2, 3]), 2)
+    S.sif_k_kv_extend(cache, _i32([2, 3]), _i32([1, 1]), 2, work, size)
+    S.sif_k_kv_free(cache, _i32([0]), 1)
+    S.sif_k_kv_compact(cache, work, size)
+    for layer in (0, 1):
+        for seq, of, m in ((2, 0, 20), (3, 1, 70), (1, 1, 70)):
+            k, v = torch.empty(m, 192, dtype=torch.bfloat16, device=DEV), torch.empty(m, 192, dtype=torch.bfloat16, device=DEV)
+            extra = 0 if seq == 1 else 1
+            k1, v1 = torch.empty(m + extra, 192, dtype=torch.bfloat16, device=DEV), torch.empty(m + extra, 192, dtype=torch.bfloat16, device=DEV)
+            S.sif_k_kv_read(cache, layer, k1, v1, _i32([seq]), 1, starts=_i32([0, m + extra]), rows=m + extra)
+            k, v = k1[:m].cpu().double(), v1[:m].cpu().double()
+            for t in range(m):
+                assert torch.equal(k[t], rows.get("k", layer, of, t).flatten()) and torch.equal(v[t], rows.get("v", layer, of, t).flatten()), (seq, t)
+
+
+def test_a_pool_past_4_gib_in_4_bits():
+    """Pages whose bytes begin beyond 32 bits, in keys and values."""
+    d, kv, page = 128, 8, 256
+    n_pages = (1 << 32) // (kv * page * d * 17 // 32) + 40
+    k, v = (torch.zeros(1, n_pages, kv, page * d * 17 // 32, dtype=torch.uint8, device=DEV) for _ in range(2))
+    table = torch.tensor([[n_pages - 1, 3]], dtype=torch.int32, device=DEV)
+    lengths, refs = torch.tensor([page + 2], dtype=torch.int32, device=DEV), torch.ones(n_pages, dtype=torch.int32, device=DEV)
+    cache = S.kv_cache(k, v, table, lengths, refs, S.SIF_E2M1, page)
+    x, y = _x(1, page + 2, kv * d), _x(2, page + 2, kv * d)
+    S.sif_k_kv_append(cache, S.rope_plan(16), S.kv_append_args(x.to(DEV), y.to(DEV), 1, rows=page + 2, starts=_i32([0, page + 2])))
+    a, b = torch.empty(page + 2, kv * d, dtype=torch.bfloat16, device=DEV), torch.empty(page + 2, kv * d, dtype=torch.bfloat16, device=DEV)
+    S.sif_k_kv_read(cache, 0, a, b, None, 1, starts=_i32([0, page + 2]), rows=page + 2)
+    from rows_reference import from_e2m1, to_e2m1
+    assert torch.equal(b.cpu().double(), from_e2m1(*to_e2m1(y.double().view(page + 2, kv, d))).flatten(1))
+    val, _ = turned(x.double().view(page + 2, kv, d), torch.arange(page + 2), frequencies(16), False)
+    assert torch.equal(a.cpu().double(), from_e2m1(*to_e2m1(val)).flatten(1))
+    assert not k[0, :3].any() and not v[0, 4:n_pages - 1].any()
