@@ -521,13 +521,13 @@ sif_status sif_k_embed_bwd(const int32_t* ids_dev, const void* dx_dev, void* dwt
 sif_status sif_k_xent_fwd_bwd(void* logits_dev, const int32_t* targets_dev, float* loss_dev, uint32_t tokens,
                               uint32_t vocab, uint32_t ld, void* stream);
 /* --- A token for every row of logits -------------------------------------------------------------------------------
- * Of a row's tokens (a logit of -inf or NaN is none) these are left, in this order:
+ * Of a row's tokens (a logit of -inf or NaN is none; beside one of +inf only those of +inf are, all alike) these are left, in this order:
  *   top_k > 0      the top_k with the largest logits, of equal ones those with the lowest numbers
  *   top_p < 1      of these the fewest, most probable first (equal ones as before), whose probabilities exp(l / temperature) make up at least top_p of
  *                  the sum of what top_k left; at least one
  *   min_p > 0      those at least min_p (held to 1) times as probable as the most probable one
  * and the token is the first, in the order of their numbers, at which the sum of the probabilities exceeds random (held to 0 .. 1 - 2^-24, NaN counts as 0) times that of all that are
- * left.  A temperature that is not above 0: the largest logit's token, of equal ones the lowest number.  Logits of +inf leave no probability to others.
+ * left.  A temperature that is not above 0: the largest logit's token, of equal ones the lowest number.
  * Probabilities are taken in 64 bits and added as integers of at least 2^-44 of the largest one, so the answer does not depend on the order of additions.  A row without a token gets -1.
  * kept: how many tokens were left (1 where the temperature is not above 0); logprob: the log of the token's share of their sum (-inf for no token). */
 typedef struct sif_sample_args {

@@ -1,8 +1,14 @@
 // One token for every row of logits: temperature, top-k, top-p, min-p, and the token that a given random number falls on.
 //
 // All limits leave the first so many of the row's tokens in the order of falling logits (equal ones by their numbers), so what is left is told by the least
-// logit and how many of those that equal it.  Both are found without sorting: logits become integers of the same order, and their bits are looked at from the
-// highest on, eleven at a time, by counts (top-k) or sums of probabilities (top-p) of all that agree in the bits so far.  Then the row is walked in the order of its numbers.
+// logit and how many of those that equal it.  A block of sixteen wavefronts takes a row:
+//   the largest logit (a temperature of 0 ends here);
+//   a bound that what is left must reach: for a top-k of up to 512 that of the k-th largest of the threads' own largest logits, else of a histogram of counts or, for top-p, of
+//     probabilities over equal steps of the logit;
+//   the tokens that reach it, listed in the order of their numbers.  Where they fit (1024), all else happens on that list: a token's rank is how many stand before it, sums
+//     over ranks decide about top-p, sums over the list about the token.  Where only those of the bound's own step fit, the list gives the least logit that is left, and
+//     the row is walked once more.  Where neither fits (many equal logits, logits of one step) the least logit is found from the bits of the logits, eleven at a time.
+// A row is read from memory once, later walks find it in the L2.
 //
 // Probabilities w = exp((l - l_max) / T) are compared with shares of their sum, and near a border the last bits decide which token comes out; 50000 of them in fp32 would put
 // one row in a hundred on the wrong token.  So they are taken in 64 bits and added as integers w 2^s, s as large as vocab of them fit into 62 bits (sums
@@ -15,7 +21,7 @@
 
 namespace sif {
 
-constexpr uint32_t SM_THREADS = 1024, SM_WAVES = SM_THREADS / 64, SM_BINS = 2048;
+constexpr uint32_t SM_THREADS = 1024, SM_WAVES = SM_THREADS / 64, SM_BINS = 2048, SM_LIST = 1024, SM_FEW = 512;      // SM_FEW: a top-k that the threads' largest bound
 constexpr uint32_t kKeyNone = 0x007FFFFFu;      // of -inf
 
 struct SampleArgs {
@@ -41,10 +47,15 @@ __device__ __forceinline__ uint32_t sm_key(float x) {
 }
 __device__ __forceinline__ float sm_value(uint32_t key) { return __uint_as_float(key & 0x80000000u ? key ^ 0x80000000u : ~key); }
 
-// exp(x), x <= 0 (NaN counts as far below): 2^n times 2^f with |f| <= 1/2, whose Taylor series to the 13th power is right to 2^-54.
-__device__ __forceinline__ double sm_exp(double x) {
-  const double t = fmax(x * 1.44269504088896340736, -1100.0), n = rint(t), r = (t - n) * 0.693147180559945309417;
-  double p = 1.0 / 6227020800.0;
+// 2^x for |x| <= 1: the Taylor series of exp(x ln 2) to the 18th power, right to 2^-52.
+__device__ __forceinline__ double sm_exp2(double x) {
+  const double r = x * 0.693147180559945309417;
+  double p = 1.0 / 6402373705728000.0;
+  p = fma(p, r, 1.0 / 355687428096000.0);
+  p = fma(p, r, 1.0 / 20922789888000.0);
+  p = fma(p, r, 1.0 / 1307674368000.0);
+  p = fma(p, r, 1.0 / 87178291200.0);
+  p = fma(p, r, 1.0 / 6227020800.0);
   p = fma(p, r, 1.0 / 479001600.0);
   p = fma(p, r, 1.0 / 39916800.0);
   p = fma(p, r, 1.0 / 3628800.0);
@@ -57,42 +68,79 @@ __device__ __forceinline__ double sm_exp(double x) {
   p = fma(p, r, 1.0 / 6.0);
   p = fma(p, r, 0.5);
   p = fma(p, r, 1.0);
-  p = fma(p, r, 1.0);
-  return ldexp(p, (int)n);
+  return fma(p, r, 1.0);
 }
 
-struct SampleScale {
-  float top;
-  double inv_t, unit;
-  __device__ __forceinline__ double x(float l) const { return l == top ? 0.0 : ((double)l - (double)top) * inv_t; }
-  __device__ __forceinline__ double w(float l) const { return sm_exp(x(l)); }
-  __device__ __forceinline__ uint64_t whole(double w) const {      // w 2^s, to the nearest (below 2^52: added to 2^52 it is the sum's mantissa)
-    return (uint64_t)__double_as_longlong(fma(w, unit, 4503599627370496.0)) & 0xFFFFFFFFFFFFFull;
+// A logit as a number of steps below the largest one, NaN and what is further as the last: t, the nearest whole number n and the rest r.  (2^52 + 2^51 in front of the point
+// leaves no bits behind it.)  Differences, products, cuts and roundings keep the order, so steps of steps do.
+struct SampleStep { int n; double r; };
+struct SampleSteps {
+  double top, per;
+  __device__ __forceinline__ SampleStep of(float l) const {
+    const double t = fmax(((double)l - top) * per, -65504.0), m = t + 6755399441055744.0;
+    return {(int)(uint32_t)__double_as_longlong(m), t - (m - 6755399441055744.0)};
   }
+  __device__ __forceinline__ static uint32_t bin(int n) { return (uint32_t)(SM_BINS - 1 + (n >> 5)); }      // 0 .. 2047
 };
 
-// A row's logits, sixteen bytes at a time: the wavefronts take one piece each, in order, the lanes of a wavefront neighbouring vectors.
+// A token's probability over the largest one's, times 2^s: 2^(t / 1024) from a table of 2^(i / 1024) and three terms of a series (the next one is 2^-50 at most).  2^-63.97 is as
+// good as nothing, and below a half as an integer.
+struct SampleScale {
+  SampleSteps steps;
+  const double* table;                // in LDS: 2^(s + i / 1024)
+  __device__ __forceinline__ double scaled(const SampleStep& x) const {
+    constexpr double k = 0.693147180559945309417 / 1024.0;
+    const double p = fma(fma(fma(k * k * k / 6.0, x.r, k * k / 2.0), x.r, k), x.r, 1.0);
+    return ldexp(table[x.n & 1023] * p, x.n >> 10);
+  }
+  __device__ __forceinline__ static uint64_t whole(double y) {      // to the nearest (below 2^52: added to 2^52 it is the sum's mantissa)
+    return (uint64_t)__double_as_longlong(y + 4503599627370496.0) & 0xFFFFFFFFFFFFFull;
+  }
+  __device__ __forceinline__ uint64_t mass(float l) const { return whole(scaled(steps.of(l))); }
+};
+
+// A row's logits, sixteen bytes at a time, neighbouring lanes neighbouring vectors.  What stands behind the row reads as -inf.
 template <typename E>
 struct SampleRow {
-  static constexpr uint32_t N = 16 / sizeof(E);
+  static constexpr uint32_t N = 16 / sizeof(E), STEP = 64 * N;
   const E* row;
-  uint32_t vocab, per_wave;           // elements of a wavefront, a multiple of 64 * N
-  // f(index of the first, N values): values past the end are -inf
-  template <typename F> __device__ __forceinline__ void each(uint32_t wave, F&& f) const {
-    const uint32_t lane = threadIdx.x & 63, end = std::min((wave + 1) * per_wave, vocab);
-    for (uint32_t at = wave * per_wave; at < end; at += 64 * N) f(at + lane * N, load(at + lane * N));
-  }
+  uint32_t vocab;
+  bool infinite;                      // there are logits of +inf: they read as 0 and the others as -inf
   struct Vec { float x[N]; };
-  __device__ __forceinline__ Vec load(uint32_t i) const {
+  __device__ __forceinline__ static Vec values(const uint4& u) {
     Vec v;
-    uint4 u = make_uint4(0, 0, 0, 0);
-    if (i < vocab) u = *reinterpret_cast<const uint4*>(row + i);       // (rows are padded to whole vectors)
     if constexpr (N == 4) { v.x[0] = __uint_as_float(u.x); v.x[1] = __uint_as_float(u.y); v.x[2] = __uint_as_float(u.z); v.x[3] = __uint_as_float(u.w); }
     else { v.x[0] = bflo(u.x); v.x[1] = bfhi(u.x); v.x[2] = bflo(u.y); v.x[3] = bfhi(u.y); v.x[4] = bflo(u.z); v.x[5] = bfhi(u.z); v.x[6] = bflo(u.w); v.x[7] = bfhi(u.w); }
-#pragma unroll
-    for (uint32_t e = 0; e < N; ++e)
-      if (i + e >= vocab) v.x[e] = -INFINITY;
     return v;
+  }
+  __device__ __forceinline__ uint4 raw(uint32_t i, uint32_t end) const {      // (rows are padded to whole vectors)
+    constexpr uint32_t none = N == 4 ? 0xFF800000u : 0xFF80FF80u;
+    return i < end ? *reinterpret_cast<const uint4*>(row + i) : make_uint4(none, none, none, none);
+  }
+  // A wavefront's part of the row, from `first` on (a multiple of N) to `end`: f(index of the lane's first value, values).  Four vectors of a lane are on the way ahead
+  // of the one in use.
+  template <typename F> __device__ __forceinline__ void each(uint32_t first, uint32_t end, F&& f) const {
+    const uint32_t lane = threadIdx.x & 63;
+    if (first >= end) return;
+    uint32_t i = first + lane * N;
+    uint4 a = raw(i, end), b = raw(i + STEP, end), c = raw(i + 2 * STEP, end), d = raw(i + 3 * STEP, end);
+#pragma unroll 1
+    for (uint32_t at = first; at < end; at += STEP, i += STEP) {
+      Vec v = values(a);
+      a = b;
+      b = c;
+      c = d;
+      d = raw(i + 4 * STEP, end);
+      if (at + STEP > vocab) {        // the row's end: the last vector may go beyond it
+#pragma unroll
+        for (uint32_t e = 0; e < N; ++e) v.x[e] = i + e < vocab ? v.x[e] : -INFINITY;
+      }
+      if (infinite) {
+#pragma unroll
+        for (uint32_t e = 0; e < N; ++e) v.x[e] = v.x[e] == INFINITY ? 0.f : -INFINITY;
+      }
+      f(i, v);
+    }
   }
 };
 
@@ -110,31 +158,53 @@ __device__ __forceinline__ uint64_t sm_scan64(uint64_t v) {            // inclus
 }
 
 struct SampleShared {
-  uint64_t bins[SM_BINS];
+  uint64_t bins[SM_BINS];             // counts or sums of probabilities
+  double table[1024];
+  uint64_t order[SM_LIST];            // a listed token's key, turned over, and its place in the list: in this order they are sorted
+  uint64_t weight[SM_LIST];           // by place
+  uint32_t token[SM_LIST], place[SM_LIST], rank[SM_LIST];      // by place, by rank, by place
   uint64_t wave[SM_WAVES];
   uint64_t above;                     // what lies above the bin that was found
-  uint32_t bin, ties[SM_WAVES], kept[SM_WAVES];
-  float red[SM_WAVES];
-  uint64_t picked[2];
+  uint32_t bin, some[SM_WAVES], more[SM_WAVES];
+  float best[SM_WAVES];
 };
 
-// The bin, from the highest on, at which the running sum of the bins reaches `target` (asked(sum): whether it does); sh.above gets the sum of those above it.
-// Returns the sum of all bins.
+// Sums over the block.  Every thread gets the whole; barriers on both sides.
+__device__ __forceinline__ uint32_t sm_count(SampleShared& sh, uint32_t x) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o, 64);
+  if ((threadIdx.x & 63) == 0) sh.some[threadIdx.x >> 6] = x;
+  __syncthreads();
+  uint32_t all = 0;
+  for (uint32_t w = 0; w < SM_WAVES; ++w) all += sh.some[w];
+  __syncthreads();
+  return all;
+}
+// Inclusive sum over the block's threads; *all: over all of them.
+__device__ __forceinline__ uint64_t sm_block_scan(SampleShared& sh, uint64_t x, uint64_t* all) {
+  const uint32_t wave = threadIdx.x >> 6;
+  uint64_t upto = sm_scan64(x), before = 0, total = 0;
+  if ((threadIdx.x & 63) == 63) sh.wave[wave] = upto;
+  __syncthreads();
+  for (uint32_t w = 0; w < SM_WAVES; ++w) {
+    const uint64_t y = sh.wave[w];
+    before += w < wave ? y : 0;
+    total += y;
+  }
+  __syncthreads();
+  *all = total;
+  return upto + before;
+}
+
+// The bin, from the highest on, at which the running sum of the bins, `above` in front, is asked for (asked_of(sum of all bins)(running sum)); sh.above gets that
+// of the bins above it.  Returns the sum of all bins.
 template <typename A>
 __device__ __forceinline__ uint64_t sm_find(SampleShared& sh, uint64_t above, A&& asked_of) {
-  const uint32_t t = threadIdx.x, lane = t & 63, wave = t >> 6;
+  const uint32_t t = threadIdx.x;
   const uint64_t hi = sh.bins[SM_BINS - 1 - 2 * t], lo = sh.bins[SM_BINS - 2 - 2 * t];
-  uint64_t upto = sm_scan64(hi + lo);
-  if (lane == 63) sh.wave[wave] = upto;
+  uint64_t all;
   if (t == 0) sh.bin = 0;
-  __syncthreads();
-  uint64_t before = 0, all = 0;
-  for (uint32_t w = 0; w < SM_WAVES; ++w) {
-    before += w < wave ? sh.wave[w] : 0;
-    all += sh.wave[w];
-  }
-  upto += before;
-  const uint64_t start = upto - hi - lo;
+  const uint64_t upto = sm_block_scan(sh, hi + lo, &all), start = upto - hi - lo;
   auto asked = asked_of(all);
   const bool s0 = asked(above + start), s1 = asked(above + start + hi), s2 = asked(above + upto);
   if (!s0 && s2) {                               // one thread, or none where all bins together do not reach it
@@ -144,238 +214,455 @@ __device__ __forceinline__ uint64_t sm_find(SampleShared& sh, uint64_t above, A&
   __syncthreads();
   return all;
 }
+__device__ __forceinline__ void sm_clear(SampleShared& sh) {
+  for (uint32_t b = threadIdx.x; b < SM_BINS; b += SM_THREADS) sh.bins[b] = 0;
+  __syncthreads();
+}
+__device__ __forceinline__ void sm_add(SampleShared& sh, uint32_t bin, uint64_t x) { atomicAdd((unsigned long long*)&sh.bins[bin], (unsigned long long)x); }
 
 template <typename E>
-__global__ __launch_bounds__(SM_THREADS) void sample_kernel(SampleArgs a) {
-  __shared__ SampleShared sh;
-  const uint32_t t = threadIdx.x, lane = t & 63, wave = t >> 6, i = blockIdx.x;
+struct Sampler {
+  static constexpr uint32_t N = SampleRow<E>::N, STEP = SampleRow<E>::STEP;
+  typedef typename SampleRow<E>::Vec Vec;
+  const SampleArgs& a;
+  SampleShared& sh;
   SampleRow<E> row;
-  row.row = (const E*)a.logits + (size_t)i * a.ld;
-  row.vocab = a.vocab;
-  constexpr uint32_t N = SampleRow<E>::N, STEP = 64 * N;
-  row.per_wave = ((a.vocab + SM_WAVES - 1) / SM_WAVES + STEP - 1) / STEP * STEP;
-  const float temperature = a.temperature_list != nullptr ? a.temperature_list[i] : a.temperature;
-  const int32_t top_k = a.top_k_list != nullptr ? a.top_k_list[i] : a.top_k;
-  const float top_p = a.top_p_list != nullptr ? a.top_p_list[i] : a.top_p;
-  const float min_p = std::min(a.min_p_list != nullptr ? a.min_p_list[i] : a.min_p, 1.f);
-
-  // the largest logit, and how many there are
-  uint32_t best = 0, some = 0;
-  row.each(wave, [&](uint32_t, const typename SampleRow<E>::Vec& v) {
-#pragma unroll
-    for (uint32_t e = 0; e < N; ++e) {
-      const uint32_t key = sm_key(v.x[e]);
-      best = std::max(best, key);
-      some += key > kKeyNone ? 1u : 0u;
-    }
-  });
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) {
-    best = std::max(best, (uint32_t)__shfl_xor(best, o, 64));
-    some += __shfl_xor(some, o, 64);
-  }
-  if (lane == 0) { sh.ties[wave] = best; sh.kept[wave] = some; }
-  __syncthreads();
-  best = some = 0;
-  for (uint32_t w = 0; w < SM_WAVES; ++w) { best = std::max(best, sh.ties[w]); some += sh.kept[w]; }
-  __syncthreads();
-  if (best <= kKeyNone) {
-    if (t == 0) {
-      a.token[i] = -1;
-      if (a.logprob != nullptr) a.logprob[i] = -INFINITY;
-      if (a.kept != nullptr) a.kept[i] = 0;
-    }
-    return;
-  }
-  const bool greedy = !(temperature > 0.f);
   SampleScale sc;
-  sc.top = sm_value(best);
-  sc.inv_t = greedy ? 1.0 : 1.0 / (double)temperature;
-  sc.unit = ldexp(1.0, (int)a.shift);
+  uint32_t i, wave, lane;
+  float temperature, top_p, min_p, top;
+  int32_t top_k;
 
-  // what is left: keys above `least`, and the first `equal` of those that are equal to it
-  uint32_t least = kKeyNone, equal = 0;
-  if (greedy) {
-    least = best;
-    equal = 1;
-  } else {
-    if (top_k > 0 && (uint32_t)top_k < some) {
-      uint32_t known = 0, mask = 0;
-      uint64_t above = 0;
-#pragma unroll 1
-      for (int level = 0; level < 3; ++level) {
-        const int low = level == 0 ? 21 : level == 1 ? 10 : 0;
-        const uint32_t bits = level == 2 ? 1023u : 2047u;
-        for (uint32_t b = t; b < SM_BINS; b += SM_THREADS) sh.bins[b] = 0;
-        __syncthreads();
-        row.each(wave, [&](uint32_t, const typename SampleRow<E>::Vec& v) {
+  template <typename F> __device__ __forceinline__ void each(F&& f) const {      // the whole row, a piece to each wavefront, in order
+    const uint32_t per = ((row.vocab + SM_WAVES - 1) / SM_WAVES + STEP - 1) / STEP * STEP;
+    row.each(wave * per, std::min((wave + 1) * per, row.vocab), f);
+  }
+  __device__ __forceinline__ void answer(uint32_t token, float l, uint64_t all, uint32_t kept) const {
+    a.token[i] = (int32_t)token;
+    const double largest = sc.table[0];
+    if (a.logprob != nullptr) a.logprob[i] = (float)(((double)l - (double)top) / (double)temperature - log((double)all / largest));
+    if (a.kept != nullptr) a.kept[i] = (int32_t)kept;
+  }
+  __device__ __forceinline__ double goal(uint64_t all) const {
+    const float u = a.random != nullptr ? a.random[i] : 0.f;
+    return (double)(u > 0.f ? std::min(u, 0.99999994f) : 0.f) * (double)all;
+  }
+  __device__ __forceinline__ double share(uint64_t all) const { return fmax((double)top_p * (double)all, 0.5); }      // what top-p asks for; at least one token
+
+  // The least logit (no -inf) whose bin is `bin` or above: a search among the numbers, 64 at a time.
+  __device__ __forceinline__ float least_of(const SampleSteps& steps, uint32_t bin) const {
+    uint32_t lo = kKeyNone, hi = sm_key(top);      // hi's bin is the highest one, lo's (if any) is not asked for
+    while (hi - lo > 1) {
+      const uint64_t step = ((uint64_t)(hi - lo) + 63) / 64, size = hi - lo;
+      const uint32_t at = lo + (uint32_t)std::min(step * (lane + 1), size);
+      const int f = __ffsll((unsigned long long)__ballot(SampleSteps::bin(steps.of(sm_value(at)).n) >= bin)) - 1;
+      hi = lo + (uint32_t)std::min(step * (uint64_t)(f + 1), size);
+      lo += (uint32_t)(step * (uint64_t)f);
+    }
+    return sm_value(hi);
+  }
+
+  // Lists the tokens with logits of `low` and above, or where these are too many those below `high`, in the order of their numbers, and ranks them.  Returns how many
+  // there are, more than SM_LIST if neither fits; *whole: the list holds all from `low` on.
+  __device__ __forceinline__ uint32_t list(float low, float high, bool* whole) {
+    uint32_t ge = 0, gt = 0;                       // (of the wavefront)
+    each([&](uint32_t, const Vec& v) {
 #pragma unroll
-          for (uint32_t e = 0; e < N; ++e) {
-            const uint32_t key = sm_key(v.x[e]);
-            if (key > kKeyNone && (key & mask) == known) atomicAdd((unsigned long long*)&sh.bins[key >> low & bits], 1ull);
-          }
-        });
-        __syncthreads();
-        sm_find(sh, above, [&](uint64_t) { return [&](uint64_t sum) { return sum >= (uint64_t)top_k; }; });
-        above = sh.above;
-        known |= sh.bin << low;
-        mask |= bits << low;
-        __syncthreads();
+      for (uint32_t e = 0; e < N; ++e) {
+        ge += (uint32_t)__popcll(__ballot(v.x[e] >= low));
+        gt += (uint32_t)__popcll(__ballot(v.x[e] >= high));
       }
+    });
+    if (lane == 0) { sh.some[wave] = ge; sh.more[wave] = ge - gt; }
+    __syncthreads();
+    uint32_t all_ge = 0, all_eq = 0, before_ge = 0, before_eq = 0;
+    for (uint32_t w = 0; w < SM_WAVES; ++w) {
+      const uint32_t x = sh.some[w], y = sh.more[w];
+      before_ge += w < wave ? x : 0u;
+      before_eq += w < wave ? y : 0u;
+      all_ge += x;
+      all_eq += y;
+    }
+    __syncthreads();
+    *whole = all_ge <= SM_LIST;
+    const uint32_t m = *whole ? all_ge : all_eq;
+    if (m > SM_LIST) return m;
+    const float end = *whole ? INFINITY : high;
+    uint32_t at = *whole ? before_ge : before_eq;
+    each([&](uint32_t first, const Vec& v) {
+      uint64_t any = 0;
+#pragma unroll
+      for (uint32_t e = 0; e < N; ++e) any |= __ballot(v.x[e] >= low);
+      if (any == 0) return;
+      uint32_t mine = 0;
+#pragma unroll
+      for (uint32_t e = 0; e < N; ++e) mine |= v.x[e] >= low && v.x[e] < end ? 1u << e : 0u;
+      const uint32_t n = __popc(mine);
+      uint32_t upto = n;
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) {
+        const uint32_t x = __shfl_up(upto, o, 64);
+        if (lane >= (uint32_t)o) upto += x;
+      }
+      uint32_t to = at + upto - n;
+#pragma unroll
+      for (uint32_t e = 0; e < N; ++e)
+        if (mine >> e & 1u) {
+          sh.order[to] = (uint64_t)(~sm_key(v.x[e])) << 32 | to;
+          sh.token[to++] = first + e;
+        }
+      at += __shfl(upto, 63, 64);
+    });
+    __syncthreads();
+    if (m <= 256) rank_by_counting(m); else rank_by_sorting(m);
+    return m;
+  }
+  // Every entry counts those in front of it, a share of the list for each of the threads that an entry gets.
+  __device__ __forceinline__ void rank_by_counting(uint32_t m) {
+    if (threadIdx.x < m) sh.rank[threadIdx.x] = 0;
+    __syncthreads();
+    uint32_t per = 1;                              // entries, as a power of two
+    while (per < m) per <<= 1;
+    const uint32_t mine = threadIdx.x & (per - 1), part = threadIdx.x / per, parts = SM_THREADS / per;
+    if (mine < m) {
+      const uint64_t x = sh.order[mine];
+      const uint32_t size = (m + parts - 1) / parts, end = std::min(m, (part + 1) * size);
+      uint32_t before = 0;
+      for (uint32_t j = part * size; j < end; ++j) before += sh.order[j] < x ? 1u : 0u;
+      if (before != 0) atomicAdd(&sh.rank[mine], before);
+    }
+    __syncthreads();
+    if (threadIdx.x < m) sh.place[sh.rank[threadIdx.x]] = threadIdx.x;
+    __syncthreads();
+  }
+  // A bitonic sort, an entry to a thread: partners in the wavefront exchange by shuffles, others through LDS.
+  __device__ __forceinline__ void rank_by_sorting(uint32_t m) {
+    const uint32_t t = threadIdx.x;
+    uint64_t x = t < m ? sh.order[t] : ~0ull;
+#pragma unroll 1
+    for (uint32_t size = 2; size <= SM_LIST; size <<= 1)
+#pragma unroll 1
+      for (uint32_t by = size >> 1; by > 0; by >>= 1) {
+        uint64_t y;
+        if (by < 64) {
+          y = (uint64_t)(uint32_t)__shfl_xor((uint32_t)(x >> 32), by, 64) << 32 | (uint32_t)__shfl_xor((uint32_t)x, by, 64);
+        } else {
+          sh.weight[t] = x;
+          __syncthreads();
+          y = sh.weight[t ^ by];
+          __syncthreads();
+        }
+        const bool small = ((t & by) == 0) == ((t & size) == 0);
+        x = (x < y) == small ? x : y;
+      }
+    if (t < m) sh.place[t] = (uint32_t)x;
+    __syncthreads();
+  }
+  __device__ __forceinline__ uint32_t ranked_key(uint32_t rank) const { return ~(uint32_t)(sh.order[sh.place[rank]] >> 32); }
+
+  // The token, where the list holds everything that is left (and what the limits leave out).  whole_sum: of all probabilities, where there is no top-k.
+  __device__ __forceinline__ void draw_from_list(uint32_t m, bool by_k, uint64_t whole_sum) {
+    const uint32_t r = threadIdx.x;
+    const uint32_t place = r < m ? sh.place[r] : 0u;
+    const double y = r < m ? sc.scaled(sc.steps.of(sm_value(ranked_key(r)))) : 0.0;
+    const uint64_t mass = SampleScale::whole(y);
+    bool left = r < (by_k ? std::min(m, (uint32_t)top_k) : m);
+    if (top_p < 1.f) {
+      uint64_t all;
+      const uint64_t upto = sm_block_scan(sh, left ? mass : 0, &all);
+      left = left && (double)(upto - mass) < share(by_k ? all : whole_sum);
+    }
+    left = left && !(y < (double)min_p * sc.table[0]);
+    if (r < m) sh.weight[place] = left ? mass : 0;
+    const uint32_t kept = sm_count(sh, left ? 1u : 0u);      // (its barriers stand behind the weights too)
+    const uint64_t mine = r < m ? sh.weight[r] : 0;
+    uint64_t all;
+    const uint64_t upto = sm_block_scan(sh, mine, &all);
+    const double target = goal(all);
+    if (!((double)(upto - mine) > target) && (double)upto > target) answer(sh.token[r], sm_value(~(uint32_t)(sh.order[r] >> 32)), all, kept);
+  }
+
+  // The least key that is left and how many of those equal to it, from the keys' bits: for top-k, or by MASS for top-p of what `least` and `equal` leave so far.
+  template <bool MASS>
+  __device__ __forceinline__ void by_bits(uint32_t& least, uint32_t& equal) {
+    uint32_t known = 0, mask = 0;
+    uint64_t above = 0;
+    double target = 0.0;
+#pragma unroll 1
+    for (int level = 0; level < 3; ++level) {
+      const int low = level == 0 ? 21 : level == 1 ? 10 : 0;
+      const uint32_t bits = level == 2 ? 1023u : 2047u;
+      sm_clear(sh);
+      each([&](uint32_t, const Vec& v) {
+#pragma unroll
+        for (uint32_t e = 0; e < N; ++e) {
+          const uint32_t key = sm_key(v.x[e]);
+          if (key > least && (key & mask) == known) sm_add(sh, key >> low & bits, MASS ? sc.mass(v.x[e]) : 1ull);
+        }
+      });
+      if (MASS && threadIdx.x == 0 && equal != 0 && (least & mask) == known) sm_add(sh, least >> low & bits, equal * sc.mass(sm_value(least)));
+      __syncthreads();
+      const int at_level = level;
+      sm_find(sh, above, [&](uint64_t all) {
+        if (at_level == 0) target = MASS ? share(all) : (double)top_k;
+        return [&](uint64_t sum) { return (double)sum >= target; };
+      });
+      above = sh.above;
+      known |= sh.bin << low;
+      mask |= bits << low;
+      __syncthreads();
+    }
+    if constexpr (!MASS) {
       least = known;
       equal = (uint32_t)top_k - (uint32_t)above;
-    }
-    if (top_p < 1.f) {
-      uint32_t known = 0, mask = 0;
-      uint64_t above = 0;
-      double target = 0.0;
-#pragma unroll 1
-      for (int level = 0; level < 3; ++level) {
-        const int low = level == 0 ? 21 : level == 1 ? 10 : 0;
-        const uint32_t bits = level == 2 ? 1023u : 2047u;
-        for (uint32_t b = t; b < SM_BINS; b += SM_THREADS) sh.bins[b] = 0;
-        __syncthreads();
-        row.each(wave, [&](uint32_t, const typename SampleRow<E>::Vec& v) {
-#pragma unroll
-          for (uint32_t e = 0; e < N; ++e) {
-            const uint32_t key = sm_key(v.x[e]);
-            if (key > least && (key & mask) == known) atomicAdd((unsigned long long*)&sh.bins[key >> low & bits], (unsigned long long)sc.whole(sc.w(sm_value(key))));
-          }
-        });
-        if (t == 0 && equal != 0 && (least & mask) == known) atomicAdd((unsigned long long*)&sh.bins[least >> low & bits], (unsigned long long)(equal * sc.whole(sc.w(sm_value(least)))));
-        __syncthreads();
-        const int at_level = level;
-        sm_find(sh, above, [&](uint64_t all) {
-          if (at_level == 0) target = fmax((double)top_p * (double)all, 0.5);      // (at least one token)
-          return [&](uint64_t sum) { return (double)sum >= target; };
-        });
-        above = sh.above;
-        known |= sh.bin << low;
-        mask |= bits << low;
-        __syncthreads();
-      }
+    } else {
       // of those equal to `known` as many as it takes
-      const uint64_t w = sc.whole(sc.w(sm_value(known)));
+      const uint64_t w = sc.mass(sm_value(known));
       uint64_t need = 1;
       if (w != 0) {
         need = (uint64_t)fmax((target - (double)above) / (double)w, 1.0);
         while (need > 1 && (double)(above + (need - 1) * w) >= target) --need;
         while ((double)(above + need * w) < target) ++need;
       }
-      if (known == least) {
-        equal = (uint32_t)std::min<uint64_t>(equal, need);
-      } else {
-        least = known;
-        equal = (uint32_t)std::min<uint64_t>(need, a.vocab);
-      }
+      equal = (uint32_t)std::min<uint64_t>(need, known == least ? equal : row.vocab);
+      least = known;
     }
   }
 
-  // The row in the order of its numbers.  First each wavefront's ties, then its sum.
-  uint32_t ties = 0;
-  if (equal != 0)
-    row.each(wave, [&](uint32_t, const typename SampleRow<E>::Vec& v) {
+  // The token, by walking the row: logits above that of `least` are left, and the first `equal` of those that are equal to it.  The sums of sixteen pieces say on which one the
+  // random number falls, this one's sixteen pieces go on, down to a vector for a lane.
+  __device__ __forceinline__ void draw_from_row(uint32_t least, uint32_t equal) {
+    const float bound = sm_value(least);
+    const double least_mass = (double)min_p * sc.table[0];
+    // what is clearly below min-p needs no exponential
+    const double cut = min_p > 0.f ? (double)top + (double)temperature * (log((double)min_p) - 1e-6) : -INFINITY;
+    const float near_cut = (float)(cut - fabs(cut) * 1e-6);
+    uint32_t lo = 0, hi = row.vocab, ties_before = 0, kept = 0;
+    uint64_t before = 0, all = 0;
+    double target = 0.0;
+    for (bool whole = true;; whole = false) {
+      const uint32_t per = ((hi - lo + SM_WAVES - 1) / SM_WAVES + STEP - 1) / STEP * STEP, first = lo + wave * per, end = std::min(first + per, hi);
+      uint32_t seen = ties_before;
+      if (equal != 0) {
+        uint32_t ties = 0;
+        row.each(first, end, [&](uint32_t, const Vec& v) {
 #pragma unroll
-      for (uint32_t e = 0; e < N; ++e) ties += sm_key(v.x[e]) == least ? 1u : 0u;
-    });
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) ties += __shfl_xor(ties, o, 64);
-  if (lane == 0) sh.ties[wave] = ties;
-  __syncthreads();
-  uint32_t ties_before = 0;
-  for (uint32_t w = 0; w < wave; ++w) ties_before += sh.ties[w];
-  // which of a vector's tokens are left, and what they weigh; `seen`: ties up to here in this wavefront
-  auto weigh = [&](const typename SampleRow<E>::Vec& v, uint32_t& seen, uint64_t (&w)[N]) {
-    uint32_t left = 0, mine = 0, key[N];
-#pragma unroll
-    for (uint32_t e = 0; e < N; ++e) {
-      key[e] = sm_key(v.x[e]);
-      mine += equal != 0 && key[e] == least ? 1u : 0u;
-    }
-    uint32_t upto = mine;
-    if (__any(mine != 0)) {
-#pragma unroll
-      for (int o = 1; o < 64; o <<= 1) {
-        const uint32_t x = __shfl_up(upto, o, 64);
-        if (lane >= (uint32_t)o) upto += x;
+          for (uint32_t e = 0; e < N; ++e) ties += (uint32_t)__popcll(__ballot(v.x[e] == bound));
+        });
+        if (lane == 0) sh.some[wave] = ties;
+        __syncthreads();
+        for (uint32_t w = 0; w < wave; ++w) seen += sh.some[w];
+        __syncthreads();
       }
-    }
-    uint32_t rank = seen + upto - mine;
+      const uint32_t seen_first = seen;
+      uint64_t sum = 0;
+      uint32_t left = 0, last_keep = 0;
+      Vec last = {};
+      row.each(first, end, [&](uint32_t, const Vec& v) {
+        last = v;
+        uint32_t keep = 0;
 #pragma unroll
-    for (uint32_t e = 0; e < N; ++e) {
-      bool keep = key[e] > least;
-      if (equal != 0 && key[e] == least) keep = rank++ < equal;
-      w[e] = 0;
-      if (keep) {
-        const double x = sc.w(sm_value(key[e]));
-        if (!(x < (double)min_p)) {
-          w[e] = sc.whole(x);
-          ++left;
+        for (uint32_t e = 0; e < N; ++e) keep |= v.x[e] > bound && v.x[e] >= near_cut ? 1u << e : 0u;
+        if (equal != 0) {
+          uint32_t mine = 0;
+#pragma unroll
+          for (uint32_t e = 0; e < N; ++e) mine += v.x[e] == bound ? 1u : 0u;
+          if (__any(mine != 0)) {
+            uint32_t upto = mine;
+#pragma unroll
+            for (int o = 1; o < 64; o <<= 1) {
+              const uint32_t x = __shfl_up(upto, o, 64);
+              if (lane >= (uint32_t)o) upto += x;
+            }
+            uint32_t rank = seen + upto - mine;
+#pragma unroll
+            for (uint32_t e = 0; e < N; ++e)
+              if (v.x[e] == bound && rank++ < equal) keep |= 1u << e;
+            seen += __shfl(upto, 63, 64);
+          }
         }
+#pragma unroll
+        for (uint32_t e = 0; e < N; ++e)
+          if (__any(keep >> e & 1u)) {
+            const double y = sc.scaled(sc.steps.of(v.x[e]));
+            if (y < least_mass) keep &= ~(1u << e);
+            sum += keep >> e & 1u ? SampleScale::whole(y) : 0;
+          }
+        left += __popc(keep);
+        last_keep = keep;
+      });
+      const uint64_t upto = sm_scan64(sum);
+      if (lane == 63) sh.wave[wave] = upto;
+      const uint32_t here = sm_count(sh, left);
+      uint64_t pieces = before, mine_before = before, won_before = before;
+      uint32_t won = SM_WAVES - 1;
+      if (whole) {
+        kept = here;
+        for (uint32_t x = 0; x < SM_WAVES; ++x) all += sh.wave[x];
+        target = goal(all);
       }
+      for (uint32_t x = SM_WAVES; x-- > 0;) pieces += sh.wave[x];
+      for (uint32_t x = SM_WAVES; x-- > 0;) {       // the first piece at whose end the sum exceeds it
+        const uint64_t start = pieces - sh.wave[x];
+        if ((double)pieces > target) { won = x; won_before = start; }
+        if (x == wave) mine_before = start;
+        pieces = start;
+      }
+      if (per == STEP) {
+        if (wave != won) return;
+        const uint64_t hits = __ballot((double)(mine_before + upto) > target);
+        if (lane != (uint32_t)__ffsll((unsigned long long)hits) - 1) return;
+        uint64_t x = mine_before + upto;
+        uint32_t e = N - 1;
+        float l = last.x[N - 1];
+#pragma unroll
+        for (uint32_t z = N; z-- > 0;) {            // the first at which the sum exceeds it, looked at from the last on
+          if ((double)x > target) { e = z; l = last.x[z]; }
+          x -= last_keep >> z & 1u ? sc.mass(last.x[z]) : 0;
+        }
+        return answer(first + lane * N + e, l, all, kept);
+      }
+      if (equal != 0) {
+        __syncthreads();
+        if (wave == won && lane == 0) sh.some[0] = seen_first;
+        __syncthreads();
+        ties_before = sh.some[0];
+      }
+      __syncthreads();                             // nobody reads this turn's sums any more
+      before = won_before;
+      lo += won * per;
+      hi = std::min(lo + per, hi);
     }
-    seen += __shfl(upto, 63, 64);
-    return left;
-  };
-  uint64_t sum = 0;
-  uint32_t left = 0, seen = ties_before;
-  row.each(wave, [&](uint32_t, const typename SampleRow<E>::Vec& v) {
-    uint64_t w[N];
-    left += weigh(v, seen, w);
-#pragma unroll
-    for (uint32_t e = 0; e < N; ++e) sum += w[e];
-  });
-  sum = sm_scan64(sum);
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) left += __shfl_xor(left, o, 64);
-  if (lane == 63) sh.wave[wave] = sum;
-  if (lane == 0) sh.kept[wave] = left;
-  __syncthreads();
-  uint64_t before = 0, all = 0;
-  uint32_t kept = 0;
-  for (uint32_t w = 0; w < SM_WAVES; ++w) {
-    before += w < wave ? sh.wave[w] : 0;
-    all += sh.wave[w];
-    kept += sh.kept[w];
   }
-  float u = a.random != nullptr ? a.random[i] : 0.f;
-  u = u > 0.f ? std::min(u, 0.99999994f) : 0.f;
-  const double target = (double)u * (double)all;
-  // the wavefront on whose piece it falls looks again
-  if ((double)before > target || !((double)(before + sh.wave[wave]) > target)) return;
-  seen = ties_before;
-  uint64_t at = before;
-  bool found = false;
-  row.each(wave, [&](uint32_t first, const typename SampleRow<E>::Vec& v) {
-    if (found) return;
-    uint64_t w[N], mine = 0;
-    weigh(v, seen, w);
+
+  __device__ __forceinline__ void run() {
+    sh.table[threadIdx.x] = ldexp(sm_exp2((double)threadIdx.x * (1.0 / 1024.0)), (int)a.shift);
+    // the largest logit, and where the first vector with it lies; and this thread's largest
+    float mine = -INFINITY;
+    uint32_t at = 0xFFFFFFFFu;
+    each([&](uint32_t first, const Vec& v) {
+      float x = v.x[0];
 #pragma unroll
-    for (uint32_t e = 0; e < N; ++e) mine += w[e];
-    const uint64_t upto = at + sm_scan64(mine);
-    const uint64_t hits = __ballot((double)upto > target);
-    if (hits != 0) {
-      found = true;
-      if (lane == (uint32_t)__ffsll((unsigned long long)hits) - 1) {
-        uint64_t x = upto - mine;
-        uint32_t e = 0;
-        for (; e + 1 < N; ++e) {
-          x += w[e];
-          if ((double)x > target) break;
-        }
-        a.token[i] = (int32_t)(first + e);
-        if (a.logprob != nullptr) {
-          float l = v.x[0];
+      for (uint32_t e = 1; e < N; ++e) x = fmaxf(x, v.x[e]);
+      if (x > mine) { mine = x; at = first; }
+    });
+    top = wave_max(mine);
+    if (lane == 0) sh.best[wave] = top;
+    __syncthreads();
+    for (uint32_t w = 0; w < SM_WAVES; ++w) top = fmaxf(top, sh.best[w]);
+    if (top == -INFINITY || !(temperature > 0.f)) {
+      at = mine == top && top > -INFINITY ? at : 0xFFFFFFFFu;
 #pragma unroll
-          for (uint32_t z = 1; z < N; ++z) l = e == z ? v.x[z] : l;
-          a.logprob[i] = greedy ? 0.f : (float)(sc.x(l) - log((double)all / sc.unit));
-        }
-        if (a.kept != nullptr) a.kept[i] = (int32_t)kept;
+      for (int o = 32; o > 0; o >>= 1) at = std::min(at, (uint32_t)__shfl_xor(at, o, 64));
+      if (lane == 0) sh.some[wave] = at;
+      __syncthreads();
+      if (threadIdx.x != 0) return;
+      for (uint32_t w = 0; w < SM_WAVES; ++w) at = std::min(at, sh.some[w]);
+      const bool none = at == 0xFFFFFFFFu;
+      if (!none) {
+        const Vec v = row.values(row.raw(at, row.vocab));
+        uint32_t e = N - 1;
+#pragma unroll
+        for (uint32_t z = N - 1; z-- > 0;) e = v.x[z] == top ? z : e;
+        at += e;
       }
+      a.token[i] = none ? -1 : (int32_t)at;
+      if (a.logprob != nullptr) a.logprob[i] = none ? -INFINITY : 0.f;
+      if (a.kept != nullptr) a.kept[i] = none ? 0 : 1;
       return;
     }
-    at = (uint64_t)(uint32_t)__shfl((uint32_t)(upto >> 32), 63, 64) << 32 | (uint32_t)__shfl((uint32_t)upto, 63, 64);
-  });
+    if (top == INFINITY) {
+      row.infinite = true;
+      mine = mine == INFINITY ? 0.f : -INFINITY;
+      top = 0.f;
+    }
+    sc.table = sh.table;
+    sc.steps = {(double)top, 1.44269504088896340736 * 1024.0 / (double)temperature};
+    // For counts, logits are divided into steps near the largest one, whatever the temperature.
+    const SampleSteps near = {(double)top, 65504.0 / (double)fmaxf(40.f * temperature, 64.f)};
+    uint32_t least = kKeyNone, equal = 0;
+    bool by_k = top_k > 0 && (uint32_t)top_k < row.vocab;
+    if (by_k) {
+      uint32_t m = SM_LIST + 1;
+      bool whole = false;
+      if ((uint32_t)top_k <= SM_FEW) {
+        // at least top_k tokens reach the top_k-th of the threads' own largest (or there are fewer threads with tokens: the lowest bin, all tokens)
+        sm_clear(sh);
+        if (mine > -INFINITY) sm_add(sh, SampleSteps::bin(near.of(mine).n), 1);
+        __syncthreads();
+        sm_find(sh, 0, [&](uint64_t) { return [&](uint64_t sum) { return sum >= (uint64_t)top_k; }; });
+        m = list(least_of(near, sh.bin), INFINITY, &whole);
+        if (m <= SM_LIST && whole) return draw_from_list(m, true, 0);
+      }
+      __syncthreads();
+      sm_clear(sh);
+      each([&](uint32_t, const Vec& v) {
+#pragma unroll
+        for (uint32_t e = 0; e < N; ++e)
+          if (v.x[e] > -INFINITY) sm_add(sh, SampleSteps::bin(near.of(v.x[e]).n), 1);
+      });
+      __syncthreads();
+      const uint64_t some = sm_find(sh, 0, [&](uint64_t) { return [&](uint64_t sum) { return sum >= (uint64_t)top_k; }; });
+      by_k = some > (uint64_t)(uint32_t)top_k;
+      if (by_k) {
+        const uint32_t bin = sh.bin;
+        const uint64_t above = sh.above;
+        m = list(least_of(near, bin), bin + 1 < SM_BINS ? least_of(near, bin + 1) : INFINITY, &whole);
+        if (m <= SM_LIST && whole) return draw_from_list(m, true, 0);
+        if (m <= SM_LIST) {
+          const uint32_t need = (uint32_t)top_k - (uint32_t)above;           // of the listed ones, in their order
+          least = ranked_key(need - 1);
+          equal = sm_count(sh, threadIdx.x < need && ranked_key(threadIdx.x) == least ? 1u : 0u);
+        } else {
+          by_bits<false>(least, equal);
+        }
+        if (top_p < 1.f) by_bits<true>(least, equal);
+      }
+    }
+    if (!by_k && top_p < 1.f) {
+      sm_clear(sh);
+      each([&](uint32_t, const Vec& v) {
+#pragma unroll
+        for (uint32_t e = 0; e < N; ++e) {
+          const SampleStep x = sc.steps.of(v.x[e]);
+          sm_add(sh, SampleSteps::bin(x.n), SampleScale::whole(sc.scaled(x)));      // (of no token: nothing)
+        }
+      });
+      __syncthreads();
+      double target = 0.0;
+      const uint64_t all = sm_find(sh, 0, [&](uint64_t sum) {
+        target = share(sum);
+        return [&](uint64_t x) { return (double)x >= target; };
+      });
+      const uint32_t bin = sh.bin;
+      const uint64_t above = sh.above;
+      bool whole;
+      const uint32_t m = list(least_of(sc.steps, bin), bin + 1 < SM_BINS ? least_of(sc.steps, bin + 1) : INFINITY, &whole);
+      if (m <= SM_LIST && whole) return draw_from_list(m, false, all);
+      if (m <= SM_LIST) {
+        const uint32_t r = threadIdx.x, key = r < m ? ranked_key(r) : kKeyNone;
+        const uint64_t mass = r < m ? sc.mass(sm_value(key)) : 0;
+        uint64_t sum;
+        const uint64_t upto = above + sm_block_scan(sh, mass, &sum);
+        const bool left = r < m && (double)(upto - mass) < target;
+        const uint32_t need = sm_count(sh, left ? 1u : 0u);
+        least = ranked_key(need - 1);
+        equal = sm_count(sh, left && key == least ? 1u : 0u);
+      } else {
+        by_bits<true>(least, equal);
+      }
+    }
+    draw_from_row(least, equal);
+  }
+};
+
+template <typename E>
+__global__ __launch_bounds__(SM_THREADS) void sample_kernel(SampleArgs a) {
+  __shared__ SampleShared sh;
+  const uint32_t i = blockIdx.x;
+  Sampler<E> s = {a, sh, {(const E*)a.logits + (size_t)i * a.ld, a.vocab, false}, {}, i, threadIdx.x >> 6, threadIdx.x & 63,
+                  a.temperature_list != nullptr ? a.temperature_list[i] : a.temperature, a.top_p_list != nullptr ? a.top_p_list[i] : a.top_p,
+                  std::min(a.min_p_list != nullptr ? a.min_p_list[i] : a.min_p, 1.f), 0.f, a.top_k_list != nullptr ? a.top_k_list[i] : a.top_k};
+  s.run();
 }
 
 }  // namespace sif

@@ -154,6 +154,8 @@ def sample(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
     """(token, log probability, tokens left) of one row, logits as float64 numbers, by the limits' definitions."""
     x = np.asarray(logits, dtype=np.float64)
     x = np.where(np.isnan(x), -np.inf, x)
+    if (x == np.inf).any():
+        x = np.where(x == np.inf, 0.0, -np.inf)
     order = [int(i) for i in np.argsort(-x, kind="stable") if x[i] > -np.inf]
     if not order:
         return -1, -math.inf, 0
