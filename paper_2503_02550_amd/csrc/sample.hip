@@ -21,7 +21,7 @@
 
 namespace sif {
 
-constexpr uint32_t SM_THREADS = 1024, SM_WAVES = SM_THREADS / 64, SM_BINS = 2048, SM_LIST = 1024, SM_FEW = 512;      // SM_FEW: a top-k that the threads' largest bound
+constexpr uint32_t SM_THREADS = 1024, SM_WAVES = SM_THREADS / 64, SM_BINS = 4096, SM_LIST = 1024, SM_FEW = 512;      // SM_FEW: a top-k that the threads' largest bound
 constexpr uint32_t kKeyNone = 0x007FFFFFu;      // of -inf
 
 struct SampleArgs {
@@ -80,7 +80,7 @@ struct SampleSteps {
     const double t = fmax(((double)l - top) * per, -65504.0), m = t + 6755399441055744.0;
     return {(int)(uint32_t)__double_as_longlong(m), t - (m - 6755399441055744.0)};
   }
-  __device__ __forceinline__ static uint32_t bin(int n) { return (uint32_t)(SM_BINS - 1 + (n >> 5)); }      // 0 .. 2047
+  __device__ __forceinline__ static uint32_t bin(int n) { return (uint32_t)(SM_BINS - 1 + (n >> 4)); }      // 1 .. 4095
 };
 
 // A token's probability over the largest one's, times 2^s: 2^(t / 1024) from a table of 2^(i / 1024) and three terms of a series (the next one is 2^-50 at most).  2^-63.97 is as
@@ -99,11 +99,14 @@ struct SampleScale {
   __device__ __forceinline__ uint64_t mass(float l) const { return whole(scaled(steps.of(l))); }
 };
 
-// A row's logits, sixteen bytes at a time, neighbouring lanes neighbouring vectors.  What stands behind the row reads as -inf.
+// A row's logits, sixteen bytes at a time, neighbouring lanes neighbouring vectors, a piece of the row to each wavefront in order.  What stands behind the row reads as -inf.
+// The first vectors of every lane stay in LDS, the others are read again for every walk: 256 rows of 50304 fp32 logits are more than the L2s hold, half of them is not.
+constexpr uint32_t SM_HELD = 6;
 template <typename E>
 struct SampleRow {
   static constexpr uint32_t N = 16 / sizeof(E), STEP = 64 * N;
   const E* row;
+  uint4* held;                        // in LDS: [wavefront][SM_HELD][lane]
   uint32_t vocab;
   bool infinite;                      // there are logits of +inf: they read as 0 and the others as -inf
   struct Vec { float x[N]; };
@@ -113,66 +116,126 @@ struct SampleRow {
     else { v.x[0] = bflo(u.x); v.x[1] = bfhi(u.x); v.x[2] = bflo(u.y); v.x[3] = bfhi(u.y); v.x[4] = bflo(u.z); v.x[5] = bfhi(u.z); v.x[6] = bflo(u.w); v.x[7] = bfhi(u.w); }
     return v;
   }
+  __device__ __forceinline__ static float largest(const Vec& v) {
+    float x = v.x[0];
+#pragma unroll
+    for (uint32_t e = 1; e < N; ++e) x = fmaxf(x, v.x[e]);
+    return x;
+  }
   __device__ __forceinline__ uint4 raw(uint32_t i, uint32_t end) const {      // (rows are padded to whole vectors)
     constexpr uint32_t none = N == 4 ? 0xFF800000u : 0xFF80FF80u;
     return i < end ? *reinterpret_cast<const uint4*>(row + i) : make_uint4(none, none, none, none);
   }
-  // A wavefront's part of the row, from `first` on (a multiple of N) to `end`: f(index of the lane's first value, values).  Four vectors of a lane are on the way ahead
-  // of the one in use.
-  template <typename F> __device__ __forceinline__ void each(uint32_t first, uint32_t end, F&& f) const {
+  __device__ __forceinline__ uint32_t piece() const { return ((vocab + SM_WAVES - 1) / SM_WAVES + STEP - 1) / STEP * STEP; }
+  __device__ __forceinline__ Vec cleaned(Vec v, uint32_t at, uint32_t i) const {
+    if (at + STEP > vocab) {          // the row's end: the last vector may go beyond it
+#pragma unroll
+      for (uint32_t e = 0; e < N; ++e) v.x[e] = i + e < vocab ? v.x[e] : -INFINITY;
+    }
+    if (infinite) {
+#pragma unroll
+      for (uint32_t e = 0; e < N; ++e) v.x[e] = v.x[e] == INFINITY ? 0.f : -INFINITY;
+    }
+    return v;
+  }
+  // Elements `first` (a multiple of N) to `end`, by one wavefront: f(index of the lane's first value, values).  Four vectors of a lane are on the way ahead of the one in use.
+  template <typename F> __device__ __forceinline__ void read(uint32_t first, uint32_t end, F&& f) const {
     const uint32_t lane = threadIdx.x & 63;
     if (first >= end) return;
     uint32_t i = first + lane * N;
     uint4 a = raw(i, end), b = raw(i + STEP, end), c = raw(i + 2 * STEP, end), d = raw(i + 3 * STEP, end);
 #pragma unroll 1
     for (uint32_t at = first; at < end; at += STEP, i += STEP) {
-      Vec v = values(a);
+      const Vec v = cleaned(values(a), at, i);
       a = b;
       b = c;
       c = d;
       d = raw(i + 4 * STEP, end);
-      if (at + STEP > vocab) {        // the row's end: the last vector may go beyond it
-#pragma unroll
-        for (uint32_t e = 0; e < N; ++e) v.x[e] = i + e < vocab ? v.x[e] : -INFINITY;
-      }
-      if (infinite) {
-#pragma unroll
-        for (uint32_t e = 0; e < N; ++e) v.x[e] = v.x[e] == INFINITY ? 0.f : -INFINITY;
-      }
       f(i, v);
+    }
+  }
+  // The whole row.  FIRST: the first time, when the vectors come into LDS.
+  template <bool FIRST, typename F> __device__ __forceinline__ void walk(F&& f) const {
+    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, first = wave * piece(), end = std::min(first + piece(), vocab);
+    uint4* mine = held + wave * SM_HELD * 64 + lane;
+    if constexpr (FIRST) {
+      uint32_t j = 0;
+      read(first, end, [&](uint32_t i, const Vec& v) {
+        if (j < SM_HELD) {
+          if constexpr (N == 4) mine[j * 64] = make_uint4(__float_as_uint(v.x[0]), __float_as_uint(v.x[1]), __float_as_uint(v.x[2]), __float_as_uint(v.x[3]));
+          else mine[j * 64] = make_uint4(pack_bf2(v.x[0], v.x[1]), pack_bf2(v.x[2], v.x[3]), pack_bf2(v.x[4], v.x[5]), pack_bf2(v.x[6], v.x[7]));
+        }
+        ++j;
+        f(i, v);
+      });
+    } else {
+      // (the first ones that are read again are asked for in front of those in LDS)
+      const uint32_t again = first + SM_HELD * STEP;
+      uint32_t i = again + lane * N;
+      uint4 a = raw(i, end), b = raw(i + STEP, end), c = raw(i + 2 * STEP, end), d = raw(i + 3 * STEP, end);
+      const uint32_t till = std::min(end, again);
+      if (first < till) {
+        uint32_t k = first + lane * N;
+        uint4 u = mine[0];
+#pragma unroll 1
+        for (uint32_t at = first, j = 1; at < till; at += STEP, k += STEP, ++j) {
+          const Vec v = cleaned(values(u), at, k);
+          if (j < SM_HELD) u = mine[j * 64];
+          f(k, v);
+        }
+      }
+#pragma unroll 1
+      for (uint32_t at = again; at < end; at += STEP, i += STEP) {
+        const Vec v = cleaned(values(a), at, i);
+        a = b;
+        b = c;
+        c = d;
+        d = raw(i + 4 * STEP, end);
+        f(i, v);
+      }
     }
   }
 };
 
-__device__ __forceinline__ uint64_t sm_up64(uint64_t x, int o) {
-  return (uint64_t)(uint32_t)__shfl_up((uint32_t)(x >> 32), o, 64) << 32 | (uint32_t)__shfl_up((uint32_t)x, o, 64);
+// Inclusive sums over a wavefront: within sixteen lanes by row shifts, then the rows' last lanes to the rows behind them.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t sm_dpp(uint32_t x) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, ROWS, 0xF, false); }
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint64_t sm_dpp(uint64_t x) { return (uint64_t)sm_dpp<CTRL, ROWS>((uint32_t)(x >> 32)) << 32 | sm_dpp<CTRL, ROWS>((uint32_t)x); }
+template <typename T>
+__device__ __forceinline__ T sm_scan(T x) {
+  x += sm_dpp<0x111, 0xF>(x);
+  x += sm_dpp<0x112, 0xF>(x);
+  x += sm_dpp<0x114, 0xF>(x);
+  x += sm_dpp<0x118, 0xF>(x);
+  x += sm_dpp<0x142, 0xA>(x);
+  x += sm_dpp<0x143, 0xC>(x);
+  return x;
 }
-__device__ __forceinline__ uint64_t sm_scan64(uint64_t v) {            // inclusive, over a wavefront
-  const uint32_t lane = threadIdx.x & 63;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const uint64_t t = sm_up64(v, o);
-    if (lane >= (uint32_t)o) v += t;
-  }
-  return v;
-}
+__device__ __forceinline__ uint32_t sm_last(uint32_t x) { return (uint32_t)__builtin_amdgcn_readlane((int)x, 63); }
+__device__ __forceinline__ uint32_t sm_sum(uint32_t x) { return sm_last(sm_scan(x)); }
 
 struct SampleShared {
-  uint64_t bins[SM_BINS];             // counts or sums of probabilities
+  union {
+    uint64_t bins[SM_BINS];           // counts or sums of probabilities
+    struct {                          // (when a list is ranked its bin is found)
+      uint64_t sorted[SM_LIST], weight[SM_LIST];      // by rank; by place among the listed ones' numbers
+      uint32_t place[SM_LIST], rank[SM_LIST], by_place[SM_LIST];
+    };
+  };
   double table[1024];
-  uint64_t order[SM_LIST];            // a listed token's key, turned over, and its place in the list: in this order they are sorted
-  uint64_t weight[SM_LIST];           // by place
-  uint32_t token[SM_LIST], place[SM_LIST], rank[SM_LIST];      // by place, by rank, by place
+  uint64_t order[SM_LIST];            // a listed token's key, turned over, and its number: in this order they are sorted
   uint64_t wave[SM_WAVES];
   uint64_t above;                     // what lies above the bin that was found
   uint32_t bin, some[SM_WAVES], more[SM_WAVES];
   float best[SM_WAVES];
+  uint32_t listed;
+  uint4 held[SM_WAVES * SM_HELD * 64];
 };
 
 // Sums over the block.  Every thread gets the whole; barriers on both sides.
 __device__ __forceinline__ uint32_t sm_count(SampleShared& sh, uint32_t x) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o, 64);
+  x = sm_sum(x);
   if ((threadIdx.x & 63) == 0) sh.some[threadIdx.x >> 6] = x;
   __syncthreads();
   uint32_t all = 0;
@@ -183,7 +246,7 @@ __device__ __forceinline__ uint32_t sm_count(SampleShared& sh, uint32_t x) {
 // Inclusive sum over the block's threads; *all: over all of them.
 __device__ __forceinline__ uint64_t sm_block_scan(SampleShared& sh, uint64_t x, uint64_t* all) {
   const uint32_t wave = threadIdx.x >> 6;
-  uint64_t upto = sm_scan64(x), before = 0, total = 0;
+  uint64_t upto = sm_scan(x), before = 0, total = 0;
   if ((threadIdx.x & 63) == 63) sh.wave[wave] = upto;
   __syncthreads();
   for (uint32_t w = 0; w < SM_WAVES; ++w) {
@@ -200,16 +263,22 @@ __device__ __forceinline__ uint64_t sm_block_scan(SampleShared& sh, uint64_t x, 
 // of the bins above it.  Returns the sum of all bins.
 template <typename A>
 __device__ __forceinline__ uint64_t sm_find(SampleShared& sh, uint64_t above, A&& asked_of) {
-  const uint32_t t = threadIdx.x;
-  const uint64_t hi = sh.bins[SM_BINS - 1 - 2 * t], lo = sh.bins[SM_BINS - 2 - 2 * t];
-  uint64_t all;
-  if (t == 0) sh.bin = 0;
-  const uint64_t upto = sm_block_scan(sh, hi + lo, &all), start = upto - hi - lo;
+  constexpr uint32_t PER = SM_BINS / SM_THREADS;
+  const uint32_t first = SM_BINS - 1 - PER * threadIdx.x;      // the highest one of this thread's
+  uint64_t x[PER], mine = 0, all;
+#pragma unroll
+  for (uint32_t e = 0; e < PER; ++e) mine += x[e] = sh.bins[first - e];
+  if (threadIdx.x == 0) sh.bin = 0;
+  const uint64_t upto = sm_block_scan(sh, mine, &all);
+  uint64_t at = above + upto - mine;
   auto asked = asked_of(all);
-  const bool s0 = asked(above + start), s1 = asked(above + start + hi), s2 = asked(above + upto);
-  if (!s0 && s2) {                               // one thread, or none where all bins together do not reach it
-    sh.bin = s1 ? SM_BINS - 1 - 2 * t : SM_BINS - 2 - 2 * t;
-    sh.above = above + (s1 ? start : start + hi);
+  if (!asked(at) && asked(above + upto)) {       // one thread, or none where all bins together do not reach it
+    uint32_t e = 0;
+#pragma unroll
+    for (uint32_t z = 0; z + 1 < PER; ++z)
+      if (e == z && !asked(at + x[z])) { at += x[z]; e = z + 1; }
+    sh.bin = first - e;
+    sh.above = at;
   }
   __syncthreads();
   return all;
@@ -229,13 +298,10 @@ struct Sampler {
   SampleRow<E> row;
   SampleScale sc;
   uint32_t i, wave, lane;
-  float temperature, top_p, min_p, top;
+  float temperature, top_p, min_p, random, top;
   int32_t top_k;
 
-  template <typename F> __device__ __forceinline__ void each(F&& f) const {      // the whole row, a piece to each wavefront, in order
-    const uint32_t per = ((row.vocab + SM_WAVES - 1) / SM_WAVES + STEP - 1) / STEP * STEP;
-    row.each(wave * per, std::min((wave + 1) * per, row.vocab), f);
-  }
+  template <typename F> __device__ __forceinline__ void each(F&& f) const { row.template walk<false>(f); }
   __device__ __forceinline__ void answer(uint32_t token, float l, uint64_t all, uint32_t kept) const {
     a.token[i] = (int32_t)token;
     const double largest = sc.table[0];
@@ -243,8 +309,7 @@ struct Sampler {
     if (a.kept != nullptr) a.kept[i] = (int32_t)kept;
   }
   __device__ __forceinline__ double goal(uint64_t all) const {
-    const float u = a.random != nullptr ? a.random[i] : 0.f;
-    return (double)(u > 0.f ? std::min(u, 0.99999994f) : 0.f) * (double)all;
+    return (double)(random > 0.f ? std::min(random, 0.99999994f) : 0.f) * (double)all;
   }
   __device__ __forceinline__ double share(uint64_t all) const { return fmax((double)top_p * (double)all, 0.5); }      // what top-p asks for; at least one token
 
@@ -261,89 +326,77 @@ struct Sampler {
     return sm_value(hi);
   }
 
-  // Lists the tokens with logits of `low` and above, or where these are too many those below `high`, in the order of their numbers, and ranks them.  Returns how many
-  // there are, more than SM_LIST if neither fits; *whole: the list holds all from `low` on.
-  __device__ __forceinline__ uint32_t list(float low, float high, bool* whole) {
-    uint32_t ge = 0, gt = 0;                       // (of the wavefront)
-    each([&](uint32_t, const Vec& v) {
-#pragma unroll
-      for (uint32_t e = 0; e < N; ++e) {
-        ge += (uint32_t)__popcll(__ballot(v.x[e] >= low));
-        gt += (uint32_t)__popcll(__ballot(v.x[e] >= high));
-      }
-    });
-    if (lane == 0) { sh.some[wave] = ge; sh.more[wave] = ge - gt; }
+  // Lists the tokens with logits from `low` up to below `high`, in no order, and ranks them (`places`: and says where each stands among the listed ones' numbers).  Returns how many there are, more than SM_LIST if they do not fit.
+  __device__ __forceinline__ uint32_t list(float low, float high, bool places) {
+    if (threadIdx.x == 0) sh.listed = 0;
     __syncthreads();
-    uint32_t all_ge = 0, all_eq = 0, before_ge = 0, before_eq = 0;
-    for (uint32_t w = 0; w < SM_WAVES; ++w) {
-      const uint32_t x = sh.some[w], y = sh.more[w];
-      before_ge += w < wave ? x : 0u;
-      before_eq += w < wave ? y : 0u;
-      all_ge += x;
-      all_eq += y;
-    }
-    __syncthreads();
-    *whole = all_ge <= SM_LIST;
-    const uint32_t m = *whole ? all_ge : all_eq;
-    if (m > SM_LIST) return m;
-    const float end = *whole ? INFINITY : high;
-    uint32_t at = *whole ? before_ge : before_eq;
     each([&](uint32_t first, const Vec& v) {
-      uint64_t any = 0;
-#pragma unroll
-      for (uint32_t e = 0; e < N; ++e) any |= __ballot(v.x[e] >= low);
-      if (any == 0) return;
+      if (row.largest(v) < low) return;            // (of most lanes; NaN is not the largest of numbers)
       uint32_t mine = 0;
 #pragma unroll
-      for (uint32_t e = 0; e < N; ++e) mine |= v.x[e] >= low && v.x[e] < end ? 1u << e : 0u;
-      const uint32_t n = __popc(mine);
-      uint32_t upto = n;
-#pragma unroll
-      for (int o = 1; o < 64; o <<= 1) {
-        const uint32_t x = __shfl_up(upto, o, 64);
-        if (lane >= (uint32_t)o) upto += x;
-      }
-      uint32_t to = at + upto - n;
+      for (uint32_t e = 0; e < N; ++e) mine |= v.x[e] >= low && v.x[e] < high ? 1u << e : 0u;
+      if (mine == 0) return;
+      uint32_t to = atomicAdd(&sh.listed, (uint32_t)__popc(mine));
 #pragma unroll
       for (uint32_t e = 0; e < N; ++e)
         if (mine >> e & 1u) {
-          sh.order[to] = (uint64_t)(~sm_key(v.x[e])) << 32 | to;
-          sh.token[to++] = first + e;
+          if (to < SM_LIST) sh.order[to] = (uint64_t)(~sm_key(v.x[e])) << 32 | (first + e);
+          ++to;
         }
-      at += __shfl(upto, 63, 64);
     });
     __syncthreads();
-    if (m <= 256) rank_by_counting(m); else rank_by_sorting(m);
+    const uint32_t m = sh.listed;
+    if (m <= SM_LIST) {
+      if (m <= 256) rank_by_counting(m); else rank_by_sorting(m, places);
+    }
     return m;
   }
-  // Every entry counts those in front of it, a share of the list for each of the threads that an entry gets.
+  // How many tokens have logits from `low` on.
+  __device__ __forceinline__ uint32_t count(float low) {
+    uint32_t n = 0;
+    each([&](uint32_t, const Vec& v) {
+#pragma unroll
+      for (uint32_t e = 0; e < N; ++e) n += v.x[e] >= low ? 1u : 0u;
+    });
+    return sm_count(sh, n);
+  }
+  // Every entry counts those in front of it, by logits and by their numbers, a share of the list for each of the threads that an entry gets.  sorted[rank]: the
+  // entry; place[rank]: where its token stands among all.
   __device__ __forceinline__ void rank_by_counting(uint32_t m) {
     if (threadIdx.x < m) sh.rank[threadIdx.x] = 0;
     __syncthreads();
     uint32_t per = 1;                              // entries, as a power of two
     while (per < m) per <<= 1;
     const uint32_t mine = threadIdx.x & (per - 1), part = threadIdx.x / per, parts = SM_THREADS / per;
+    const uint64_t x = mine < m ? sh.order[mine] : 0;
     if (mine < m) {
-      const uint64_t x = sh.order[mine];
       const uint32_t size = (m + parts - 1) / parts, end = std::min(m, (part + 1) * size);
-      uint32_t before = 0;
-      for (uint32_t j = part * size; j < end; ++j) before += sh.order[j] < x ? 1u : 0u;
+      uint32_t before = 0;                         // (at most 256 of each: two numbers in a word)
+#pragma unroll 4
+      for (uint32_t j = part * size; j < end; ++j) {
+        const uint64_t y = sh.order[j];
+        before += (y < x ? 1u : 0u) + ((uint32_t)y < (uint32_t)x ? 1u << 16 : 0u);
+      }
       if (before != 0) atomicAdd(&sh.rank[mine], before);
     }
     __syncthreads();
-    if (threadIdx.x < m) sh.place[sh.rank[threadIdx.x]] = threadIdx.x;
+    if (threadIdx.x < m) {
+      const uint32_t r = sh.rank[threadIdx.x];
+      sh.sorted[r & 0xFFFFu] = x;
+      sh.place[r & 0xFFFFu] = r >> 16;
+    }
     __syncthreads();
   }
   // A bitonic sort, an entry to a thread: partners in the wavefront exchange by shuffles, others through LDS.
-  __device__ __forceinline__ void rank_by_sorting(uint32_t m) {
+  __device__ __forceinline__ uint64_t sorted_one(uint64_t x, uint32_t all) {
     const uint32_t t = threadIdx.x;
-    uint64_t x = t < m ? sh.order[t] : ~0ull;
 #pragma unroll 1
-    for (uint32_t size = 2; size <= SM_LIST; size <<= 1)
+    for (uint32_t size = 2; size <= all; size <<= 1)
 #pragma unroll 1
       for (uint32_t by = size >> 1; by > 0; by >>= 1) {
         uint64_t y;
         if (by < 64) {
+          if (t >= all) continue;
           y = (uint64_t)(uint32_t)__shfl_xor((uint32_t)(x >> 32), by, 64) << 32 | (uint32_t)__shfl_xor((uint32_t)x, by, 64);
         } else {
           sh.weight[t] = x;
@@ -354,15 +407,23 @@ struct Sampler {
         const bool small = ((t & by) == 0) == ((t & size) == 0);
         x = (x < y) == small ? x : y;
       }
-    if (t < m) sh.place[t] = (uint32_t)x;
+    return x;
+  }
+  __device__ __forceinline__ void rank_by_sorting(uint32_t m, bool places) {
+    const uint32_t t = threadIdx.x, all = m <= SM_LIST / 2 ? SM_LIST / 2 : SM_LIST;
+    const uint64_t x = sorted_one(t < m ? sh.order[t] : ~0ull, all);
+    if (t < m) sh.sorted[t] = x;
+    if (places) {                                  // by their numbers, the rank beside them
+      const uint64_t y = sorted_one(t < m ? x << 32 | t : ~0ull, all);
+      if (t < m) sh.place[(uint32_t)y] = t;
+    }
     __syncthreads();
   }
-  __device__ __forceinline__ uint32_t ranked_key(uint32_t rank) const { return ~(uint32_t)(sh.order[sh.place[rank]] >> 32); }
+  __device__ __forceinline__ uint32_t ranked_key(uint32_t rank) const { return ~(uint32_t)(sh.sorted[rank] >> 32); }
 
   // The token, where the list holds everything that is left (and what the limits leave out).  whole_sum: of all probabilities, where there is no top-k.
   __device__ __forceinline__ void draw_from_list(uint32_t m, bool by_k, uint64_t whole_sum) {
     const uint32_t r = threadIdx.x;
-    const uint32_t place = r < m ? sh.place[r] : 0u;
     const double y = r < m ? sc.scaled(sc.steps.of(sm_value(ranked_key(r)))) : 0.0;
     const uint64_t mass = SampleScale::whole(y);
     bool left = r < (by_k ? std::min(m, (uint32_t)top_k) : m);
@@ -372,13 +433,19 @@ struct Sampler {
       left = left && (double)(upto - mass) < share(by_k ? all : whole_sum);
     }
     left = left && !(y < (double)min_p * sc.table[0]);
-    if (r < m) sh.weight[place] = left ? mass : 0;
+    if (r < m) {
+      sh.weight[sh.place[r]] = left ? mass : 0;
+      sh.by_place[sh.place[r]] = r;
+    }
     const uint32_t kept = sm_count(sh, left ? 1u : 0u);      // (its barriers stand behind the weights too)
     const uint64_t mine = r < m ? sh.weight[r] : 0;
     uint64_t all;
     const uint64_t upto = sm_block_scan(sh, mine, &all);
     const double target = goal(all);
-    if (!((double)(upto - mine) > target) && (double)upto > target) answer(sh.token[r], sm_value(~(uint32_t)(sh.order[r] >> 32)), all, kept);
+    if (!((double)(upto - mine) > target) && (double)upto > target) {
+      const uint32_t rank = sh.by_place[r];
+      answer((uint32_t)sh.sorted[rank], sm_value(ranked_key(rank)), all, kept);
+    }
   }
 
   // The least key that is left and how many of those equal to it, from the keys' bits: for top-k, or by MASS for top-p of what `least` and `equal` leave so far.
@@ -433,6 +500,7 @@ struct Sampler {
   __device__ __forceinline__ void draw_from_row(uint32_t least, uint32_t equal) {
     const float bound = sm_value(least);
     const double least_mass = (double)min_p * sc.table[0];
+    const bool by_least = min_p > 0.f;
     // what is clearly below min-p needs no exponential
     const double cut = min_p > 0.f ? (double)top + (double)temperature * (log((double)min_p) - 1e-6) : -INFINITY;
     const float near_cut = (float)(cut - fabs(cut) * 1e-6);
@@ -444,10 +512,12 @@ struct Sampler {
       uint32_t seen = ties_before;
       if (equal != 0) {
         uint32_t ties = 0;
-        row.each(first, end, [&](uint32_t, const Vec& v) {
+        auto count = [&](uint32_t, const Vec& v) {
 #pragma unroll
-          for (uint32_t e = 0; e < N; ++e) ties += (uint32_t)__popcll(__ballot(v.x[e] == bound));
-        });
+          for (uint32_t e = 0; e < N; ++e) ties += v.x[e] == bound ? 1u : 0u;
+        };
+        if (whole) each(count); else row.read(first, end, count);
+        ties = sm_sum(ties);
         if (lane == 0) sh.some[wave] = ties;
         __syncthreads();
         for (uint32_t w = 0; w < wave; ++w) seen += sh.some[w];
@@ -457,7 +527,7 @@ struct Sampler {
       uint64_t sum = 0;
       uint32_t left = 0, last_keep = 0;
       Vec last = {};
-      row.each(first, end, [&](uint32_t, const Vec& v) {
+      auto weigh = [&](uint32_t, const Vec& v) {
         last = v;
         uint32_t keep = 0;
 #pragma unroll
@@ -467,30 +537,29 @@ struct Sampler {
 #pragma unroll
           for (uint32_t e = 0; e < N; ++e) mine += v.x[e] == bound ? 1u : 0u;
           if (__any(mine != 0)) {
-            uint32_t upto = mine;
-#pragma unroll
-            for (int o = 1; o < 64; o <<= 1) {
-              const uint32_t x = __shfl_up(upto, o, 64);
-              if (lane >= (uint32_t)o) upto += x;
-            }
+            const uint32_t upto = sm_scan(mine);
             uint32_t rank = seen + upto - mine;
 #pragma unroll
             for (uint32_t e = 0; e < N; ++e)
               if (v.x[e] == bound && rank++ < equal) keep |= 1u << e;
-            seen += __shfl(upto, 63, 64);
+            seen += sm_last(upto);
           }
         }
+        last_keep = keep;
+        if (!__any(keep != 0)) return;
+        double y[N];                               // (all of them at once: one by one each would wait for its table entry)
 #pragma unroll
-        for (uint32_t e = 0; e < N; ++e)
-          if (__any(keep >> e & 1u)) {
-            const double y = sc.scaled(sc.steps.of(v.x[e]));
-            if (y < least_mass) keep &= ~(1u << e);
-            sum += keep >> e & 1u ? SampleScale::whole(y) : 0;
-          }
+        for (uint32_t e = 0; e < N; ++e) y[e] = sc.scaled(sc.steps.of(v.x[e]));
+#pragma unroll
+        for (uint32_t e = 0; e < N; ++e) {
+          if (by_least && y[e] < least_mass) keep &= ~(1u << e);
+          sum += keep >> e & 1u ? SampleScale::whole(y[e]) : 0;
+        }
         left += __popc(keep);
         last_keep = keep;
-      });
-      const uint64_t upto = sm_scan64(sum);
+      };
+      if (whole) each(weigh); else row.read(first, end, weigh);
+      const uint64_t upto = sm_scan(sum);
       if (lane == 63) sh.wave[wave] = upto;
       const uint32_t here = sm_count(sh, left);
       uint64_t pieces = before, mine_before = before, won_before = before;
@@ -539,10 +608,8 @@ struct Sampler {
     // the largest logit, and where the first vector with it lies; and this thread's largest
     float mine = -INFINITY;
     uint32_t at = 0xFFFFFFFFu;
-    each([&](uint32_t first, const Vec& v) {
-      float x = v.x[0];
-#pragma unroll
-      for (uint32_t e = 1; e < N; ++e) x = fmaxf(x, v.x[e]);
+    row.template walk<true>([&](uint32_t first, const Vec& v) {
+      const float x = row.largest(v);
       if (x > mine) { mine = x; at = first; }
     });
     top = wave_max(mine);
@@ -582,16 +649,16 @@ struct Sampler {
     uint32_t least = kKeyNone, equal = 0;
     bool by_k = top_k > 0 && (uint32_t)top_k < row.vocab;
     if (by_k) {
-      uint32_t m = SM_LIST + 1;
-      bool whole = false;
       if ((uint32_t)top_k <= SM_FEW) {
         // at least top_k tokens reach the top_k-th of the threads' own largest (or there are fewer threads with tokens: the lowest bin, all tokens)
         sm_clear(sh);
         if (mine > -INFINITY) sm_add(sh, SampleSteps::bin(near.of(mine).n), 1);
         __syncthreads();
         sm_find(sh, 0, [&](uint64_t) { return [&](uint64_t sum) { return sum >= (uint64_t)top_k; }; });
-        m = list(least_of(near, sh.bin), INFINITY, &whole);
-        if (m <= SM_LIST && whole) return draw_from_list(m, true, 0);
+        // (the bin's lower end, a little below where it is)
+        const double end = (double)top + ((double)((int)sh.bin - (int)(SM_BINS - 1)) * 16.0 - 1.0) / near.per;
+        const uint32_t m = list(sh.bin != 0 ? fmaxf((float)(end - fabs(end) * 1e-6), -3.4028235e38f) : -3.4028235e38f, INFINITY, true);
+        if (m <= SM_LIST) return draw_from_list(m, true, 0);
       }
       __syncthreads();
       sm_clear(sh);
@@ -604,12 +671,13 @@ struct Sampler {
       const uint64_t some = sm_find(sh, 0, [&](uint64_t) { return [&](uint64_t sum) { return sum >= (uint64_t)top_k; }; });
       by_k = some > (uint64_t)(uint32_t)top_k;
       if (by_k) {
-        const uint32_t bin = sh.bin;
-        const uint64_t above = sh.above;
-        m = list(least_of(near, bin), bin + 1 < SM_BINS ? least_of(near, bin + 1) : INFINITY, &whole);
+        const uint32_t bin = sh.bin, above = (uint32_t)sh.above, here = (uint32_t)sh.bins[bin];
+        const bool whole = above + here <= SM_LIST;
+        uint32_t m = SM_LIST + 1;
+        if (whole || here <= SM_LIST) m = list(least_of(near, bin), whole || bin + 1 == SM_BINS ? INFINITY : least_of(near, bin + 1), whole);
         if (m <= SM_LIST && whole) return draw_from_list(m, true, 0);
         if (m <= SM_LIST) {
-          const uint32_t need = (uint32_t)top_k - (uint32_t)above;           // of the listed ones, in their order
+          const uint32_t need = (uint32_t)top_k - above;                     // of the listed ones, in their order
           least = ranked_key(need - 1);
           equal = sm_count(sh, threadIdx.x < need && ranked_key(threadIdx.x) == least ? 1u : 0u);
         } else {
@@ -635,8 +703,10 @@ struct Sampler {
       });
       const uint32_t bin = sh.bin;
       const uint64_t above = sh.above;
-      bool whole;
-      const uint32_t m = list(least_of(sc.steps, bin), bin + 1 < SM_BINS ? least_of(sc.steps, bin + 1) : INFINITY, &whole);
+      const float low = least_of(sc.steps, bin);
+      // (they are counted only where that many of the least possible weight would not make up far more than there is)
+      const bool whole = above + sh.bins[bin] <= 16 * SM_LIST * sc.mass(low) && count(low) <= SM_LIST;
+      const uint32_t m = list(low, whole || bin + 1 == SM_BINS ? INFINITY : least_of(sc.steps, bin + 1), whole);
       if (m <= SM_LIST && whole) return draw_from_list(m, false, all);
       if (m <= SM_LIST) {
         const uint32_t r = threadIdx.x, key = r < m ? ranked_key(r) : kKeyNone;
@@ -659,9 +729,9 @@ template <typename E>
 __global__ __launch_bounds__(SM_THREADS) void sample_kernel(SampleArgs a) {
   __shared__ SampleShared sh;
   const uint32_t i = blockIdx.x;
-  Sampler<E> s = {a, sh, {(const E*)a.logits + (size_t)i * a.ld, a.vocab, false}, {}, i, threadIdx.x >> 6, threadIdx.x & 63,
+  Sampler<E> s = {a, sh, {(const E*)a.logits + (size_t)i * a.ld, sh.held, a.vocab, false}, {}, i, threadIdx.x >> 6, threadIdx.x & 63,
                   a.temperature_list != nullptr ? a.temperature_list[i] : a.temperature, a.top_p_list != nullptr ? a.top_p_list[i] : a.top_p,
-                  std::min(a.min_p_list != nullptr ? a.min_p_list[i] : a.min_p, 1.f), 0.f, a.top_k_list != nullptr ? a.top_k_list[i] : a.top_k};
+                  std::min(a.min_p_list != nullptr ? a.min_p_list[i] : a.min_p, 1.f), a.random != nullptr ? a.random[i] : 0.f, 0.f, a.top_k_list != nullptr ? a.top_k_list[i] : a.top_k};
   s.run();
 }
 
