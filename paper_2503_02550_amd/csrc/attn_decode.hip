@@ -258,6 +258,8 @@ __global__ __launch_bounds__(256) void attn_decode_join_kernel(DecodeArgs a) {
 // the join (64 of 4096 170 -> 177, of 64-token pages 188 -> 197; 16 of 8000 85 -> 89 and 99 -> 112; 32 of 4000 the same; one of 262011
 // 189 -> 198 in pages of 64).  Splits that may be as short as a step cost more (128 of 500 13 -> 21), of 1024 tokens too (64 of 4096 182),
 // of 4096 leave 32 of 1 to 8000 at 111.
+// In 4 bits two blocks for each CU: a step is as long in time as there, but half of it is a wavefront's own work, and one wavefront on a SIMD leaves the memory idle meanwhile (one
+// sequence of 262011 tokens 70 -> 56 us); splits of 1366 to 4096 tokens all take 75 to 78 us for 64 sequences of 1 to 8192.
 static sif_status decode_plan(const char* who, const sif_kv_cache* c, const sif_attn_decode_args* a, DecodeArgs* out, uint64_t* bytes) {
   if (sif_status st = kv_check(who, c, &out->c)) return st;
   if (!a) return fail(SIF_E_INVAL, "%s: null arguments", who);
@@ -280,7 +282,7 @@ static sif_status decode_plan(const char* who, const sif_kv_cache* c, const sif_
   if (a->window != 0) seen = std::min<uint64_t>(seen, (uint64_t)a->window + a->sinks + 2 * tok);
   const uint64_t steps = std::max<uint64_t>(1, (seen + tok - 1) / tok);
   const uint64_t most = std::max<uint64_t>(1, steps / AD_WAVES);
-  const uint64_t one = std::min<uint64_t>(most, AD_BLOCKS / units), eight = a->n > 1 ? std::min<uint64_t>(seen / 2048, 8 * AD_BLOCKS / units) : 0;
+  const uint64_t one = std::min<uint64_t>(most, (c->dtype == SIF_E2M1 ? 2 : 1) * AD_BLOCKS / units), eight = a->n > 1 ? std::min<uint64_t>(seen / 2048, 8 * AD_BLOCKS / units) : 0;
   out->splits = (uint32_t)std::min<uint64_t>(AD_BLOCKS, std::max<uint64_t>(1, std::max(one, eight)));
   out->chunk = (uint32_t)((steps + out->splits - 1) / out->splits);
   *bytes = out->splits > 1 ? (uint64_t)a->n * a->heads * out->splits * (c->d_head + 4) * sizeof(float) : 256;

@@ -1,14 +1,19 @@
 // Attention of one new token per sequence over a paged cache in 4 bits (the formulas and the division of the work: attn_decode.hip).
 //
 // A token of a kv head of 128 is 136 bytes, so that what the memory delivers in a given time is four times as many tokens as in bf16 and the vector units have to
-// keep up: numbers are brought to bf16 two at a time by the conversion instruction, which takes the keys' powers of two along, and go into the matrix units as
-// they are.  A wavefront's step is 64 tokens:
+// keep up.  A wavefront's step is 64 tokens:
 //
-//   S^T = K Q^T    row 4a + b of tile t is token 16 a + 4 b + t.  A lane (row, g) has the d of its token that make one 16-byte fetch (8 of a head of 64): 32
-//                  consecutive d, so one power; its four tiles' powers are one word.  Its results (column = query head, rows 4g ..) are 16 consecutive tokens
-//   O^T = V^T P^T  byte (b, c) of a token holds d = 32 b + c and d + 16, so a lane's 16-byte fetch is the operand of two tiles of 16 d and 16 tokens.  The values'
-//                  powers differ from token to token: they go into P, whose rounding to bf16 they do not touch, once for each 32 d.  Lane (c, g) has those of
-//                  token 16 g + c, and hands them to the others of its sixteen as it multiplies.
+//   S^T = K Q^T    heads of 128: the matrix units take K's numbers and powers as they lie (16x16x128, numbers of 4 bits by such of 8), a lane (row, g) the 32 consecutive d
+//                  of its token that make one 16-byte fetch and share one power; its four tiles' powers are the bytes of one word.  Row 4a + b of tile t is token 16 a + 4 b + t.
+//                  Each 32 of q are split into two numbers of 4 bits of mantissa with a power of two of their own, which together are q: bf16 has 8 bits, the upper number takes
+//                  four of them, rounded, the lower one what is left (elements below 2^-14 of the 32's largest lose their last bits, 2^-22 of the largest).
+//                  Heads of 64: K is brought to bf16 by the conversion instruction, which takes the powers along.
+//   O^T = V^T P^T  byte (b, c) of a token holds d = 32 b + c and d + 16.  The conversion makes a pair of it, times the token's power, and a pair is two elements of a product's k
+//                  as well as any: P stands in one and zero in the other, first for the tile of d, then for that of d + 16.  That is twice the products for no shuffles at all;
+//                  the matrix units have the time.  Lane (c, g) has the powers of token 16 g + c and hands them to the others of its sixteen.
+//
+// Measured (64 sequences of 1 to 8192 tokens, 8 kv heads of 128, 286 MB): with K in bf16, V's halves brought together by masks and shifts and its powers multiplied into P
+// 612 vector instructions a step and 82 us.
 #include <type_traits>
 #include <utility>
 
@@ -25,15 +30,57 @@ __device__ __forceinline__ float of_row(float x) {
 template <typename F, int... I>
 __device__ __forceinline__ void for_each(std::integer_sequence<int, I...>, F&& f) { (f(std::integral_constant<int, I>{}), ...); }
 
+// Half of a query's split: 32 numbers of 8 bits, and the byte of the power that goes with the product's k from 32 g on.
+typedef int intx8 __attribute__((ext_vector_type(8)));
+struct SplitQ { intx8 x; int power; };
+// x: the lane's two runs of sixteen; neighbouring groups of sixteen lanes share the 32 that one power goes with.
+__device__ __forceinline__ void split_q(const uint4 (&x)[4], uint32_t g, SplitQ& hi, SplitQ& lo) {
+  int e[2];
+#pragma unroll
+  for (uint32_t r = 0; r < 2; ++r) {
+    uint32_t top = 0;
+    const uint32_t w[8] = {x[2 * r].x, x[2 * r].y, x[2 * r].z, x[2 * r].w, x[2 * r + 1].x, x[2 * r + 1].y, x[2 * r + 1].z, x[2 * r + 1].w};
+#pragma unroll
+    for (uint32_t k = 0; k < 8; ++k) top = std::max(top, std::max(w[k] << 16 & 0x7FFF0000u, w[k] & 0x7FFF0000u));
+    top = std::max(top, (uint32_t)__shfl_xor(top, 16, 64));
+    e[r] = std::max((int)(top >> 23), 12) - 127 - 7;                  // the largest becomes 128 to 256 (the lower half's power is 2^-4 of this one's, and not below 2^-127)
+    float f[16];
+#pragma unroll
+    for (uint32_t k = 0; k < 8; ++k) { f[2 * k] = ldexpf(bflo(w[k]), -e[r]); f[2 * k + 1] = ldexpf(bfhi(w[k]), -e[r]); }
+#pragma unroll
+    for (uint32_t k = 0; k < 4; ++k) {
+      int h = __builtin_amdgcn_cvt_pk_fp8_f32(f[4 * k], f[4 * k + 1], 0, false);
+      h = __builtin_amdgcn_cvt_pk_fp8_f32(f[4 * k + 2], f[4 * k + 3], h, true);
+      const floatx2_hw a = __builtin_amdgcn_cvt_pk_f32_fp8(h, false), b = __builtin_amdgcn_cvt_pk_f32_fp8(h, true);
+      int l = __builtin_amdgcn_cvt_pk_fp8_f32(16.f * (f[4 * k] - a[0]), 16.f * (f[4 * k + 1] - a[1]), 0, false);
+      l = __builtin_amdgcn_cvt_pk_fp8_f32(16.f * (f[4 * k + 2] - b[0]), 16.f * (f[4 * k + 3] - b[1]), l, true);
+      hi.x[4 * r + k] = h;
+      lo.x[4 * r + k] = l;
+    }
+  }
+  // the 32 from 32 g on: runs 2 g and 2 g + 1, the first four of which are the lanes' first ones
+  const uint32_t lane = threadIdx.x & 63, from = (g & 1) * 32 + (lane & 15);
+  const int e0 = __shfl(e[0], from, 64), e1 = __shfl(e[1], from, 64);
+  hi.power = (g < 2 ? e0 : e1) + 127;
+  lo.power = hi.power - 4;
+}
+
 template <int DH, bool STREAM>
 __global__ __launch_bounds__(256, 2) void attn_decode4_kernel(DecodeArgs a) {
   constexpr uint32_t TOK = 64, NT = 4, NB = DH / 32, KW = DH / 32, DT = DH / 16;      // tiles of 16 tokens; powers of a token; words of a lane's d
   const KvView& c = a.c;
-  const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, g = lane >> 4;
+  const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, g = lane >> 4;      // (steps are scalars)
   const uint32_t ht = blockIdx.x % a.head_tiles, kvh = blockIdx.x / a.head_tiles % c.kv_heads, i = blockIdx.x / a.head_tiles / c.kv_heads;
+  // the query first, looked at when the first contents are on their way: from the list to the length, the table and the pages there are four round trips
+  const uint32_t in_group = ht * AD_HEADS + col, head = kvh * a.group + in_group;
+  const bool head_ok = in_group < a.group;
+  const bf16_t* qp = a.q + (size_t)i * a.ld_q + (size_t)(head_ok ? head : kvh * a.group) * DH;
+  uint4 xq[DH / 32];
+#pragma unroll
+  for (uint32_t j = 0; j < DH / 32; ++j) xq[j] = *reinterpret_cast<const uint4*>(qp + (j >> 1) * 64 + g * 16 + (j & 1) * 8);      // the lane's runs of sixteen
   const int32_t s = kv_listed(c, a.seqs, i);
   const DecodeSpan sp = decode_span<TOK>(s >= 0 ? kv_length(c, s) : 0u, a.window, a.sinks);
-  const uint32_t parts = sp.steps == 0 ? 1u : std::min((sp.steps + a.chunk - 1) / a.chunk, a.splits), split = blockIdx.y;
+  const uint32_t parts = sp.steps == 0 ? 1u : std::min((sp.steps + a.chunk - 1) / a.chunk, a.splits), split = a.splits - 1 - blockIdx.y;      // (the last splits, which only long sequences have, first)
   auto unused = [&](uint32_t which) {
     if (threadIdx.x < std::min(a.group - ht * AD_HEADS, AD_HEADS))
       a.part[(((size_t)i * a.heads + kvh * a.group + ht * AD_HEADS + threadIdx.x) * a.splits + which) * (DH + 4) + 1] = kNoSplit;
@@ -41,19 +88,6 @@ __global__ __launch_bounds__(256, 2) void attn_decode4_kernel(DecodeArgs a) {
   if (split >= parts) { unused(split); return; }
   if (parts == 1 && a.splits > 1) unused(0);
   const uint32_t per = (sp.steps + parts - 1) / parts, end = std::min(sp.steps, (split + 1) * per);
-  const uint32_t in_group = ht * AD_HEADS + col, head = kvh * a.group + in_group;
-  const bool head_ok = in_group < a.group;
-
-  bf16x8 fq[KW];
-  {
-    const bf16_t* qp = a.q + (size_t)i * a.ld_q + (size_t)(head_ok ? head : kvh * a.group) * DH + g * (DH / 4);
-#pragma unroll
-    for (uint32_t j = 0; j < KW; ++j) {
-      uint4 v = *reinterpret_cast<const uint4*>(qp + j * 8);
-      if (!head_ok) v = make_uint4(0, 0, 0, 0);
-      fq[j] = as_bf16(v);
-    }
-  }
   const float c2 = a.scale * 1.44269504088896f;
   const size_t head_off = (size_t)kvh * (c.page_bytes / c.kv_heads), layer_off = (size_t)a.layer * c.n_pages;
   const unsigned char* kbase = c.k + layer_off * c.page_bytes + head_off;
@@ -65,23 +99,25 @@ __global__ __launch_bounds__(256, 2) void attn_decode4_kernel(DecodeArgs a) {
 #pragma unroll
   for (uint32_t d = 0; d < DT; ++d) oacc[d] = floatx4{0.f, 0.f, 0.f, 0.f};
   float m_run = -INFINITY, l_run = 0.f;
+  bf16x8 fq[DH == 64 ? KW : 1];                  // heads of 64
+  SplitQ hi, lo;                                 // heads of 128
 
-  struct Tile { uint32_t k[NT][KW]; uint4 v[NB]; uint32_t kpow, vpow, base; bool there; };
+  struct Tile { uint32_t k[NT][KW]; uint4 v[NB]; uint4 kpow; uint32_t vpow, base; bool there; };
   auto base_of = [&](uint32_t step) { return step < sp.sink_steps ? step * TOK : sp.from + (step - sp.sink_steps) * TOK; };
   auto page_at = [&](uint32_t token) { const uint32_t slot = token >> c.page_lg; return slot < pages ? row[slot] : -1; };
   auto fetch = [&](Tile& t, uint32_t step, int32_t kp, int32_t vp) {
     t.base = base_of(step);
     t.there = (uint32_t)vp < c.n_pages;
-    const uint32_t koff = (t.base + (col >> 2) * 16 + (col & 3) * 4) & page_mask, voff = (t.base + g * 16) & page_mask;
+    const uint32_t koff = (t.base + (col >> 2) * 16 + (col & 3)) & page_mask, voff = (t.base + g * 16) & page_mask;
     const unsigned char* kp8 = kbase + (size_t)((uint32_t)kp < c.n_pages ? kp : 0) * c.page_bytes;
     const unsigned char* vp8 = vbase + (size_t)(t.there ? vp : 0) * c.page_bytes;
 #pragma unroll
     for (uint32_t n = 0; n < NT; ++n) {
-      const unsigned char* at = kp8 + (koff + n) * (DH / 2) + g * (DH / 8);
+      const unsigned char* at = kp8 + (koff + 4 * n) * (DH / 2) + g * (DH / 8);
       if constexpr (KW == 4) *reinterpret_cast<uint4*>(t.k[n]) = *reinterpret_cast<const uint4*>(at);
       else *reinterpret_cast<uint2*>(t.k[n]) = *reinterpret_cast<const uint2*>(at);
     }
-    t.kpow = *reinterpret_cast<const uint32_t*>(kp8 + powers + ((g * DH / 128) << c.page_lg) + koff);
+    t.kpow = *reinterpret_cast<const uint4*>(kp8 + powers + ((g * DH / 128) << c.page_lg) + (koff & ~15u));
 #pragma unroll
     for (uint32_t b = 0; b < NB; ++b) {
       const unsigned char* at = vp8 + ((b * 16 + col) << c.page_lg) + voff;
@@ -92,21 +128,28 @@ __global__ __launch_bounds__(256, 2) void attn_decode4_kernel(DecodeArgs a) {
   };
   auto use = [&](Tile& t) {
     floatx4 sc[NT];                                        // element e of sc[n]: token 4 e + n of the lane's sixteen
-#pragma unroll
-    for (uint32_t n = 0; n < NT; ++n) {
-      const float power = e2m1_power(t.kpow >> (8 * n) & 255u);
+    for_each(std::make_integer_sequence<int, 4>{}, [&](auto nc) {
+      constexpr int n = decltype(nc)::value;
       sc[n] = floatx4{0.f, 0.f, 0.f, 0.f};
+      if constexpr (DH == 128) {
+        const uint32_t kp = (n == 0 ? t.kpow.x : n == 1 ? t.kpow.y : n == 2 ? t.kpow.z : t.kpow.w) >> (8 * (col & 3));
+        const intx8 x = {(int)t.k[n][0], (int)t.k[n][1], (int)t.k[n][2], (int)t.k[n][3], 0, 0, 0, 0};
+        sc[n] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x, hi.x, sc[n], 4, 0, 0, (int)kp, 0, hi.power);
+        sc[n] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x, lo.x, sc[n], 4, 0, 0, (int)kp, 0, lo.power);
+      } else {
+        const uint32_t kp = (n == 0 ? t.kpow.x : n == 1 ? t.kpow.y : n == 2 ? t.kpow.z : t.kpow.w) >> (8 * (col & 3));
+        const float power = e2m1_power(kp & 255u);
 #pragma unroll
-      for (uint32_t j = 0; j < KW; ++j) {
-        const uint32_t w = t.k[n][j];
-        sc[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16(make_uint4(e2m1x2<0>(w, power), e2m1x2<1>(w, power), e2m1x2<2>(w, power), e2m1x2<3>(w, power))), fq[j], sc[n], 0, 0, 0);
+        for (uint32_t j = 0; j < KW; ++j) {
+          const uint32_t w = t.k[n][j];
+          sc[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16(make_uint4(e2m1x2<0>(w, power), e2m1x2<1>(w, power), e2m1x2<2>(w, power), e2m1x2<3>(w, power))), fq[j], sc[n], 0, 0, 0);
+        }
       }
-      sc[n] *= c2;
-    }
+    });
     float vp[NB];
 #pragma unroll
     for (uint32_t b = 0; b < NB; ++b) vp[b] = e2m1_power(t.vpow >> (8 * b) & 255u);
-    // masks: what is held in tokens that are not visible may be anything, and their powers NaN: scores become -inf, powers zero
+    // masks: what is held in tokens that are not visible may be anything, and their powers NaN: scores become -inf, powers of two any number
     const uint32_t first = t.base + g * 16;
     const bool whole = t.base + TOK <= sp.len && (t.base >= sp.lo || t.base + TOK <= a.sinks);
     if (!whole || !__all(t.there)) {
@@ -119,17 +162,18 @@ __global__ __launch_bounds__(256, 2) void attn_decode4_kernel(DecodeArgs a) {
 #pragma unroll
       for (uint32_t n = 0; n < NT; ++n)
 #pragma unroll
-        for (uint32_t e = 0; e < 4; ++e) sc[n][e] = (keep >> (e * 4 + n)) & 1u ? sc[n][e] : -INFINITY;
+        for (uint32_t e = 0; e < 4; ++e) sc[n][e] = (keep >> (n * 4 + e)) & 1u ? sc[n][e] : -INFINITY;
 #pragma unroll
-      for (uint32_t b = 0; b < NB; ++b) vp[b] = (keep >> col) & 1u ? vp[b] : 0.f;
+      for (uint32_t b = 0; b < NB; ++b) vp[b] = (keep >> col) & 1u ? vp[b] : 1.f;
     }
+    // (the scale is above 0: the largest product is the largest score; the maximum is kept as a score, base 2)
     float mx = -INFINITY;
 #pragma unroll
     for (uint32_t n = 0; n < NT; ++n)
 #pragma unroll
       for (uint32_t e = 0; e < 4; ++e) mx = fmaxf(mx, sc[n][e]);
     mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
-    mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+    mx = fmaxf(mx, __shfl_xor(mx, 32, 64)) * c2;
     const float m_new = fmaxf(m_run, mx), m_use = m_new == -INFINITY ? 0.f : m_new;
     if (__any(m_new > m_run)) {
       const float alpha = __builtin_amdgcn_exp2f(m_run - m_use);
@@ -138,57 +182,57 @@ __global__ __launch_bounds__(256, 2) void attn_decode4_kernel(DecodeArgs a) {
       for (uint32_t d = 0; d < DT; ++d) oacc[d] *= alpha;
     }
     m_run = m_new;
+    for_each(std::make_integer_sequence<int, 4>{}, [&](auto nc) {
+      constexpr int n = decltype(nc)::value;               // tokens 4 n .. 4 n + 3
+      uint32_t lo_p[4], hi_p[4];                           // beside d, beside d + 16
 #pragma unroll
-    for (uint32_t e = 0; e < 4; ++e)
-#pragma unroll
-      for (uint32_t n = 0; n < NT; ++n) { sc[n][e] = __builtin_amdgcn_exp2f(sc[n][e] - m_use); l_run += sc[n][e]; }
-#pragma unroll
-    for (uint32_t b = 0; b < NB; ++b) {
-      uint32_t pk[8];                                      // words 2 e and 2 e + 1: tokens 4 e .. 4 e + 3
-      for_each(std::make_integer_sequence<int, 4>{}, [&](auto ec) {
-        constexpr int e = decltype(ec)::value;
-        pk[2 * e] = pack_bf2(sc[0][e] * of_row<4 * e>(vp[b]), sc[1][e] * of_row<4 * e + 1>(vp[b]));
-        pk[2 * e + 1] = pack_bf2(sc[2][e] * of_row<4 * e + 2>(vp[b]), sc[3][e] * of_row<4 * e + 3>(vp[b]));
-      });
-      const uint32_t w[4] = {t.v[b].x, t.v[b].y, t.v[b].z, t.v[b].w};
-#pragma unroll
-      for (uint32_t h = 0; h < 2; ++h) {
-        uint32_t x[4];                                     // of four tokens' bytes one half each, two to a byte: bytes 0 and 2
-#pragma unroll
-        for (uint32_t e = 0; e < 4; ++e) {
-          x[e] = (h == 0 ? w[e] : w[e] >> 4) & 0x0F0F0F0Fu;
-          x[e] |= x[e] >> 4;
-        }
-#pragma unroll
-        for (uint32_t o = 0; o < 2; ++o)
-          oacc[2 * b + h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-              as_bf16(make_uint4(e2m1x2<0>(x[2 * o], 1.f), e2m1x2<2>(x[2 * o], 1.f), e2m1x2<0>(x[2 * o + 1], 1.f), e2m1x2<2>(x[2 * o + 1], 1.f))),
-              as_bf16(make_uint4(pk[4 * o], pk[4 * o + 1], pk[4 * o + 2], pk[4 * o + 3])), oacc[2 * b + h], 0, 0, 0);
+      for (uint32_t e = 0; e < 4; ++e) {
+        const float p = __builtin_amdgcn_exp2f(fmaf(sc[n][e], c2, -m_use));
+        l_run += p;
+        lo_p[e] = pack_bf2(p, 0.f);
+        hi_p[e] = lo_p[e] << 16;
       }
-    }
+#pragma unroll
+      for (uint32_t b = 0; b < NB; ++b) {
+        const uint32_t w = n == 0 ? t.v[b].x : n == 1 ? t.v[b].y : n == 2 ? t.v[b].z : t.v[b].w;
+        const bf16x8 x = as_bf16(make_uint4(e2m1x2<0>(w, of_row<4 * n>(vp[b])), e2m1x2<1>(w, of_row<4 * n + 1>(vp[b])),
+                                            e2m1x2<2>(w, of_row<4 * n + 2>(vp[b])), e2m1x2<3>(w, of_row<4 * n + 3>(vp[b]))));
+        oacc[2 * b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, as_bf16(make_uint4(lo_p[0], lo_p[1], lo_p[2], lo_p[3])), oacc[2 * b], 0, 0, 0);
+        oacc[2 * b + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, as_bf16(make_uint4(hi_p[0], hi_p[1], hi_p[2], hi_p[3])), oacc[2 * b + 1], 0, 0, 0);
+      }
+    });
   };
-  // (every fourth of the split's steps, the next one's contents on the way, in front of them the page numbers of the one after that)
-  auto kpage_of = [&](uint32_t step) { return step < end ? page_at(base_of(step) + (col >> 2) * 16) : -1; };
-  auto vpage_of = [&](uint32_t step) { return step < end ? page_at(base_of(step) + g * 16) : -1; };
-  uint32_t step = split * per + wave;
-  if (step < end) {
+  // Every fourth of the split's steps, the next one's contents on the way, in front of them the page numbers of the one after that.  Behind the last step it is fetched
+  // once more: a fetch under a condition would make every step wait for all that is under way.
+  const uint32_t mine = split * per + wave;
+  if (mine < end) {
+    const uint32_t last = mine + (end - 1 - mine) / AD_WAVES * AD_WAVES;
+    auto kpage_of = [&](uint32_t step) { return page_at(base_of(std::min(step, last)) + (col >> 2) * 16); };
+    auto vpage_of = [&](uint32_t step) { return page_at(base_of(std::min(step, last)) + g * 16); };
     Tile t0, t1;
+    uint32_t step = mine;
     int32_t kp = kpage_of(step), vp = vpage_of(step), kn = kpage_of(step + AD_WAVES), vn = vpage_of(step + AD_WAVES);
     fetch(t0, step, kp, vp);
+#pragma unroll
+    for (uint32_t j = 0; j < DH / 32; ++j) xq[j] = head_ok ? xq[j] : make_uint4(0, 0, 0, 0);
+    if constexpr (DH == 64) {
+      fq[0] = as_bf16(xq[0]);
+      fq[1] = as_bf16(xq[1]);
+    } else {
+      split_q(xq, g, hi, lo);
+    }
     for (;;) {
       kp = kpage_of(step + 2 * AD_WAVES);
       vp = vpage_of(step + 2 * AD_WAVES);
-      const bool more = step + AD_WAVES < end;
-      if (more) fetch(t1, step + AD_WAVES, kn, vn);
+      fetch(t1, std::min(step + AD_WAVES, last), kn, vn);
       use(t0);
-      if (!more) break;
+      if (step == last) break;
       step += AD_WAVES;
       kn = kpage_of(step + 2 * AD_WAVES);
       vn = vpage_of(step + 2 * AD_WAVES);
-      const bool more2 = step + AD_WAVES < end;
-      if (more2) fetch(t0, step + AD_WAVES, kp, vp);
+      fetch(t0, std::min(step + AD_WAVES, last), kp, vp);
       use(t1);
-      if (!more2) break;
+      if (step == last) break;
       step += AD_WAVES;
     }
   }
