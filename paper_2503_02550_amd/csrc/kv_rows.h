@@ -1,5 +1,7 @@
 // Which token a row of new or read-back keys and values is, for the kernels that take rows by the list of a paged cache's sequences.
 #pragma once
+#include <algorithm>
+
 #include "common.h"
 #include "kv_cache.h"
 
@@ -7,21 +9,25 @@ namespace sif {
 
 constexpr uint32_t kKvRows = 16;         // rows of a block, sixteen threads each
 
-// Rows row0 .. row0 + 15 of lists as in sif_k_kv_write: pos the row's place in its sequence (kNoRow: the row is no sequence's; kBefore: it lies in
-// front of the sequence's first token), page its page or -1.  With `once` a sequence that stands in the list before has no page either.
+// Rows row0 .. row0 + 15 of lists as in sif_k_kv_write, sixteen threads to a row: s_pos gets the row's place in its sequence (kNoRow: the row is no sequence's; kBefore: it lies
+// in front of the sequence's first token).  Returns, in the first of the sixteen, the number of its page as the table has it, or -1; that load is still on its way.  With
+// `once` a sequence that stands in the list before has no page either.  The lists are read sixteen entries at a time: what counts is how many loads wait for one another.
 constexpr uint32_t kNoRow = 0xFFFFFFFFu, kBefore = 0xFFFFFFFEu;
 struct KvRowList { const int32_t* seqs; const int32_t* starts; uint32_t n, rows; };
-__device__ __forceinline__ void kv_find_rows(const KvView& c, const KvRowList& l, uint32_t row0, bool once, uint32_t* s_pos, int32_t* s_page) {
-  const uint32_t t = threadIdx.x, r = t >> 4, row = row0 + r;
+__device__ __forceinline__ int32_t kv_find_rows(const KvView& c, const KvRowList& l, uint32_t row0, bool pages, bool once, uint32_t* s_pos) {
+  const uint32_t t = threadIdx.x, r = t >> 4, part = t & 15, row = row0 + r, shift = t & 48;
   uint32_t i = row, pos = kNoRow;
   int32_t s = -1;
   if (row < l.rows) {
     uint32_t from = row, to = row + 1;
     if (l.starts != nullptr) {
-      uint32_t lo = 0, hi = l.n;                 // the last entry that begins at or before the row
-      while (lo < hi) {
-        const uint32_t mid = (lo + hi) >> 1;
-        if (l.starts[mid] <= (int32_t)row) lo = mid + 1; else hi = mid;
+      uint32_t lo = 0, size = l.n;               // the first entry that begins behind the row is one of lo .. lo + size
+      while (size > 0) {
+        const uint32_t step = (size + 15) / 16, at = (part + 1) * step - 1;
+        const bool upto = at < size && l.starts[lo + at] <= (int32_t)row;
+        const uint32_t c16 = __popc((uint32_t)(__ballot(upto) >> shift) & 0xFFFFu), skip = c16 * step;
+        lo += skip;
+        size = size > skip ? std::min(step - 1, size - skip) : 0u;
       }
       i = lo - 1;
       from = lo > 0 ? (uint32_t)l.starts[i] : 0u;
@@ -36,15 +42,17 @@ __device__ __forceinline__ void kv_find_rows(const KvView& c, const KvRowList& l
     }
   }
   bool again = false;
-  if (once && s >= 0 && l.seqs != nullptr)
-    for (uint32_t j = t & 15; j < i; j += 16) again |= l.seqs[j] == s;
-  const uint64_t votes = __ballot(again);
-  if ((t & 15) == 0) {
-    int32_t p = -1;
-    if (pos < kBefore && ((votes >> (t & 63)) & 0xFFFFull) == 0) p = c.table[(size_t)s * c.table_ld + (pos >> c.page_lg)];
-    s_page[r] = (uint32_t)p < c.n_pages ? p : -1;
+  if (once && s >= 0 && l.seqs != nullptr) {
+#pragma unroll 8
+    for (uint32_t j = part; j < i; j += 16) again |= l.seqs[j] == s;
+  }
+  const uint32_t votes = (uint32_t)(__ballot(again) >> shift) & 0xFFFFu;
+  int32_t p = -1;
+  if (part == 0) {
+    if (pages && pos < kBefore && votes == 0) p = c.table[(size_t)s * c.table_ld + (pos >> c.page_lg)];
     s_pos[r] = pos;
   }
+  return p;
 }
 
 // float -> e4m3, held at +-448, NaN kept; two at a time into the low half of a word

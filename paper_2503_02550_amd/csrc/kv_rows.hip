@@ -69,6 +69,8 @@ __device__ __forceinline__ uint64_t kv_xor64(uint64_t x, int lane) {
   const uint32_t lo = __shfl_xor((uint32_t)x, lane, 64), hi = __shfl_xor((uint32_t)(x >> 32), lane, 64);
   return (uint64_t)hi << 32 | lo;
 }
+typedef uint32_t u32x4_kv __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ uint4 kv_uint4(const u32x4_kv& x) { return make_uint4(x[0], x[1], x[2], x[3]); }
 __device__ __forceinline__ void kv_unpack8(const uint4& x, float (&f)[8]) {
   f[0] = bflo(x.x); f[1] = bfhi(x.x); f[2] = bflo(x.y); f[3] = bfhi(x.y);
   f[4] = bflo(x.z); f[5] = bfhi(x.z); f[6] = bflo(x.w); f[7] = bfhi(x.w);
@@ -92,41 +94,65 @@ __global__ __launch_bounds__(256) void kv_append_kernel(RopeView r, KvAppend a) 
   const KvView& c = a.c;
   const uint32_t t = threadIdx.x, row0 = blockIdx.x * kKvRows;
   const bool of_q = blockIdx.y >= a.kv_blocks;
-  kv_find_rows(c, a.l, row0, !of_q, s_pos, s_page);
-  __syncthreads();
   if (of_q) {
+    // (the first vectors are on their way while the rows are looked for)
+    const uint32_t units = r.half / 8, slots = 16 / units;
+    const uint32_t unit = t % units, slot = t / units % slots, row = t / (units * slots);
+    const uint32_t x = r.interleaved ? unit * 16 : unit * 8, y = r.interleaved ? x + 8 : x + r.half;
+    const size_t at = row0 + row;
+    uint32_t h = (blockIdx.y - a.kv_blocks) * slots + slot;
+    const size_t safe = std::min(row0 + row, a.l.rows - 1);
+    u32x4_kv nu = *reinterpret_cast<const u32x4_kv*>(a.q + safe * a.ld_q + std::min(h, a.heads - 1) * DH + x);
+    u32x4_kv nw = *reinterpret_cast<const u32x4_kv*>(a.q + safe * a.ld_q + std::min(h, a.heads - 1) * DH + y);
+    kv_find_rows(c, a.l, row0, false, false, s_pos);
+    __syncthreads();
     CosSin<float>* cs_all = reinterpret_cast<CosSin<float>*>(s_table);
     for (uint32_t i = t; i < kKvRows * r.half; i += 256) {
       const uint32_t pos = s_pos[i / r.half];
       if (pos < kBefore) cs_all[i] = rope_cos_sin<float>(r, (double)pos, i % r.half);
     }
     __syncthreads();
-    const uint32_t units = r.half / 8, slots = 16 / units;
-    const uint32_t unit = t % units, slot = t / units % slots, row = t / (units * slots);
     if (row >= kKvRows || s_pos[row] >= kBefore) return;
-    const size_t at = row0 + row;
     CosSin<float> cs[8];
 #pragma unroll
     for (uint32_t e = 0; e < 8; e += 2) *reinterpret_cast<float4*>(&cs[e]) = *reinterpret_cast<const float4*>(&cs_all[row * r.half + unit * 8 + e]);
-    const uint32_t x = r.interleaved ? unit * 16 : unit * 8, y = r.interleaved ? x + 8 : x + r.half;
-    for (uint32_t h = (blockIdx.y - a.kv_blocks) * slots + slot; h < a.heads; h += (gridDim.y - a.kv_blocks) * slots) {
+    while (h < a.heads) {
+      const uint32_t next = h + (gridDim.y - a.kv_blocks) * slots;
+      uint4 u = kv_uint4(nu), w = kv_uint4(nw);
+      nu = *reinterpret_cast<const u32x4_kv*>(a.q + at * a.ld_q + std::min(next, a.heads - 1) * DH + x);
+      nw = *reinterpret_cast<const u32x4_kv*>(a.q + at * a.ld_q + std::min(next, a.heads - 1) * DH + y);
       const bf16_t* from = a.q + at * a.ld_q + h * DH;
       bf16_t* to = a.q_out + at * a.ld_q_out + h * DH;
-      uint4 u = *reinterpret_cast<const uint4*>(from + x), w = *reinterpret_cast<const uint4*>(from + y);
       rope_turn8(r.interleaved, cs, 1.f, u, w);
       *reinterpret_cast<uint4*>(to + x) = u;
       *reinterpret_cast<uint4*>(to + y) = w;
       for (uint32_t e = unit; e < a.copy_q; e += units) *reinterpret_cast<uint4*>(to + 2 * r.half + e * 8) = *reinterpret_cast<const uint4*>(from + 2 * r.half + e * 8);
+      h = next;
     }
     return;
   }
-  CosSin<T>* cs_all = reinterpret_cast<CosSin<T>*>(s_table);
-  if constexpr (TURN) {
-    for (uint32_t i = t; i < kKvRows * r.half; i += 256)
-      if (s_page[i / r.half] >= 0) cs_all[i] = rope_cos_sin<T>(r, (double)s_pos[i / r.half], i % r.half);
-    __syncthreads();
-  }
   const uint32_t row = t / CH % kKvRows, ch = t % CH, hp = t / (CH * kKvRows), pt = 1u << c.page_lg;
+  // (of a turned chunk also the one whose elements are its partners)
+  const bool turned = TURN && ch * 8 < 2 * r.half, first = ch * 8 < r.half;
+  const uint32_t other = !turned || r.interleaved ? ch * 8 : first ? ch * 8 + r.half : ch * 8 - r.half;
+  struct Vectors { u32x4_kv own, partner, val; };
+  auto fetch = [&](uint32_t group) {
+    const uint32_t head = std::min(group * HP + hp, c.kv_heads - 1);       // (a head or a row too many is the last one)
+    const size_t at = std::min(row0 + row, a.l.rows - 1);
+    const bf16_t* from = a.k + at * a.ld_k + head * DH;
+    return Vectors{*reinterpret_cast<const u32x4_kv*>(from + ch * 8), *reinterpret_cast<const u32x4_kv*>(from + other), *reinterpret_cast<const u32x4_kv*>(a.v + at * a.ld_v + head * DH + ch * 8)};
+  };
+  Vectors next = fetch(blockIdx.y);                // (the first heads' vectors are on their way while the rows are looked for)
+  const int32_t found = kv_find_rows(c, a.l, row0, true, true, s_pos);
+  __syncthreads();
+  CosSin<T>* cs_all = reinterpret_cast<CosSin<T>*>(s_table);
+  if constexpr (TURN)
+    for (uint32_t i = t; i < kKvRows * r.half; i += 256) {
+      const uint32_t pos = s_pos[i / r.half];
+      if (pos < kBefore) cs_all[i] = rope_cos_sin<T>(r, (double)pos, i % r.half);
+    }
+  if ((t & 15) == 0) s_page[t >> 4] = (uint32_t)found < c.n_pages ? found : -1;
+  __syncthreads();
   const int32_t page = s_page[row];
   const uint32_t off = s_pos[row] & (pt - 1u);
   const size_t head_bytes = kv_head_bytes<DH, FMT>(c.page_lg), pool = ((size_t)a.layer * c.n_pages + (uint32_t)std::max(page, 0)) * c.page_bytes;
@@ -135,15 +161,12 @@ __global__ __launch_bounds__(256) void kv_append_kernel(RopeView r, KvAppend a) 
     const bool there = page >= 0 && head < c.kv_heads;
     const float ks = FMT == SIF_E4M3 && c.k_scale != nullptr && there ? c.k_scale[a.layer * c.kv_heads + head] : 1.f;
     const float vs = FMT == SIF_E4M3 && c.v_scale != nullptr && there ? c.v_scale[a.layer * c.kv_heads + head] : 1.f;
-    __syncthreads();                               // nobody reads the last heads' values any more
+    const uint4 own = kv_uint4(next.own), partner = kv_uint4(next.partner), val = kv_uint4(next.val);
+    next = fetch(group + a.kv_blocks);
     if (there) {
-      const bf16_t* from = a.k + (size_t)(row0 + row) * a.ld_k + head * DH;
-      const uint4 own = *reinterpret_cast<const uint4*>(from + ch * 8);
-      const uint4 val = *reinterpret_cast<const uint4*>(a.v + (size_t)(row0 + row) * a.ld_v + head * DH + ch * 8);
       float x[8], p[8];
       kv_unpack8(own, x);
       T y[8];
-      const bool turned = TURN && ch * 8 < 2 * r.half;
       if (turned) {
         const CosSin<T>* cs = cs_all + row * r.half;
         if (r.interleaved) {
@@ -154,9 +177,8 @@ __global__ __launch_bounds__(256) void kv_append_kernel(RopeView r, KvAppend a) 
             y[e + 1] = fma((T)x[e + 1], f.c, (T)x[e] * f.s);
           }
         } else {
-          const bool first = ch * 8 < r.half;
-          const uint32_t other = first ? ch * 8 + r.half : ch * 8 - r.half, pair = first ? ch * 8 : other;
-          kv_unpack8(*reinterpret_cast<const uint4*>(from + other), p);
+          const uint32_t pair = first ? ch * 8 : other;
+          kv_unpack8(partner, p);
 #pragma unroll
           for (uint32_t e = 0; e < 8; ++e) {
             const CosSin<T> f = cs[pair + e];
@@ -233,6 +255,7 @@ __global__ __launch_bounds__(256) void kv_append_kernel(RopeView r, KvAppend a) 
         else at[(line << c.page_lg) + voff] = from[line];
       }
     }
+    __syncthreads();                               // nobody reads these heads' values any more
   }
 }
 
@@ -259,74 +282,100 @@ __device__ __forceinline__ uint32_t kv_from_e4m3_hi(uint32_t w, float scale) {
   return pack_bf2(f[0] * scale, f[1] * scale);
 }
 
-// grid: (sixteen rows, groups of heads)
+// grid: (sixteen rows, groups of heads).  Four heads at a time: what a block takes is not bytes but loads that wait for one another.
 template <int DH, uint32_t FMT>
 __global__ __launch_bounds__(256) void kv_read_kernel(KvRead a) {
-  constexpr uint32_t CH = DH / 8, HP = 16 / CH;
+  constexpr uint32_t CH = DH / 8, HP = 16 / CH, TURNS = 4 / HP;
   constexpr uint32_t ROW = FMT == SIF_BF16 ? DH * 2 + 4 : FMT == SIF_E4M3 ? DH + 4 : DH / 2 + 4;
+  constexpr uint32_t LINES = FMT == SIF_E2M1 ? DH / 2 : DH, PER = LINES * HP / 16;      // rows of tokens of a page's head; of them a thread's
+  typedef typename std::conditional<FMT == SIF_BF16, uint16_t, uint8_t>::type Held;
   __shared__ int32_t s_page[kKvRows];
   __shared__ uint32_t s_pos[kKvRows];
-  __shared__ __align__(16) unsigned char s_v[HP * kKvRows * ROW];
+  __shared__ __align__(16) unsigned char s_v[TURNS * HP * kKvRows * ROW];
   const KvView& c = a.c;
   const uint32_t t = threadIdx.x, row0 = blockIdx.x * kKvRows;
-  kv_find_rows(c, a.l, row0, false, s_pos, s_page);
+  const int32_t found = kv_find_rows(c, a.l, row0, true, false, s_pos);
+  if ((t & 15) == 0) s_page[t >> 4] = (uint32_t)found < c.n_pages ? found : -1;
   __syncthreads();
   const uint32_t row = t / CH % kKvRows, ch = t % CH, hp = t / (CH * kKvRows), pt = 1u << c.page_lg;
   const int32_t page = s_page[row];
   const uint32_t off = s_pos[row] & (pt - 1u);
   const bool wanted = s_pos[row] != kNoRow;
   const size_t head_bytes = kv_head_bytes<DH, FMT>(c.page_lg), layer = (size_t)a.layer * c.n_pages;
-  constexpr uint32_t LINES = FMT == SIF_E2M1 ? DH / 2 : DH;
-  for (uint32_t group = blockIdx.y; group * HP < c.kv_heads; group += gridDim.y) {
-    const uint32_t vr = t & 15;
-    const int32_t vpage = s_page[vr];
-    __syncthreads();
-    if (vpage >= 0) {
-      const uint32_t voff = s_pos[vr] & (pt - 1u);
-      const unsigned char* from = c.v + (layer + (uint32_t)vpage) * c.page_bytes;
+  const uint32_t vr = t & 15;                      // the row whose values this thread fetches
+  const int32_t vpage = s_page[vr];
+  const uint32_t voff = s_pos[vr] & (pt - 1u);
+  const size_t pool = (layer + (uint32_t)std::max(page, 0)) * c.page_bytes, vpool = (layer + (uint32_t)std::max(vpage, 0)) * c.page_bytes;
+  for (uint32_t group = blockIdx.y * TURNS; group * HP < c.kv_heads; group += gridDim.y * TURNS) {
+    Held held[TURNS][PER];
+    uint4 k[TURNS];
+    uint32_t pk[TURNS], pv[TURNS];
 #pragma unroll
-      for (uint32_t j = 0; j < LINES * HP / 16; ++j) {
-        const uint32_t line = (j * 16 + (t >> 4)) % LINES, vh = (j * 16 + (t >> 4)) / LINES;
-        if (group * HP + vh >= c.kv_heads) continue;
-        const unsigned char* at = from + (group * HP + vh) * head_bytes;
-        unsigned char* to = s_v + (vh * kKvRows + vr) * ROW;
-        if constexpr (FMT == SIF_BF16) reinterpret_cast<bf16_t*>(to)[line] = reinterpret_cast<const bf16_t*>(at)[(line << c.page_lg) + voff];
-        else to[line] = at[(line << c.page_lg) + voff];
+    for (uint32_t u = 0; u < TURNS; ++u) {
+#pragma unroll
+      for (uint32_t j = 0; j < PER; ++j) {
+        const uint32_t line = (j * 16 + (t >> 4)) % LINES, vh = (group + u) * HP + (j * 16 + (t >> 4)) / LINES;
+        held[u][j] = 0;
+        if (vpage >= 0 && vh < c.kv_heads) held[u][j] = reinterpret_cast<const Held*>(c.v + vpool + vh * head_bytes)[(line << c.page_lg) + voff];
+      }
+      const uint32_t head = (group + u) * HP + hp;
+      k[u] = make_uint4(0, 0, 0, 0);
+      pk[u] = pv[u] = 0;
+      if (page >= 0 && head < c.kv_heads) {
+        const unsigned char* from = c.k + pool + head * head_bytes;
+        if constexpr (FMT == SIF_BF16) {
+          k[u] = *reinterpret_cast<const uint4*>(from + (off * DH + ch * 8) * 2);
+        } else if constexpr (FMT == SIF_E4M3) {
+          const uint2 w = *reinterpret_cast<const uint2*>(from + off * DH + ch * 8);
+          k[u].x = w.x;
+          k[u].y = w.y;
+        } else {
+          k[u].x = *reinterpret_cast<const uint32_t*>(from + off * (DH / 2) + ch * 4);
+          pk[u] = from[((DH / 2) << c.page_lg) + ((ch / 4) << c.page_lg) + off];
+          pv[u] = c.v[pool + head * head_bytes + ((DH / 2) << c.page_lg) + off * (DH / 32) + ch / 4];
+        }
       }
     }
+#pragma unroll
+    for (uint32_t u = 0; u < TURNS; ++u)
+#pragma unroll
+      for (uint32_t j = 0; j < PER; ++j) {
+        const uint32_t line = (j * 16 + (t >> 4)) % LINES, vh = u * HP + (j * 16 + (t >> 4)) / LINES;
+        reinterpret_cast<Held*>(s_v + (vh * kKvRows + vr) * ROW)[line] = held[u][j];
+      }
     __syncthreads();
-    const uint32_t head = group * HP + hp;
-    if (!wanted || head >= c.kv_heads) continue;
-    uint4 k = make_uint4(0, 0, 0, 0), v = k;
-    if (page >= 0) {
-      const size_t pool = (layer + (uint32_t)page) * c.page_bytes + head * head_bytes;
-      const unsigned char* from = c.k + pool;
-      const uint32_t* sv = reinterpret_cast<const uint32_t*>(s_v + (hp * kKvRows + row) * ROW);
-      if constexpr (FMT == SIF_BF16) {
-        k = *reinterpret_cast<const uint4*>(from + (off * DH + ch * 8) * 2);
-        v = make_uint4(sv[ch * 4], sv[ch * 4 + 1], sv[ch * 4 + 2], sv[ch * 4 + 3]);
-      } else if constexpr (FMT == SIF_E4M3) {
-        const float ks = c.k_scale != nullptr ? c.k_scale[a.layer * c.kv_heads + head] : 1.f, vs = c.v_scale != nullptr ? c.v_scale[a.layer * c.kv_heads + head] : 1.f;
-        const uint2 w = *reinterpret_cast<const uint2*>(from + off * DH + ch * 8);
-        k = make_uint4(kv_from_e4m3_lo(w.x, ks), kv_from_e4m3_hi(w.x, ks), kv_from_e4m3_lo(w.y, ks), kv_from_e4m3_hi(w.y, ks));
-        const uint32_t x = sv[ch * 2], y = sv[ch * 2 + 1];
-        v = make_uint4(kv_from_e4m3_lo(x, vs), kv_from_e4m3_hi(x, vs), kv_from_e4m3_lo(y, vs), kv_from_e4m3_hi(y, vs));
-      } else {
-        const unsigned char* tv = c.v + pool;
-        const float pk = e2m1_power(from[((DH / 2) << c.page_lg) + ((ch / 4) << c.page_lg) + off]), pv = e2m1_power(tv[((DH / 2) << c.page_lg) + off * (DH / 32) + ch / 4]);
-        const uint32_t w = *reinterpret_cast<const uint32_t*>(from + off * (DH / 2) + ch * 4);
-        k = make_uint4(kv_e2m1x2(w & 255u, pk), kv_e2m1x2(w >> 8 & 255u, pk), kv_e2m1x2(w >> 16 & 255u, pk), kv_e2m1x2(w >> 24, pk));
-        // eight bytes, of each the half that belongs to this chunk; two of these to a byte
-        uint32_t x = sv[ch / 4 * 4 + ch % 2 * 2], y = sv[ch / 4 * 4 + ch % 2 * 2 + 1];
-        x = (ch % 4 < 2 ? x : x >> 4) & 0x0F0F0F0Fu;
-        y = (ch % 4 < 2 ? y : y >> 4) & 0x0F0F0F0Fu;
-        x |= x >> 4;
-        y |= y >> 4;
-        v = make_uint4(kv_e2m1x2(x & 255u, pv), kv_e2m1x2(x >> 16 & 255u, pv), kv_e2m1x2(y & 255u, pv), kv_e2m1x2(y >> 16 & 255u, pv));
+#pragma unroll
+    for (uint32_t u = 0; u < TURNS; ++u) {
+      const uint32_t head = (group + u) * HP + hp;
+      if (!wanted || head >= c.kv_heads) continue;
+      const uint32_t* sv = reinterpret_cast<const uint32_t*>(s_v + ((u * HP + hp) * kKvRows + row) * ROW);
+      uint4 x = make_uint4(0, 0, 0, 0), y = x;
+      if (page >= 0) {
+        if constexpr (FMT == SIF_BF16) {
+          x = k[u];
+          y = make_uint4(sv[ch * 4], sv[ch * 4 + 1], sv[ch * 4 + 2], sv[ch * 4 + 3]);
+        } else if constexpr (FMT == SIF_E4M3) {
+          const float ks = c.k_scale != nullptr ? c.k_scale[a.layer * c.kv_heads + head] : 1.f, vs = c.v_scale != nullptr ? c.v_scale[a.layer * c.kv_heads + head] : 1.f;
+          x = make_uint4(kv_from_e4m3_lo(k[u].x, ks), kv_from_e4m3_hi(k[u].x, ks), kv_from_e4m3_lo(k[u].y, ks), kv_from_e4m3_hi(k[u].y, ks));
+          const uint32_t p = sv[ch * 2], q = sv[ch * 2 + 1];
+          y = make_uint4(kv_from_e4m3_lo(p, vs), kv_from_e4m3_hi(p, vs), kv_from_e4m3_lo(q, vs), kv_from_e4m3_hi(q, vs));
+        } else {
+          const float kp = e2m1_power(pk[u]), vp = e2m1_power(pv[u]);
+          const uint32_t w = k[u].x;
+          x = make_uint4(kv_e2m1x2(w & 255u, kp), kv_e2m1x2(w >> 8 & 255u, kp), kv_e2m1x2(w >> 16 & 255u, kp), kv_e2m1x2(w >> 24, kp));
+          // eight bytes, of each the half that belongs to this chunk; two of these to a byte
+          uint32_t p = sv[ch / 4 * 4 + ch % 2 * 2], q = sv[ch / 4 * 4 + ch % 2 * 2 + 1];
+          p = (ch % 4 < 2 ? p : p >> 4) & 0x0F0F0F0Fu;
+          q = (ch % 4 < 2 ? q : q >> 4) & 0x0F0F0F0Fu;
+          p |= p >> 4;
+          q |= q >> 4;
+          y = make_uint4(kv_e2m1x2(p & 255u, vp), kv_e2m1x2(p >> 16 & 255u, vp), kv_e2m1x2(q & 255u, vp), kv_e2m1x2(q >> 16 & 255u, vp));
+        }
       }
+      *reinterpret_cast<uint4*>(a.k + (size_t)(row0 + row) * a.ld_k + head * DH + ch * 8) = x;
+      *reinterpret_cast<uint4*>(a.v + (size_t)(row0 + row) * a.ld_v + head * DH + ch * 8) = y;
     }
-    *reinterpret_cast<uint4*>(a.k + (size_t)(row0 + row) * a.ld_k + head * DH + ch * 8) = k;
-    *reinterpret_cast<uint4*>(a.v + (size_t)(row0 + row) * a.ld_v + head * DH + ch * 8) = v;
+    __syncthreads();                               // nobody reads these heads' values any more
   }
 }
 
@@ -428,8 +477,8 @@ sif_status sif_k_kv_read(const sif_kv_cache* c, uint32_t layer, void* k, void* v
   a.layer = layer;
   a.ld_k = ld_k;
   a.ld_v = ld_v;
-  const uint32_t tiles = (rows + kKvRows - 1) / kKvRows, at_once = 128 / c->d_head, groups = (a.c.kv_heads + at_once - 1) / at_once;
-  const dim3 grid(tiles, kv_share(tiles, groups));
+  const uint32_t tiles = (rows + kKvRows - 1) / kKvRows;
+  const dim3 grid(tiles, kv_share(tiles, (a.c.kv_heads + 3) / 4));
 #define KV_READ(DH, F) hipLaunchKernelGGL((kv_read_kernel<DH, F>), grid, dim3(256), 0, S(stream), a)
   if (c->d_head == 64) { if (c->dtype == SIF_BF16) KV_READ(64, SIF_BF16); else if (c->dtype == SIF_E4M3) KV_READ(64, SIF_E4M3); else KV_READ(64, SIF_E2M1); }
   else { if (c->dtype == SIF_BF16) KV_READ(128, SIF_BF16); else if (c->dtype == SIF_E4M3) KV_READ(128, SIF_E4M3); else KV_READ(128, SIF_E2M1); }
