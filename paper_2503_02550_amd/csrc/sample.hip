@@ -154,6 +154,12 @@ struct SampleRow {
       f(i, v);
     }
   }
+  // A part of one wavefront's piece, by any wavefront: a vector for each lane from LDS, where it is there.
+  template <typename F> __device__ __forceinline__ void again(uint32_t first, uint32_t end, uint32_t piece_of, F&& f) const {
+    const uint32_t lane = threadIdx.x & 63, j = (first - piece_of * piece()) / STEP;
+    if (first >= end || end - first > STEP || j >= SM_HELD) return read(first, end, f);
+    f(first + lane * N, cleaned(values(held[(piece_of * SM_HELD + j) * 64 + lane]), first, first + lane * N));
+  }
   // The whole row.  FIRST: the first time, when the vectors come into LDS.
   template <bool FIRST, typename F> __device__ __forceinline__ void walk(F&& f) const {
     const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, first = wave * piece(), end = std::min(first + piece(), vocab);
@@ -504,7 +510,7 @@ struct Sampler {
     // what is clearly below min-p needs no exponential
     const double cut = min_p > 0.f ? (double)top + (double)temperature * (log((double)min_p) - 1e-6) : -INFINITY;
     const float near_cut = (float)(cut - fabs(cut) * 1e-6);
-    uint32_t lo = 0, hi = row.vocab, ties_before = 0, kept = 0;
+    uint32_t lo = 0, hi = row.vocab, ties_before = 0, kept = 0, won_piece = 0;
     uint64_t before = 0, all = 0;
     double target = 0.0;
     for (bool whole = true;; whole = false) {
@@ -516,7 +522,7 @@ struct Sampler {
 #pragma unroll
           for (uint32_t e = 0; e < N; ++e) ties += v.x[e] == bound ? 1u : 0u;
         };
-        if (whole) each(count); else row.read(first, end, count);
+        if (whole) each(count); else row.again(first, end, won_piece, count);
         ties = sm_sum(ties);
         if (lane == 0) sh.some[wave] = ties;
         __syncthreads();
@@ -525,13 +531,17 @@ struct Sampler {
       }
       const uint32_t seen_first = seen;
       uint64_t sum = 0;
-      uint32_t left = 0, last_keep = 0;
-      Vec last = {};
-      auto weigh = [&](uint32_t, const Vec& v) {
-        last = v;
-        uint32_t keep = 0;
+      uint32_t left = 0;
+      Vec last;                                    // a lane's last vector, what is not left as -inf
 #pragma unroll
-        for (uint32_t e = 0; e < N; ++e) keep |= v.x[e] > bound && v.x[e] >= near_cut ? 1u << e : 0u;
+      for (uint32_t e = 0; e < N; ++e) last.x[e] = -INFINITY;
+      auto weigh = [&](uint32_t, const Vec& v) {
+        uint32_t here = 0;
+#pragma unroll
+        for (uint32_t e = 0; e < N; ++e) {
+          last.x[e] = v.x[e] > bound && v.x[e] >= near_cut ? v.x[e] : -INFINITY;
+          here += v.x[e] > bound && v.x[e] >= near_cut ? 1u : 0u;
+        }
         if (equal != 0) {
           uint32_t mine = 0;
 #pragma unroll
@@ -541,24 +551,31 @@ struct Sampler {
             uint32_t rank = seen + upto - mine;
 #pragma unroll
             for (uint32_t e = 0; e < N; ++e)
-              if (v.x[e] == bound && rank++ < equal) keep |= 1u << e;
+              if (v.x[e] == bound && rank++ < equal) {
+                last.x[e] = bound;
+                ++here;
+              }
             seen += sm_last(upto);
           }
         }
-        last_keep = keep;
-        if (!__any(keep != 0)) return;
+        if (!__any(here != 0)) return;
         double y[N];                               // (all of them at once: one by one each would wait for its table entry)
 #pragma unroll
-        for (uint32_t e = 0; e < N; ++e) y[e] = sc.scaled(sc.steps.of(v.x[e]));
+        for (uint32_t e = 0; e < N; ++e) y[e] = sc.scaled(sc.steps.of(last.x[e]));
+        if (by_least) {
 #pragma unroll
-        for (uint32_t e = 0; e < N; ++e) {
-          if (by_least && y[e] < least_mass) keep &= ~(1u << e);
-          sum += keep >> e & 1u ? SampleScale::whole(y[e]) : 0;
+          for (uint32_t e = 0; e < N; ++e)
+            if (last.x[e] > -INFINITY && y[e] < least_mass) {
+              last.x[e] = -INFINITY;
+              y[e] = 0.0;
+              --here;
+            }
         }
-        left += __popc(keep);
-        last_keep = keep;
+#pragma unroll
+        for (uint32_t e = 0; e < N; ++e) sum += SampleScale::whole(y[e]);
+        left += here;
       };
-      if (whole) each(weigh); else row.read(first, end, weigh);
+      if (whole) each(weigh); else row.again(first, end, won_piece, weigh);
       const uint64_t upto = sm_scan(sum);
       if (lane == 63) sh.wave[wave] = upto;
       const uint32_t here = sm_count(sh, left);
@@ -586,7 +603,7 @@ struct Sampler {
 #pragma unroll
         for (uint32_t z = N; z-- > 0;) {            // the first at which the sum exceeds it, looked at from the last on
           if ((double)x > target) { e = z; l = last.x[z]; }
-          x -= last_keep >> z & 1u ? sc.mass(last.x[z]) : 0;
+          x -= sc.mass(last.x[z]);
         }
         return answer(first + lane * N + e, l, all, kept);
       }
@@ -598,6 +615,7 @@ struct Sampler {
       }
       __syncthreads();                             // nobody reads this turn's sums any more
       before = won_before;
+      if (whole) won_piece = won;
       lo += won * per;
       hi = std::min(lo + per, hi);
     }
