@@ -21,7 +21,8 @@
 
 namespace sif {
 
-constexpr uint32_t SM_THREADS = 1024, SM_WAVES = SM_THREADS / 64, SM_BINS = 4096, SM_LIST = 1024, SM_FEW = 512;      // SM_FEW: a top-k that the threads' largest bound
+constexpr uint32_t SM_THREADS = 1024, SM_WAVES = SM_THREADS / 64, SM_BINS = 4096, SM_LIST = 1024, SM_COUNTED = 512;
+constexpr uint32_t SM_FEW = 512;       // a top-k that the threads' largest bound
 constexpr uint32_t kKeyNone = 0x007FFFFFu;      // of -inf
 
 struct SampleArgs {
@@ -91,11 +92,13 @@ struct SampleScale {
   __device__ __forceinline__ double scaled(const SampleStep& x) const {
     constexpr double k = 0.693147180559945309417 / 1024.0;
     const double p = fma(fma(fma(k * k * k / 6.0, x.r, k * k / 2.0), x.r, k), x.r, 1.0);
-    return ldexp(table[x.n & 1023] * p, x.n >> 10);
+    const double y = table[x.n & 1023] * p;        // (no less than 2^s, s from 30 on, so the exponent takes n's whole part as it is)
+    return __hiloint2double(__double2hiint(y) + (x.n >> 10 << 20), __double2loint(y));
   }
-  __device__ __forceinline__ static uint64_t whole(double y) {      // to the nearest (below 2^52: added to 2^52 it is the sum's mantissa)
-    return (uint64_t)__double_as_longlong(y + 4503599627370496.0) & 0xFFFFFFFFFFFFFull;
-  }
+  // To the nearest whole number: below 2^52 it is the mantissa of the sum with 2^52, whose other bits sums may leave in and take away once.
+  static constexpr uint64_t kRaw = 0x4330000000000000ull;
+  __device__ __forceinline__ static uint64_t raw(double y) { return (uint64_t)__double_as_longlong(y + 4503599627370496.0); }
+  __device__ __forceinline__ static uint64_t whole(double y) { return raw(y) & 0xFFFFFFFFFFFFFull; }
   __device__ __forceinline__ uint64_t mass(float l) const { return whole(scaled(steps.of(l))); }
 };
 
@@ -224,9 +227,9 @@ __device__ __forceinline__ uint32_t sm_sum(uint32_t x) { return sm_last(sm_scan(
 struct SampleShared {
   union {
     uint64_t bins[SM_BINS];           // counts or sums of probabilities
-    struct {                          // (when a list is ranked its bin is found)
+    struct {                          // (when a list is made its bin is found)
       uint64_t sorted[SM_LIST], weight[SM_LIST];      // by rank; by place among the listed ones' numbers
-      uint32_t place[SM_LIST], rank[SM_LIST], by_place[SM_LIST];
+      uint32_t turn[SM_LIST], number[SM_LIST], rank[SM_LIST];      // as it was listed: its turn in its wavefront; by place
     };
   };
   double table[1024];
@@ -332,29 +335,38 @@ struct Sampler {
     return sm_value(hi);
   }
 
-  // Lists the tokens with logits from `low` up to below `high`, in no order, and ranks them (`places`: and says where each stands among the listed ones' numbers).  Returns how many there are, more than SM_LIST if they do not fit.
-  __device__ __forceinline__ uint32_t list(float low, float high, bool places) {
+  // Lists the tokens with logits from `low` up to below `high`, in no order, and ranks them.  Returns how many there are, more than SM_LIST if they do not fit.
+  __device__ __forceinline__ uint32_t list(float low, float high) {
     if (threadIdx.x == 0) sh.listed = 0;
     __syncthreads();
+    uint32_t listed = 0;                           // by this wavefront, which comes to them in the order of their numbers
     each([&](uint32_t first, const Vec& v) {
-      if (row.largest(v) < low) return;            // (of most lanes; NaN is not the largest of numbers)
+      if (!__any(row.largest(v) >= low)) return;   // (of most vectors; NaN is not the largest of numbers)
       uint32_t mine = 0;
 #pragma unroll
       for (uint32_t e = 0; e < N; ++e) mine |= v.x[e] >= low && v.x[e] < high ? 1u << e : 0u;
-      if (mine == 0) return;
-      uint32_t to = atomicAdd(&sh.listed, (uint32_t)__popc(mine));
+      const uint32_t upto = sm_scan((uint32_t)__popc(mine)), n = sm_last(upto), before = upto - (uint32_t)__popc(mine);
+      if (n == 0) return;
+      uint32_t to = 0;                             // the wavefront's places, one request for all of them
+      if (lane == 0) to = atomicAdd(&sh.listed, n);
+      to = (uint32_t)__builtin_amdgcn_readfirstlane((int)to) + before;
+      uint32_t turn = listed + before;
+      for (; mine != 0; mine &= mine - 1, ++to, ++turn) {
+        const uint32_t e = (uint32_t)__ffs((int)mine) - 1;
+        float x = v.x[0];
 #pragma unroll
-      for (uint32_t e = 0; e < N; ++e)
-        if (mine >> e & 1u) {
-          if (to < SM_LIST) sh.order[to] = (uint64_t)(~sm_key(v.x[e])) << 32 | (first + e);
-          ++to;
+        for (uint32_t z = 1; z < N; ++z) x = e == z ? v.x[z] : x;
+        if (to < SM_LIST) {
+          sh.order[to] = (uint64_t)(~sm_key(x)) << 32 | (first + e);
+          sh.turn[to] = turn;
         }
+      }
+      listed += n;
     });
+    if (lane == 0) sh.some[wave] = listed;
     __syncthreads();
     const uint32_t m = sh.listed;
-    if (m <= SM_LIST) {
-      if (m <= 256) rank_by_counting(m); else rank_by_sorting(m, places);
-    }
+    if (m <= SM_LIST) rank(m);
     return m;
   }
   // How many tokens have logits from `low` on.
@@ -362,47 +374,58 @@ struct Sampler {
     uint32_t n = 0;
     each([&](uint32_t, const Vec& v) {
 #pragma unroll
-      for (uint32_t e = 0; e < N; ++e) n += v.x[e] >= low ? 1u : 0u;
+      for (uint32_t e = 0; e < N; ++e) n += (uint32_t)__popcll(__ballot(v.x[e] >= low));
     });
-    return sm_count(sh, n);
+    return sm_count(sh, lane == 0 ? n : 0);
   }
-  // Every entry counts those in front of it, by logits and by their numbers, a share of the list for each of the threads that an entry gets.  sorted[rank]: the
-  // entry; place[rank]: where its token stands among all.
-  __device__ __forceinline__ void rank_by_counting(uint32_t m) {
-    if (threadIdx.x < m) sh.rank[threadIdx.x] = 0;
-    __syncthreads();
-    uint32_t per = 1;                              // entries, as a power of two
-    while (per < m) per <<= 1;
-    const uint32_t mine = threadIdx.x & (per - 1), part = threadIdx.x / per, parts = SM_THREADS / per;
-    const uint64_t x = mine < m ? sh.order[mine] : 0;
-    if (mine < m) {
-      const uint32_t size = (m + parts - 1) / parts, end = std::min(m, (part + 1) * size);
-      uint32_t before = 0;                         // (at most 256 of each: two numbers in a word)
-#pragma unroll 4
-      for (uint32_t j = part * size; j < end; ++j) {
-        const uint64_t y = sh.order[j];
-        before += (y < x ? 1u : 0u) + ((uint32_t)y < (uint32_t)x ? 1u << 16 : 0u);
-      }
-      if (before != 0) atomicAdd(&sh.rank[mine], before);
+  // Ranks the list, by falling logits and rising numbers.  Beside its logit an entry gets in the place of its number the place among the listed ones' numbers, which is of the same
+  // order.  sorted[rank]: the entry; number[place].
+  __device__ __forceinline__ void rank(uint32_t m) {
+    const uint32_t t = threadIdx.x;
+    uint64_t x = ~0ull;
+    if (t < m) {
+      const uint32_t at = (uint32_t)sh.order[t];
+      uint32_t place = sh.turn[t];
+#pragma unroll
+      for (uint32_t w = 0; w + 1 < SM_WAVES; ++w) place += at >= (w + 1) * row.piece() ? sh.some[w] : 0;
+      x = sh.order[t] >> 32 << 32 | place;
+      sh.number[place] = at;
     }
-    __syncthreads();
-    if (threadIdx.x < m) {
-      const uint32_t r = sh.rank[threadIdx.x];
-      sh.sorted[r & 0xFFFFu] = x;
-      sh.place[r & 0xFFFFu] = r >> 16;
+    if (m <= SM_COUNTED) {
+      // Every entry counts those in front of it, a share of the list for each of the threads that it gets.  (One row, top-k 200: 17.4 us so, 22.6 sorted; 500, some 800 listed: 32.2 and 23.3.)
+      if (t < m) {
+        sh.order[t] = x;
+        sh.rank[t] = 0;
+      }
+      __syncthreads();
+      uint32_t per = 1;                            // entries, as a power of two
+      while (per < m) per <<= 1;
+      const uint32_t mine = t & (per - 1), part = t / per, parts = SM_THREADS / per;
+      if (mine < m) {
+        const uint32_t size = (m + parts - 1) / parts, end = std::min(m, (part + 1) * size);
+        x = sh.order[mine];
+        uint32_t before = 0;
+#pragma unroll 4
+        for (uint32_t j = part * size; j < end; ++j) before += sh.order[j] < x ? 1u : 0u;
+        if (before != 0) atomicAdd(&sh.rank[mine], before);
+      }
+      __syncthreads();
+      if (t < m) sh.sorted[sh.rank[t]] = x;
+    } else {
+      x = sorted_one(x);
+      if (t < m) sh.sorted[t] = x;
     }
     __syncthreads();
   }
   // A bitonic sort, an entry to a thread: partners in the wavefront exchange by shuffles, others through LDS.
-  __device__ __forceinline__ uint64_t sorted_one(uint64_t x, uint32_t all) {
+  __device__ __forceinline__ uint64_t sorted_one(uint64_t x) {
     const uint32_t t = threadIdx.x;
 #pragma unroll 1
-    for (uint32_t size = 2; size <= all; size <<= 1)
+    for (uint32_t size = 2; size <= SM_LIST; size <<= 1)
 #pragma unroll 1
       for (uint32_t by = size >> 1; by > 0; by >>= 1) {
         uint64_t y;
         if (by < 64) {
-          if (t >= all) continue;
           y = (uint64_t)(uint32_t)__shfl_xor((uint32_t)(x >> 32), by, 64) << 32 | (uint32_t)__shfl_xor((uint32_t)x, by, 64);
         } else {
           sh.weight[t] = x;
@@ -414,16 +437,6 @@ struct Sampler {
         x = (x < y) == small ? x : y;
       }
     return x;
-  }
-  __device__ __forceinline__ void rank_by_sorting(uint32_t m, bool places) {
-    const uint32_t t = threadIdx.x, all = m <= SM_LIST / 2 ? SM_LIST / 2 : SM_LIST;
-    const uint64_t x = sorted_one(t < m ? sh.order[t] : ~0ull, all);
-    if (t < m) sh.sorted[t] = x;
-    if (places) {                                  // by their numbers, the rank beside them
-      const uint64_t y = sorted_one(t < m ? x << 32 | t : ~0ull, all);
-      if (t < m) sh.place[(uint32_t)y] = t;
-    }
-    __syncthreads();
   }
   __device__ __forceinline__ uint32_t ranked_key(uint32_t rank) const { return ~(uint32_t)(sh.sorted[rank] >> 32); }
 
@@ -440,18 +453,16 @@ struct Sampler {
     }
     left = left && !(y < (double)min_p * sc.table[0]);
     if (r < m) {
-      sh.weight[sh.place[r]] = left ? mass : 0;
-      sh.by_place[sh.place[r]] = r;
+      const uint32_t place = (uint32_t)sh.sorted[r];
+      sh.weight[place] = left ? mass : 0;
+      sh.rank[place] = r;
     }
     const uint32_t kept = sm_count(sh, left ? 1u : 0u);      // (its barriers stand behind the weights too)
     const uint64_t mine = r < m ? sh.weight[r] : 0;
     uint64_t all;
     const uint64_t upto = sm_block_scan(sh, mine, &all);
     const double target = goal(all);
-    if (!((double)(upto - mine) > target) && (double)upto > target) {
-      const uint32_t rank = sh.by_place[r];
-      answer((uint32_t)sh.sorted[rank], sm_value(ranked_key(rank)), all, kept);
-    }
+    if (!((double)(upto - mine) > target) && (double)upto > target) answer(sh.number[r], sm_value(ranked_key(sh.rank[r])), all, kept);
   }
 
   // The least key that is left and how many of those equal to it, from the keys' bits: for top-k, or by MASS for top-p of what `least` and `equal` leave so far.
@@ -502,123 +513,110 @@ struct Sampler {
   }
 
   // The token, by walking the row: logits above that of `least` are left, and the first `equal` of those that are equal to it.  The sums of sixteen pieces say on which one the
-  // random number falls, this one's sixteen pieces go on, down to a vector for a lane.
+  // random number falls, this one's sixteen pieces go on, down to a vector for a lane.  The equal ones weigh all the same, so pieces only count them.
   __device__ __forceinline__ void draw_from_row(uint32_t least, uint32_t equal) {
     const float bound = sm_value(least);
-    const double least_mass = (double)min_p * sc.table[0];
-    const bool by_least = min_p > 0.f;
+    const double least_mass = min_p > 0.f ? (double)min_p * sc.table[0] : 0.0, tie = sc.scaled(sc.steps.of(bound));
+    if (tie < least_mass) equal = 0;
+    const uint64_t tie_mass = SampleScale::whole(tie);
     // what is clearly below min-p needs no exponential
     const double cut = min_p > 0.f ? (double)top + (double)temperature * (log((double)min_p) - 1e-6) : -INFINITY;
-    const float near_cut = (float)(cut - fabs(cut) * 1e-6);
-    uint32_t lo = 0, hi = row.vocab, ties_before = 0, kept = 0, won_piece = 0;
+    const float low = fmaxf(sm_value(least + 1), (float)(cut - fabs(cut) * 1e-6));
+    uint32_t lo = 0, hi = row.vocab, ties_before = 0, kept = 0, piece = 0;
     uint64_t before = 0, all = 0;
     double target = 0.0;
     for (bool whole = true;; whole = false) {
       const uint32_t per = ((hi - lo + SM_WAVES - 1) / SM_WAVES + STEP - 1) / STEP * STEP, first = lo + wave * per, end = std::min(first + per, hi);
-      uint32_t seen = ties_before;
-      if (equal != 0) {
-        uint32_t ties = 0;
-        auto count = [&](uint32_t, const Vec& v) {
-#pragma unroll
-          for (uint32_t e = 0; e < N; ++e) ties += v.x[e] == bound ? 1u : 0u;
-        };
-        if (whole) each(count); else row.again(first, end, won_piece, count);
-        ties = sm_sum(ties);
-        if (lane == 0) sh.some[wave] = ties;
-        __syncthreads();
-        for (uint32_t w = 0; w < wave; ++w) seen += sh.some[w];
-        __syncthreads();
-      }
-      const uint32_t seen_first = seen;
       uint64_t sum = 0;
-      uint32_t left = 0;
-      Vec last;                                    // a lane's last vector, what is not left as -inf
-#pragma unroll
-      for (uint32_t e = 0; e < N; ++e) last.x[e] = -INFINITY;
+      uint32_t left = 0, ties = 0;                 // of the wavefront
       auto weigh = [&](uint32_t, const Vec& v) {
-        uint32_t here = 0;
+        uint64_t in[N], some = 0;
 #pragma unroll
-        for (uint32_t e = 0; e < N; ++e) {
-          last.x[e] = v.x[e] > bound && v.x[e] >= near_cut ? v.x[e] : -INFINITY;
-          here += v.x[e] > bound && v.x[e] >= near_cut ? 1u : 0u;
-        }
+        for (uint32_t e = 0; e < N; ++e) some |= in[e] = __ballot(v.x[e] >= low);
         if (equal != 0) {
-          uint32_t mine = 0;
 #pragma unroll
-          for (uint32_t e = 0; e < N; ++e) mine += v.x[e] == bound ? 1u : 0u;
-          if (__any(mine != 0)) {
-            const uint32_t upto = sm_scan(mine);
-            uint32_t rank = seen + upto - mine;
-#pragma unroll
-            for (uint32_t e = 0; e < N; ++e)
-              if (v.x[e] == bound && rank++ < equal) {
-                last.x[e] = bound;
-                ++here;
-              }
-            seen += sm_last(upto);
-          }
+          for (uint32_t e = 0; e < N; ++e) ties += (uint32_t)__popcll(__ballot(v.x[e] == bound));
         }
-        if (!__any(here != 0)) return;
+        if (some == 0) return;
         double y[N];                               // (all of them at once: one by one each would wait for its table entry)
 #pragma unroll
-        for (uint32_t e = 0; e < N; ++e) y[e] = sc.scaled(sc.steps.of(last.x[e]));
-        if (by_least) {
+        for (uint32_t e = 0; e < N; ++e) y[e] = sc.scaled(sc.steps.of(v.x[e] >= low ? v.x[e] : -INFINITY));
+        if (least_mass > 0.0) {
 #pragma unroll
-          for (uint32_t e = 0; e < N; ++e)
-            if (last.x[e] > -INFINITY && y[e] < least_mass) {
-              last.x[e] = -INFINITY;
-              y[e] = 0.0;
-              --here;
-            }
+          for (uint32_t e = 0; e < N; ++e) {
+            in[e] &= __ballot(!(y[e] < least_mass));
+            y[e] = y[e] < least_mass ? 0.0 : y[e];
+          }
         }
 #pragma unroll
-        for (uint32_t e = 0; e < N; ++e) sum += SampleScale::whole(y[e]);
-        left += here;
+        for (uint32_t e = 0; e < N; ++e) {
+          sum += SampleScale::raw(y[e]);
+          left += (uint32_t)__popcll(in[e]);
+        }
+        sum -= N * SampleScale::kRaw;
       };
-      if (whole) each(weigh); else row.again(first, end, won_piece, weigh);
-      const uint64_t upto = sm_scan(sum);
-      if (lane == 63) sh.wave[wave] = upto;
-      const uint32_t here = sm_count(sh, left);
-      uint64_t pieces = before, mine_before = before, won_before = before;
-      uint32_t won = SM_WAVES - 1;
+      if (whole) each(weigh); else row.again(first, end, piece, weigh);
+      sum = sm_scan(sum);
+      if (lane == 63) {
+        sh.wave[wave] = sum;
+        sh.some[wave] = ties;
+        sh.more[wave] = left;
+      }
+      __syncthreads();
+      auto mass_of = [&](uint32_t x, uint32_t seen) { return sh.wave[x] + tie_mass * std::min(sh.some[x], equal - std::min(equal, seen)); };
       if (whole) {
-        kept = here;
-        for (uint32_t x = 0; x < SM_WAVES; ++x) all += sh.wave[x];
+        uint32_t seen = 0;
+        for (uint32_t x = 0; x < SM_WAVES; ++x) {
+          all += mass_of(x, seen);
+          kept += sh.more[x];
+          seen += sh.some[x];
+        }
+        kept += std::min(equal, seen);
         target = goal(all);
       }
-      for (uint32_t x = SM_WAVES; x-- > 0;) pieces += sh.wave[x];
-      for (uint32_t x = SM_WAVES; x-- > 0;) {       // the first piece at whose end the sum exceeds it
-        const uint64_t start = pieces - sh.wave[x];
-        if ((double)pieces > target) { won = x; won_before = start; }
-        if (x == wave) mine_before = start;
-        pieces = start;
-      }
-      if (per == STEP) {
-        if (wave != won) return;
-        const uint64_t hits = __ballot((double)(mine_before + upto) > target);
-        if (lane != (uint32_t)__ffsll((unsigned long long)hits) - 1) return;
-        uint64_t x = mine_before + upto;
-        uint32_t e = N - 1;
-        float l = last.x[N - 1];
-#pragma unroll
-        for (uint32_t z = N; z-- > 0;) {            // the first at which the sum exceeds it, looked at from the last on
-          if ((double)x > target) { e = z; l = last.x[z]; }
-          x -= sc.mass(last.x[z]);
+      uint32_t won = SM_WAVES - 1;                 // the first piece at whose end the sum exceeds it
+      for (uint32_t x = 0; x < SM_WAVES; ++x) {
+        const uint64_t here = mass_of(x, ties_before);
+        if ((double)(before + here) > target) {
+          won = x;
+          break;
         }
-        return answer(first + lane * N + e, l, all, kept);
+        if (x + 1 == SM_WAVES) break;
+        before += here;
+        ties_before += sh.some[x];
       }
-      if (equal != 0) {
-        __syncthreads();
-        if (wave == won && lane == 0) sh.some[0] = seen_first;
-        __syncthreads();
-        ties_before = sh.some[0];
-      }
-      __syncthreads();                             // nobody reads this turn's sums any more
-      before = won_before;
-      if (whole) won_piece = won;
+      if (whole) piece = won;
       lo += won * per;
       hi = std::min(lo + per, hi);
+      if (per == STEP) break;
+      __syncthreads();                             // nobody reads this turn's sums any more
     }
+    if (wave != 0) return;
+    row.again(lo, hi, piece, [&](uint32_t i, const Vec& v) {
+      uint64_t x[N], sum = 0;
+      uint32_t mine = 0;
+#pragma unroll
+      for (uint32_t e = 0; e < N; ++e) mine += v.x[e] == bound ? 1u : 0u;
+      uint32_t rank = ties_before + sm_scan(mine) - mine;
+#pragma unroll
+      for (uint32_t e = 0; e < N; ++e) {
+        const double y = sc.scaled(sc.steps.of(v.x[e]));
+        x[e] = v.x[e] >= low && !(y < least_mass) ? SampleScale::whole(y) : 0;
+        if (v.x[e] == bound && rank++ < equal) x[e] = tie_mass;
+        sum += x[e];
+      }
+      uint64_t at = before + sm_scan(sum);
+      const uint64_t hits = __ballot((double)at > target);
+      if (lane != (uint32_t)__ffsll((unsigned long long)hits) - 1) return;
+      uint32_t e = N - 1;
+      float l = v.x[N - 1];
+#pragma unroll
+      for (uint32_t z = N; z-- > 0;) {              // the first at which the sum exceeds it, looked at from the last on
+        if ((double)at > target) { e = z; l = v.x[z]; }
+        at -= x[z];
+      }
+      answer(i + e, l, all, kept);
+    });
   }
 
   __device__ __forceinline__ void run() {
@@ -675,7 +673,7 @@ struct Sampler {
         sm_find(sh, 0, [&](uint64_t) { return [&](uint64_t sum) { return sum >= (uint64_t)top_k; }; });
         // (the bin's lower end, a little below where it is)
         const double end = (double)top + ((double)((int)sh.bin - (int)(SM_BINS - 1)) * 16.0 - 1.0) / near.per;
-        const uint32_t m = list(sh.bin != 0 ? fmaxf((float)(end - fabs(end) * 1e-6), -3.4028235e38f) : -3.4028235e38f, INFINITY, true);
+        const uint32_t m = list(sh.bin != 0 ? fmaxf((float)(end - fabs(end) * 1e-6), -3.4028235e38f) : -3.4028235e38f, INFINITY);
         if (m <= SM_LIST) return draw_from_list(m, true, 0);
       }
       __syncthreads();
@@ -692,7 +690,7 @@ struct Sampler {
         const uint32_t bin = sh.bin, above = (uint32_t)sh.above, here = (uint32_t)sh.bins[bin];
         const bool whole = above + here <= SM_LIST;
         uint32_t m = SM_LIST + 1;
-        if (whole || here <= SM_LIST) m = list(least_of(near, bin), whole || bin + 1 == SM_BINS ? INFINITY : least_of(near, bin + 1), whole);
+        if (whole || here <= SM_LIST) m = list(least_of(near, bin), whole || bin + 1 == SM_BINS ? INFINITY : least_of(near, bin + 1));
         if (m <= SM_LIST && whole) return draw_from_list(m, true, 0);
         if (m <= SM_LIST) {
           const uint32_t need = (uint32_t)top_k - above;                     // of the listed ones, in their order
@@ -724,7 +722,7 @@ struct Sampler {
       const float low = least_of(sc.steps, bin);
       // (they are counted only where that many of the least possible weight would not make up far more than there is)
       const bool whole = above + sh.bins[bin] <= 16 * SM_LIST * sc.mass(low) && count(low) <= SM_LIST;
-      const uint32_t m = list(low, whole || bin + 1 == SM_BINS ? INFINITY : least_of(sc.steps, bin + 1), whole);
+      const uint32_t m = list(low, whole || bin + 1 == SM_BINS ? INFINITY : least_of(sc.steps, bin + 1));
       if (m <= SM_LIST && whole) return draw_from_list(m, false, all);
       if (m <= SM_LIST) {
         const uint32_t r = threadIdx.x, key = r < m ? ranked_key(r) : kKeyNone;
