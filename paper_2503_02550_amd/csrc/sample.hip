@@ -222,6 +222,9 @@ __device__ __forceinline__ T sm_scan(T x) {
   return x;
 }
 __device__ __forceinline__ uint32_t sm_last(uint32_t x) { return (uint32_t)__builtin_amdgcn_readlane((int)x, 63); }
+__device__ __forceinline__ uint64_t sm_lane(uint64_t x, uint32_t l) {
+  return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(x >> 32), (int)l) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)x, (int)l);
+}
 __device__ __forceinline__ uint32_t sm_sum(uint32_t x) { return sm_last(sm_scan(x)); }
 
 struct SampleShared {
@@ -322,13 +325,21 @@ struct Sampler {
   }
   __device__ __forceinline__ double share(uint64_t all) const { return fmax((double)top_p * (double)all, 0.5); }      // what top-p asks for; at least one token
 
-  // The least logit (no -inf) whose bin is `bin` or above: a search among the numbers, 64 at a time.
+  // The least logit (no -inf) whose bin is `bin` or above.  It lies next to the bin's lower end: 64 numbers there are looked at, and where it is not among them (large logits
+  // and temperatures) all numbers, 64 at a time.
   __device__ __forceinline__ float least_of(const SampleSteps& steps, uint32_t bin) const {
+    auto reaches = [&](uint32_t key) { return SampleSteps::bin(steps.of(sm_value(key)).n) >= bin; };
     uint32_t lo = kKeyNone, hi = sm_key(top);      // hi's bin is the highest one, lo's (if any) is not asked for
+    const float end = (float)(steps.top + ((double)((int)(bin - (SM_BINS - 1)) * 16) - 0.5) / steps.per);
+    const uint32_t near_end = sm_key(fminf(fmaxf(end, -3.4028235e38f), top));
+    if (near_end > lo + 64 && near_end < hi - 64) {
+      const uint64_t f = __ballot(reaches(near_end - 32 + lane));
+      if ((f & 1) == 0 && f != 0) return sm_value(near_end - 32 + (uint32_t)__ffsll((unsigned long long)f) - 1);
+    }
     while (hi - lo > 1) {
       const uint64_t step = ((uint64_t)(hi - lo) + 63) / 64, size = hi - lo;
       const uint32_t at = lo + (uint32_t)std::min(step * (lane + 1), size);
-      const int f = __ffsll((unsigned long long)__ballot(SampleSteps::bin(steps.of(sm_value(at)).n) >= bin)) - 1;
+      const int f = __ffsll((unsigned long long)__ballot(reaches(at))) - 1;
       hi = lo + (uint32_t)std::min(step * (uint64_t)(f + 1), size);
       lo += (uint32_t)(step * (uint64_t)f);
     }
@@ -563,28 +574,19 @@ struct Sampler {
         sh.more[wave] = left;
       }
       __syncthreads();
-      auto mass_of = [&](uint32_t x, uint32_t seen) { return sh.wave[x] + tie_mass * std::min(sh.some[x], equal - std::min(equal, seen)); };
+      // the first piece at whose end the sum exceeds the target, a piece to a lane
+      const bool mine = lane < SM_WAVES;
+      const uint32_t equals = mine ? sh.some[lane] : 0, seen = ties_before + sm_scan(equals) - equals;
+      const uint64_t here = mine ? sh.wave[lane] + tie_mass * std::min(equals, equal - std::min(equal, seen)) : 0, upto = before + sm_scan(here);
       if (whole) {
-        uint32_t seen = 0;
-        for (uint32_t x = 0; x < SM_WAVES; ++x) {
-          all += mass_of(x, seen);
-          kept += sh.more[x];
-          seen += sh.some[x];
-        }
-        kept += std::min(equal, seen);
+        all = sm_lane(upto, 63);
+        kept = sm_sum(mine ? sh.more[lane] : 0) + std::min(equal, (uint32_t)__builtin_amdgcn_readlane((int)(seen + equals), 63));
         target = goal(all);
       }
-      uint32_t won = SM_WAVES - 1;                 // the first piece at whose end the sum exceeds it
-      for (uint32_t x = 0; x < SM_WAVES; ++x) {
-        const uint64_t here = mass_of(x, ties_before);
-        if ((double)(before + here) > target) {
-          won = x;
-          break;
-        }
-        if (x + 1 == SM_WAVES) break;
-        before += here;
-        ties_before += sh.some[x];
-      }
+      const uint64_t beyond = __ballot(mine && (double)upto > target);
+      const uint32_t won = beyond != 0 ? (uint32_t)__ffsll((unsigned long long)beyond) - 1 : SM_WAVES - 1;
+      before = sm_lane(upto - here, won);
+      ties_before = (uint32_t)__builtin_amdgcn_readlane((int)seen, (int)won);
       if (whole) piece = won;
       lo += won * per;
       hi = std::min(lo + per, hi);
