@@ -528,7 +528,7 @@ sif_status sif_k_xent_fwd_bwd(void* logits_dev, const int32_t* targets_dev, floa
  *   min_p > 0      those at least min_p (held to 1) times as probable as the most probable one
  * and the token is the first, in the order of their numbers, at which the sum of the probabilities exceeds random (held to 0 .. 1 - 2^-24, NaN counts as 0) times that of all that are
  * left.  A temperature that is not above 0: the largest logit's token, of equal ones the lowest number.
- * Probabilities are taken in 64 bits and added as integers of at least 2^-44 of the largest one, so the answer does not depend on the order of additions.  A row without a token gets -1.
+ * Probabilities are taken in 64 bits and added as integers of at most 2^-44 of the largest one (less than half of that is nothing), so the answer does not depend on the order of additions.  A row without a token gets -1.
  * kept: how many tokens were left (1 where the temperature is not above 0); logprob: the log of the token's share of their sum (-inf for no token). */
 typedef struct sif_sample_args {
   uint32_t struct_size;

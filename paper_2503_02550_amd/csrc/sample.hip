@@ -325,6 +325,20 @@ struct Sampler {
   }
   __device__ __forceinline__ double share(uint64_t all) const { return fmax((double)top_p * (double)all, 0.5); }      // what top-p asks for; at least one token
 
+  // Min-p: what is left has at least this logit, which lies a little below the limit (what is clearly below it needs no exponential), and at least this mass.  A limit below those that
+  // masses are told from nothing by is one of the logit alone.
+  struct MinP { double mass; float logit; };
+  __device__ __forceinline__ MinP limit() const {
+    if (!(min_p > 0.f)) return {0.0, -INFINITY};
+    if (min_p >= 0x1p-60f) {
+      const double below = (double)top + (double)temperature * (log((double)min_p) - 1e-6);
+      return {(double)min_p * sc.table[0], (float)(below - fabs(below) * 1e-6)};
+    }
+    const double cut = (double)top + (double)temperature * log((double)min_p);
+    const float f = (float)cut;
+    return {0.0, (double)f < cut ? sm_value(sm_key(f) + 1) : f};
+  }
+
   // The least logit (no -inf) whose bin is `bin` or above.  It lies next to the bin's lower end: 64 numbers there are looked at, and where it is not among them (large logits
   // and temperatures) all numbers, 64 at a time.
   __device__ __forceinline__ float least_of(const SampleSteps& steps, uint32_t bin) const {
@@ -462,7 +476,8 @@ struct Sampler {
       const uint64_t upto = sm_block_scan(sh, left ? mass : 0, &all);
       left = left && (double)(upto - mass) < share(by_k ? all : whole_sum);
     }
-    left = left && !(y < (double)min_p * sc.table[0]);
+    const MinP min = limit();
+    left = left && !(y < min.mass) && sm_value(ranked_key(r)) >= min.logit;
     if (r < m) {
       const uint32_t place = (uint32_t)sh.sorted[r];
       sh.weight[place] = left ? mass : 0;
@@ -527,12 +542,11 @@ struct Sampler {
   // random number falls, this one's sixteen pieces go on, down to a vector for a lane.  The equal ones weigh all the same, so pieces only count them.
   __device__ __forceinline__ void draw_from_row(uint32_t least, uint32_t equal) {
     const float bound = sm_value(least);
-    const double least_mass = min_p > 0.f ? (double)min_p * sc.table[0] : 0.0, tie = sc.scaled(sc.steps.of(bound));
-    if (tie < least_mass) equal = 0;
+    const MinP min = limit();
+    const double least_mass = min.mass, tie = sc.scaled(sc.steps.of(bound));
+    if (tie < least_mass || bound < min.logit) equal = 0;
     const uint64_t tie_mass = SampleScale::whole(tie);
-    // what is clearly below min-p needs no exponential
-    const double cut = min_p > 0.f ? (double)top + (double)temperature * (log((double)min_p) - 1e-6) : -INFINITY;
-    const float low = fmaxf(sm_value(least + 1), (float)(cut - fabs(cut) * 1e-6));
+    const float low = fmaxf(sm_value(least + 1), min.logit);
     uint32_t lo = 0, hi = row.vocab, ties_before = 0, kept = 0, piece = 0;
     uint64_t before = 0, all = 0;
     double target = 0.0;
@@ -673,9 +687,9 @@ struct Sampler {
         if (mine > -INFINITY) sm_add(sh, SampleSteps::bin(near.of(mine).n), 1);
         __syncthreads();
         sm_find(sh, 0, [&](uint64_t) { return [&](uint64_t sum) { return sum >= (uint64_t)top_k; }; });
-        // (the bin's lower end, a little below where it is)
+        // (the bin's lower end, a little below where it is; the first one also holds all that is further away)
         const double end = (double)top + ((double)((int)sh.bin - (int)(SM_BINS - 1)) * 16.0 - 1.0) / near.per;
-        const uint32_t m = list(sh.bin != 0 ? fmaxf((float)(end - fabs(end) * 1e-6), -3.4028235e38f) : -3.4028235e38f, INFINITY);
+        const uint32_t m = list(sh.bin > 1 ? fmaxf((float)(end - fabs(end) * 1e-6), -3.4028235e38f) : -3.4028235e38f, INFINITY);
         if (m <= SM_LIST) return draw_from_list(m, true, 0);
       }
       __syncthreads();
@@ -723,7 +737,7 @@ struct Sampler {
       const uint64_t above = sh.above;
       const float low = least_of(sc.steps, bin);
       // (they are counted only where that many of the least possible weight would not make up far more than there is)
-      const bool whole = above + sh.bins[bin] <= 16 * SM_LIST * sc.mass(low) && count(low) <= SM_LIST;
+      const bool whole = (above + sh.bins[bin]) / (16 * SM_LIST) <= sc.mass(low) && count(low) <= SM_LIST;
       const uint32_t m = list(low, whole || bin + 1 == SM_BINS ? INFINITY : least_of(sc.steps, bin + 1));
       if (m <= SM_LIST && whole) return draw_from_list(m, false, all);
       if (m <= SM_LIST) {
@@ -784,7 +798,7 @@ sif_status sif_k_sample(const sif_sample_args* a, void* stream) {
   x.vocab = a->vocab;
   x.ld = a->ld;
   x.shift = 51;
-  while ((uint64_t)a->vocab << x.shift > 1ull << 62) --x.shift;
+  while (1ull << (62 - x.shift) < a->vocab) --x.shift;
   x.temperature = a->temperature;
   x.top_k = a->top_k;
   x.top_p = a->top_p;

@@ -178,8 +178,10 @@ def sample(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
         order, w = order[:n], w[:n]
     left = sorted(zip(order, w))
     goal, total = min(max(u, 0.0) if u == u else 0.0, 1 - 2.0 ** -24) * w.sum(), 0.0
+    # the sums are of whole numbers w 2^s, s the largest up to 51 with which `vocab` of them stay within 2^62: less than half of one is nothing, which shows at u = 0
+    least = 2.0 ** -(1 + min(51, 62 - math.ceil(math.log2(len(x)))))
     for i, share in left:
-        total += share
+        total += share if share > least else 0.0
         if total > goal:
             return i, math.log(share / w.sum()) if share > 0 else -math.inf, len(left)
     raise AssertionError("no token")

@@ -115,6 +115,12 @@ def test_numbers_at_their_ends():
     assert off == _run(x, 777, [0.5] * 12)
     hot = _run(x, 777, [0.5] * 12, temperature=[math.inf] * 12)
     assert hot[0] == [388] * 12 and hot[2] == [777] * 12
+    assert _run(x, 777, [0.5] * 12, temperature=[math.inf] * 12, min_p=1.0)[0] == [388] * 12
+    y = torch.zeros(4, 777)
+    y[:, ::3], y[:, 1::3] = -80.0, -43.0                   # probabilities of 2^-115 and 2^-62
+    _check(y, [0.1, 0.4, 0.7, 0.99], min_p=[1e-34, 1e-36, 1e-18, 1e-19])
+    _check(y, [0.1, 0.4, 0.7, 0.99], min_p=[1e-34, 1e-36, 1e-18, 1e-19], top_k=500)
+    _check(y, [0.1, 0.4, 0.7, 0.99], min_p=[1e-34, 1e-36, 1e-18, 1e-19], top_k=600, top_p=0.9)
 
 
 def test_tokens_follow_the_random_number():
@@ -136,6 +142,84 @@ def test_only_a_token_is_asked_for():
     assert torch.equal(a, b)
     S.sif_k_sample(S.sample_args(x, a, 3, 1000, temperature=0.0))
     assert a.cpu().tolist() == x.float().argmax(1).cpu().tolist()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
+def test_tokens_far_below_the_largest(dtype):
+    """Some tokens far above the others, whose probabilities are nothing beside theirs: they count among what is left all the same."""
+    for vocab in (900, 20000):
+        x = _logits(10, 8, vocab, dtype, 1.0)
+        x[:, 123], x[4:, 7] = 1000.0, 900.0
+        u = [0.0, 0.3, 0.6, 0.99] * 2
+        for kw in (dict(top_k=50), dict(top_k=3), dict(top_k=600), dict(top_k=50, min_p=1e-30), dict(top_k=50, top_p=0.9), dict(temperature=30.0, top_k=40), dict(temperature=400.0, top_k=300, top_p=0.8), dict(top_p=0.5)):
+            _check(x, u, **kw)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("vocab", [5003, 70000])
+def test_many_equal_logits(vocab, dtype):
+    """More equal ones than a list holds, on both sides of the border and in all parts of the row."""
+    n = 12
+    u = [(i + 0.5) / n for i in range(n)]
+    zeros = torch.zeros(n, vocab, dtype=dtype)
+    _check(zeros, u, top_k=[1, 63, 512, 513, 1024, 1025, 3000, vocab - 1, vocab, 2049, 4096, 0])
+    _check(zeros, u, top_p=[0.5, 0.001, 0.999, 0.25, 1e-6, 0.75, 0.1, 0.9, 0.3, 0.6, 0.05, 0.8])
+    few = torch.randint(0, 4, (n, vocab), generator=torch.Generator().manual_seed(12)).to(dtype)
+    few[6:, vocab // 3:] = few[6:, vocab // 3:].clamp(max=1)      # the most probable ones at the row's start
+    _check(few, u, top_k=[vocab // 3 + 17 * i for i in range(n)])
+    _check(few, u, top_p=[0.4 + 0.05 * i for i in range(n)])
+    _check(few, u, top_k=vocab // 2, top_p=[0.3 + 0.05 * i for i in range(n)], min_p=[0.0, 0.04, 0.05, 0.1, 0.13, 0.14, 0.3, 0.36, 0.37, 0.5, 1.0, 0.01])
+    _check(few, u, top_k=2000, min_p=0.2)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("descending", [False, True])
+def test_rows_in_order(descending, dtype):
+    """All that is left lies in one part of the row."""
+    n, vocab = 10, 60001
+    x = _logits(13, n, vocab, dtype, 2.0).sort(1, descending=descending)[0]
+    u = [(i + 0.5) / n for i in range(n)]
+    for kw in (dict(top_k=[1, 30, 100, 255, 257, 500, 512, 513, 900, 1100]), dict(top_p=0.02), dict(top_p=0.9), dict(top_p=0.6, temperature=0.5), dict(min_p=0.05), dict(top_k=30000, top_p=0.7, min_p=0.001), dict()):
+        _check(x, u, **kw)
+
+
+def test_logits_large_and_small_over_long_rows():
+    """Steps of the logit far finer and far coarser than the numbers."""
+    n, vocab = 9, 6007
+    x = _logits(14, n, vocab, torch.float32, 2.0)
+    u = [(i + 0.37) / n for i in range(n)]
+    t = [1e-3, 0.03, 1.0, 1e2, 1e5, 1e9, 1e-8, 1e30, 0.3]
+    for scale in (1e-30, 1e-4, 1.0, 1e4):
+        for kw in (dict(top_p=0.5), dict(top_k=600), dict(top_k=40), dict(top_k=3000, top_p=0.7), dict(min_p=0.3)):
+            _check(x * scale, u, temperature=t, **kw)
+
+
+def test_rows_at_once_on_streams_and_in_a_graph():
+    """Two calls under way at the same time, and a captured one whose numbers change between replays."""
+    n, vocab = 40, 20000
+    x, y = _logits(15, n, vocab, torch.bfloat16).to(DEV), _logits(16, n, vocab, torch.float32).to(DEV)
+    u = torch.rand(n, generator=torch.Generator().manual_seed(17)).to(DEV)
+    out = [torch.zeros(n, dtype=torch.int32, device=DEV) for _ in range(4)]
+    S.sif_k_sample(S.sample_args(x, out[0], n, vocab, random=u, top_p=0.9))
+    S.sif_k_sample(S.sample_args(y, out[1], n, vocab, random=u, top_k=300))
+    torch.cuda.synchronize()
+    one, two = torch.cuda.Stream(), torch.cuda.Stream()
+    for _ in range(5):
+        out[2].zero_(), out[3].zero_()
+        torch.cuda.synchronize()
+        S.sif_k_sample(S.sample_args(x, out[2], n, vocab, random=u, top_p=0.9), stream=one)
+        S.sif_k_sample(S.sample_args(y, out[3], n, vocab, random=u, top_k=300), stream=two)
+        torch.cuda.synchronize()
+        assert torch.equal(out[0], out[2]) and torch.equal(out[1], out[3])
+    graph, v = torch.cuda.CUDAGraph(), u.clone()
+    with torch.cuda.graph(graph):
+        S.sif_k_sample(S.sample_args(x, out[2], n, vocab, random=v, top_p=0.9), stream=torch.cuda.current_stream())
+    for turn in range(4):
+        v.copy_((u + 0.21 * turn) % 1.0)
+        graph.replay()
+        S.sif_k_sample(S.sample_args(x, out[0], n, vocab, random=v, top_p=0.9))
+        torch.cuda.synchronize()
+        assert torch.equal(out[0], out[2])
 
 
 def test_rows_past_32_bits():
