@@ -140,6 +140,34 @@ def test_a_captured_step_goes_on_by_itself():
         assert torch.equal(rows.t[name], eager.rows.t[name]), name
 
 
+def test_two_programs_at_once():
+    """Steps of two programs under way at the same time, on streams, caches and workspaces of their own."""
+    def start(seed):
+        return Step(_rows(seed), 6, 304, 20 + seed, 4)
+
+    def numbers(seed):
+        return [torch.rand(4, generator=torch.Generator().manual_seed(100 * seed + t)).to(DEV) for t in range(10)]
+    want = {}
+    for seed in (3, 4):
+        s = start(seed)
+        for u in numbers(seed):
+            s.random.copy_(u)
+            s.run()
+        want[seed] = [x.clone() for x in (s.token, s.logprob, s.o, s.rows.t["k"], s.rows.t["v"], s.rows.t["lengths"], s.rows.t["table"])]
+    both, streams = [start(3), start(4)], [torch.cuda.Stream(), torch.cuda.Stream()]
+    given = [numbers(3), numbers(4)]
+    torch.cuda.synchronize()
+    for t in range(10):
+        for s, stream, u in zip(both, streams, given):
+            with torch.cuda.stream(stream):
+                s.random.copy_(u[t])
+                s.run(stream)
+    torch.cuda.synchronize()
+    for seed, s in zip((3, 4), both):
+        for a, b in zip((s.token, s.logprob, s.o, s.rows.t["k"], s.rows.t["v"], s.rows.t["lengths"], s.rows.t["table"]), want[seed]):
+            assert torch.equal(a, b), seed
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "e4m3", "e2m1"])
 def test_a_prompt_in_pieces(dtype):
     """The next piece of a prompt attends to what the cache holds of the earlier ones: written, read back as rows, windowed attention over them."""

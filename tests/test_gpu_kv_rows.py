@@ -183,6 +183,75 @@ def test_reading_back(dtype, d, kv, page):
         rows.check("untouched")
 
 
+@pytest.mark.parametrize("dtype", FORMATS)
+def test_as_many_heads_as_there_may_be(dtype):
+    rows = Rows(dtype, [3, 18], 16, 1024, 64, layers=2, seed=21)
+    _append(rows, 1, 1024, None, [0, 2, 3], 2, 3, 64)
+    rows = Rows(dtype, [1], 16, 1, 64, seed=22)
+    _append(rows, 0, 1024, None, None, 1, 1, 16, True, there=True)
+
+
+@pytest.mark.parametrize("dtype", FORMATS)
+def test_lists_as_long_as_they_may_be(dtype):
+    """One call with 16384 entries, of which some are unknown or listed before, leaves what calls with 512 of them and without those leave; so too reading back, where sequences may be listed again."""
+    n, page, d, heads, g = 16384, 16, 64, 2, torch.Generator().manual_seed(23)
+    lens = torch.randint(2, 33, (n,), generator=g).int()
+    table = torch.randperm(2 * n, generator=g).int().view(n, 2)
+    table = torch.where(lens[:, None] > torch.tensor([0, page]), table, -1)
+    seqs = torch.randperm(n, generator=g).int()
+    seqs[16000], seqs[16383], seqs[700], seqs[9000], seqs[12345] = seqs[3], seqs[16382], seqs[699], -1, n
+    count = torch.randint(0, 3, (n,), generator=g)
+    count[[3, 16000, 16382, 16383, 699, 700, 9000, 12345]] = 2
+    starts = torch.cat([torch.zeros(1, dtype=torch.long), count.cumsum(0)]).int() + 5
+    rows = int(starts[-1]) + 3
+    q, k, v = (_x(24 + i, rows, w).to(DEV) for i, w in enumerate((heads * d, d, d)))
+    rope = S.rope_plan(d)
+    kind = {"bf16": S.SIF_BF16, "e4m3": S.SIF_E4M3, "e2m1": S.SIF_E2M1}[dtype]
+
+    def pool(*shape):
+        of = {"bf16": (shape, torch.bfloat16), "e4m3": (shape, torch.uint8), "e2m1": (shape[:3] + (page * d * 17 // 32,), torch.uint8)}[dtype]
+        return torch.zeros(of[0], dtype=of[1], device=DEV)
+    held = []
+    for _ in range(2):
+        kp, vp = pool(1, 2 * n, 1, page, d), pool(1, 2 * n, 1, d, page)
+        t = (kp, vp, table.to(DEV), lens.to(DEV), torch.ones(2 * n, dtype=torch.int32, device=DEV))
+        held.append((t, S.kv_cache(*t, kind, page), torch.full_like(q, 7.0)))
+    listed, at = seqs.to(DEV), starts.to(DEV)
+    S.sif_k_kv_append(held[0][1], rope, S.kv_append_args(k, v, n, rows=rows, seqs=listed, starts=at, q=q, q_out=held[0][2], heads=heads))
+    first = {}
+    again = torch.zeros(n, dtype=torch.bool)
+    for i, s in enumerate(seqs.tolist()):
+        again[i] = s in first
+        first[s] = i
+    assert int(again.sum()) == 3
+    alone = torch.where(again, -1, seqs).to(DEV)
+    for lo in range(0, n, 512):
+        a, b = int(starts[lo]), int(starts[lo + 512])
+        S.sif_k_kv_append(held[1][1], rope, S.kv_append_args(k[a:], v[a:], 512, rows=b - a, seqs=alone[lo:lo + 512], starts=at[lo:lo + 513] - a, q=q[a:], q_out=held[1][2][a:], heads=heads))
+    torch.cuda.synchronize()
+    for x, y in zip(held[0][0], held[1][0]):
+        assert torch.equal(x, y)
+    twice = torch.zeros(rows, dtype=torch.bool)
+    for i in again.nonzero().flatten().tolist():
+        twice[int(starts[i]):int(starts[i + 1])] = True
+    assert int(twice.sum()) == 6 and torch.equal(held[0][2][~twice.to(DEV)], held[1][2][~twice.to(DEV)])
+    assert not bool((held[0][2][twice.to(DEV)] == 7.0).any()) and bool((held[0][2][:5] == 7.0).all()) and bool((held[0][2][rows - 3:] == 7.0).all())
+    out = [torch.full((rows, d), 5.0, dtype=torch.bfloat16, device=DEV) for _ in range(4)]
+    S.sif_k_kv_read(held[0][1], 0, out[0], out[1], listed, n, starts=at, rows=rows)
+    for lo in range(0, n, 512):
+        a, b = int(starts[lo]), int(starts[lo + 512])
+        S.sif_k_kv_read(held[0][1], 0, out[2][a:], out[3][a:], listed[lo:lo + 512], 512, starts=at[lo:lo + 513] - a, rows=b - a)
+    torch.cuda.synchronize()
+    assert torch.equal(out[0], out[2]) and torch.equal(out[1], out[3])
+    # (values come back as they were written: in bf16 the same, of sequences that are listed once)
+    if dtype == "bf16":
+        known = torch.zeros(rows, dtype=torch.bool)
+        for i in range(n):
+            if 0 <= int(seqs[i]) < n and not again[i]:
+                known[int(starts[i]):int(starts[i + 1])] = True
+        assert torch.equal(out[1][known.to(DEV)], v[known.to(DEV)])
+
+
 def test_4_bit_pages_are_copied_whole():
     """Forking, extending, copying and compacting move powers along with what they belong to."""
     rows = Rows("e2m1", [20, 70, 0, 0], 32, 3, 64, layers=2, seed=10, spare=5, wider=2)
