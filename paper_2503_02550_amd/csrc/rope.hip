@@ -1,5 +1,6 @@
 // Rotary positions of rows of query and key heads, forward and back.  Every element is read and written once and costs three operations, so
-// the memory's rate is the bound; what could get in the way are the sines: a block takes them once for its rows and all their heads.
+// the memory's rate is the bound; what could get in the way are the sines: a block takes them once for its rows and all their heads.  671 MB take 119 us, 5.6 TB/s, a plain copy
+// 5.1; 50 MB 13; a few rows 3.4, the launch.
 #include <algorithm>
 
 #include "rope.h"
@@ -32,12 +33,14 @@ struct RopeArgs {
   uint32_t rows, heads, all_heads, d_head, seq, ld_q, ld_q_out, ld_k, ld_k_out;
   int32_t first;
   float back;
-  uint32_t units, slots, tile;       // eight pairs each of a head; heads a block takes at once; rows it takes at once
-  uint32_t copy_q, copy_k;           // vectors of eight elements behind the rotated ones, where results do not take their operands' place
+  uint32_t units, slots, tile;       // sixteen elements each of a head; heads a block takes at once; rows it takes at once
+  uint32_t copies;                   // of the units, those of elements behind the rotated ones, where results do not take their operands' place
+  bool copy_q, copy_k;
 };
 
-// Sixteen elements (eight pairs) of a head and row to a thread, two 16-byte vectors in, two out: consecutive threads take a head's units, then
-// the next heads', which lie next to it in memory, then the next row's.
+// Sixteen elements of a head and row to a thread, eight pairs or what stands behind the rotated ones, two 16-byte vectors in, two out: consecutive threads take a head's units,
+// then the next heads', which lie next to it in memory, then the next row's.  (With the elements behind left to the threads that turn, 32768 rows of 16 heads of 128 of which 16 elements are
+// turned took 210 us, 32 elements 98, all of them 52.)
 __global__ __launch_bounds__(256) void rope_kernel(RopeView r, RopeArgs a) {
   __shared__ __align__(16) CosSin<float> s_cs[2048];      // [row][pair]
   const uint32_t tid = threadIdx.x, unit = tid % a.units, slot = tid / a.units % a.slots, row = tid / (a.units * a.slots);
@@ -55,21 +58,29 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeView r, RopeArgs a) {
     __syncthreads();
     const uint32_t at = row0 + row;
     if (row >= a.tile || at >= a.rows) continue;
+    const uint32_t turning = a.units - a.copies;
+    const bool turns = unit < turning;
     CosSin<float> cs[8];
+    uint32_t x, y;
+    if (turns) {
 #pragma unroll
-    for (uint32_t e = 0; e < 8; e += 2) *reinterpret_cast<float4*>(&cs[e]) = *reinterpret_cast<const float4*>(&s_cs[row * r.half + unit * 8 + e]);
-    const uint32_t x = r.interleaved ? unit * 16 : unit * 8, y = r.interleaved ? x + 8 : x + r.half;
+      for (uint32_t e = 0; e < 8; e += 2) *reinterpret_cast<float4*>(&cs[e]) = *reinterpret_cast<const float4*>(&s_cs[row * r.half + unit * 8 + e]);
+      x = r.interleaved ? unit * 16 : unit * 8;
+      y = r.interleaved ? x + 8 : x + r.half;
+    } else {
+      x = 2 * r.half + (unit - turning) * 8;
+      y = x + a.copies * 8 < a.d_head ? x + a.copies * 8 : x;      // (of an odd number the last one twice)
+    }
     for (uint32_t h = blockIdx.y * a.slots + slot; h < a.all_heads; h += gridDim.y * a.slots) {
       const bool of_q = h < a.heads;
+      if (!turns && !(of_q ? a.copy_q : a.copy_k)) continue;
       const uint32_t c = (of_q ? h : h - a.heads) * a.d_head;
       const bf16_t* from = of_q ? a.q + (size_t)at * a.ld_q + c : a.k + (size_t)at * a.ld_k + c;
       bf16_t* to = of_q ? a.q_out + (size_t)at * a.ld_q_out + c : a.k_out + (size_t)at * a.ld_k_out + c;
       uint4 u = *reinterpret_cast<const uint4*>(from + x), v = *reinterpret_cast<const uint4*>(from + y);
-      rope_turn8(r.interleaved, cs, a.back, u, v);
+      if (turns) rope_turn8(r.interleaved, cs, a.back, u, v);
       *reinterpret_cast<uint4*>(to + x) = u;
       *reinterpret_cast<uint4*>(to + y) = v;
-      for (uint32_t e = unit; e < (of_q ? a.copy_q : a.copy_k); e += a.units)
-        *reinterpret_cast<uint4*>(to + 2 * r.half + e * 8) = *reinterpret_cast<const uint4*>(from + 2 * r.half + e * 8);
     }
   }
 }
@@ -148,10 +159,12 @@ sif_status sif_k_rope(const sif_rope* rope, const sif_rope_args* a, void* stream
   x.ld_q_out = a->ld_q_out;
   x.ld_k = a->ld_k;
   x.ld_k_out = a->ld_k_out;
-  const uint32_t rest = (a->d_head - 2 * v.half) / 8;
-  x.copy_q = q_there ? 0 : rest;
-  x.copy_k = k_there ? 0 : rest;
-  x.units = v.half / 8;                            // 1 .. 16
+  x.copy_q = !q_there;
+  x.copy_k = !k_there;
+  x.copies = q_there && (k_there || !a->kv_heads) ? 0 : ((a->d_head - 2 * v.half) / 8 + 1) / 2;
+  x.units = v.half / 8 + x.copies;                 // 1 .. 16
+  // Two rows or more to a block, and as many heads as that leaves: they lie next to each other in its loads, and each row's sines serve them all.  (Rows to a block at least 1, 2, 4, 8: 32762 rows of
+  // 40 heads of 128, half of each turned 124, 120, 125, 130 us; 16384 of 16 heads of 256 50 to 53, 49 to 51, 51, 54; 52428 of 16 heads of 80, where two rows fill 240 to 250 of a block's threads and four 192 or 200, 51, 51, 56, 54.)
   x.slots = std::min(x.all_heads, 256 / x.units / 2);
   x.tile = 256 / (x.units * x.slots);
   x.tile = std::min(x.tile, 2048 / v.half);        // the table's size

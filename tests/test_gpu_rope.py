@@ -61,6 +61,19 @@ def test_rows_of_heads(rows, heads, kv, d, rot, inter):
                     assert torch.equal(ok[:, :k.shape[1]].cpu(), k if there else torch.zeros_like(k))
 
 
+@pytest.mark.parametrize("d,rot", [(40, 16), (256, 16), (128, 48), (64, 64)])
+def test_one_in_place_and_one_not(d, rot):
+    rows, heads, kv = 37, 3, 2
+    f, rope, pos = frequencies(rot), S.rope_plan(rot), torch.arange(rows)
+    q, k = _x(4, rows, heads * d), _x(5, rows, kv * d)
+    for q_there in (False, True):
+        wq, wk = _wide(q), _wide(k, 16)
+        oq, ok = (wq, _wide(torch.zeros_like(k))) if q_there else (_wide(torch.zeros_like(q), 24), wk)
+        S.sif_k_rope(rope, S.rope_args(wq, oq, rows, heads, d, k=wk, k_out=ok, kv_heads=kv, seq=rows))
+        _check(oq, q, pos, f, heads, d, False, 1.0, False, ("q", q_there))
+        _check(ok, k, pos, f, kv, d, False, 1.0, False, ("k", q_there))
+
+
 @pytest.mark.parametrize("kw", [dict(scaling="linear", factor=4.0), dict(scaling="base", factor=8.0), dict(scaling="parts", factor=32.0, trained=4096.0)], ids=str)
 def test_scaled_frequencies(kw):
     how = {"linear": "SIF_ROPE_LINEAR", "base": "SIF_ROPE_BASE", "parts": "SIF_ROPE_PARTS"}[kw["scaling"]]
