@@ -221,20 +221,47 @@ __global__ __launch_bounds__(256) void attn_decode_join_kernel(DecodeArgs a) {
   // Everything that is known only on the device - how many splits the sequence has - stands in the splits themselves: the first
   // `parts` have an l, the others kNoSplit (all of them if one block did the whole sequence).  So there are two rounds of loads, and not the
   // length's and the list's before them.
-  float2 ml = make_float2(-INFINITY, kNoSplit);
-  if (t < a.splits) ml = *reinterpret_cast<const float2*>(from + (size_t)t * (DH + 4));
-  const bool here = ml.y != kNoSplit;
-  const uint32_t parts = (uint32_t)block_sum(here ? 1.f : 0.f, sm);
-  if (parts == 0) return;
-  const float m = block_max(here ? ml.x : -INFINITY, sm), w = here && m != -INFINITY ? __builtin_amdgcn_exp2f(ml.x - m) : 0.f;
-  s_w[t] = w;
-  const float l = block_sum(here ? w * ml.y : 0.f, sm);      // (its barriers stand behind the weights too)
   float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+  float m, l;
+  if (a.splits <= 64) {
+    // A split per lane, in every wavefront: no barriers, and the splits' rows on their way beside the sums (of splits that are none too: anything, not looked at).  The same operations in the same order as
+    // below.  (One sequence in 4 bits, heads of 128, the whole call: 1000 tokens 10.6 -> 8.3 us, 100000 27.9 -> 25.3; 64 of 1 to 8192 75 -> 74.)
+    const uint32_t lane = t & 63, first = t / LANES;
+    float2 ml = make_float2(-INFINITY, kNoSplit);
+    if (lane < a.splits) ml = *reinterpret_cast<const float2*>(from + (size_t)lane * (DH + 4));
+    float4 v[64 / ROWS];
+#pragma unroll
+    for (uint32_t round = 0; round < 64 / ROWS; ++round)
+      if (round * ROWS < a.splits) v[round] = *reinterpret_cast<const float4*>(from + (size_t)std::min(round * ROWS + first, a.splits - 1) * (DH + 4) + 4 + t % LANES * 4);
+    const bool here = ml.y != kNoSplit;
+    const uint32_t parts = (uint32_t)__popcll(__ballot(here));
+    if (parts == 0) return;
+    m = wave_max(here ? ml.x : -INFINITY);
+    const float w = here && m != -INFINITY ? __builtin_amdgcn_exp2f(ml.x - m) : 0.f;
+    l = wave_sum(here ? w * ml.y : 0.f);
+#pragma unroll
+    for (uint32_t round = 0; round < 64 / ROWS; ++round)
+      if (round * ROWS < parts) {
+        const uint32_t p = round * ROWS + first;
+        const float f = __shfl(w, p, 64);
+        if (p < parts) { y.x += f * v[round].x; y.y += f * v[round].y; y.z += f * v[round].z; y.w += f * v[round].w; }
+      }
+  } else {
+    float2 ml = make_float2(-INFINITY, kNoSplit);
+    if (t < a.splits) ml = *reinterpret_cast<const float2*>(from + (size_t)t * (DH + 4));
+    const bool here = ml.y != kNoSplit;
+    const uint32_t parts = (uint32_t)block_sum(here ? 1.f : 0.f, sm);
+    if (parts == 0) return;
+    m = block_max(here ? ml.x : -INFINITY, sm);
+    const float w = here && m != -INFINITY ? __builtin_amdgcn_exp2f(ml.x - m) : 0.f;
+    s_w[t] = w;
+    l = block_sum(here ? w * ml.y : 0.f, sm);      // (its barriers stand behind the weights too)
 #pragma unroll 8
-  for (uint32_t p = t / LANES; p < parts; p += ROWS) {
-    const float4 v = *reinterpret_cast<const float4*>(from + (size_t)p * (DH + 4) + 4 + t % LANES * 4);
-    const float f = s_w[p];
-    y.x += f * v.x; y.y += f * v.y; y.z += f * v.z; y.w += f * v.w;
+    for (uint32_t p = t / LANES; p < parts; p += ROWS) {
+      const float4 v = *reinterpret_cast<const float4*>(from + (size_t)p * (DH + 4) + 4 + t % LANES * 4);
+      const float f = s_w[p];
+      y.x += f * v.x; y.y += f * v.y; y.z += f * v.z; y.w += f * v.w;
+    }
   }
   s_o[t] = y;
   __syncthreads();

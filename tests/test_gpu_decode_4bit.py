@@ -79,6 +79,20 @@ def test_long_sequences_in_several_splits(page):
         _attend(rows, _q(4, 4, 8 * 128), 8, max_tokens=most, cache=cache)
 
 
+@pytest.mark.parametrize("n", [65, 130, 256, 257])
+def test_more_blocks_than_run_at_once(n):
+    """Where the longest sequences come first: all lengths, many of them alike, none, unknown numbers, listed again."""
+    g = torch.Generator().manual_seed(n)
+    lens = torch.randint(0, 60, (40,), generator=g).tolist() + [0, 1, 64, 64, 64, 65, 300, 300, 128, 1000]
+    rows = Rows("e2m1", lens, 16, 8, 64, layers=1, seed=n)
+    seqs = torch.randint(0, len(lens), (n,), generator=g).tolist()
+    seqs[3], seqs[n - 1], seqs[n // 2] = -1, len(lens), len(lens) - 1
+    _attend(rows, _q(n, n, 8 * 64), 8, seqs=seqs)
+    _attend(rows, _q(n, n, 8 * 64), 8, seqs=seqs, window=50, sinks=3)
+    everyone = Rows("e2m1", [7] * n, 16, 8, 64, layers=1, seed=1)
+    _attend(everyone, _q(n + 1, n, 16 * 64), 16)
+
+
 def test_pages_that_are_none():
     rows = Rows("e2m1", [100, 64, 40], 16, 2, 64, layers=1, seed=6)
     rows.table[0][2], rows.table[0][6], rows.table[1] = -1, 10 ** 6, [-1] * rows.ld
