@@ -224,14 +224,31 @@ __device__ __forceinline__ uint32_t sm_dpp(uint32_t x) { return (uint32_t)__buil
 template <int CTRL, int ROWS>
 __device__ __forceinline__ uint64_t sm_dpp(uint64_t x) { return (uint64_t)sm_dpp<CTRL, ROWS>((uint32_t)(x >> 32)) << 32 | sm_dpp<CTRL, ROWS>((uint32_t)x); }
 template <typename T>
-__device__ __forceinline__ T sm_scan(T x) {
+__device__ __forceinline__ T sm_row_scan(T x) {
   x += sm_dpp<0x111, 0xF>(x);
   x += sm_dpp<0x112, 0xF>(x);
   x += sm_dpp<0x114, 0xF>(x);
   x += sm_dpp<0x118, 0xF>(x);
+  return x;
+}
+template <typename T>
+__device__ __forceinline__ T sm_scan(T x) {
+  x = sm_row_scan(x);
   x += sm_dpp<0x142, 0xA>(x);
   x += sm_dpp<0x143, 0xC>(x);
   return x;
+}
+// The largest of a wavefront's, in all lanes.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ float sm_dpp_max(float x) { return fmaxf(x, __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(x), __float_as_int(x), CTRL, ROWS, 0xF, false))); }
+__device__ __forceinline__ float sm_max(float x) {
+  x = sm_dpp_max<0x111, 0xF>(x);
+  x = sm_dpp_max<0x112, 0xF>(x);
+  x = sm_dpp_max<0x114, 0xF>(x);
+  x = sm_dpp_max<0x118, 0xF>(x);
+  x = sm_dpp_max<0x142, 0xA>(x);
+  x = sm_dpp_max<0x143, 0xC>(x);
+  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 63));
 }
 __device__ __forceinline__ uint32_t sm_last(uint32_t x) { return (uint32_t)__builtin_amdgcn_readlane((int)x, 63); }
 __device__ __forceinline__ uint64_t sm_lane(uint64_t x, uint32_t l) {
@@ -265,25 +282,20 @@ __device__ __forceinline__ uint32_t sm_count(SampleShared& sh, uint32_t x) {
   x = sm_sum(x);
   if ((threadIdx.x & 63) == 0) sh.some[threadIdx.x >> 6] = x;
   __syncthreads();
-  uint32_t all = 0;
-  for (uint32_t w = 0; w < SM_WAVES; ++w) all += sh.some[w];
+  x = sm_row_scan(sh.some[threadIdx.x & 15]);
   __syncthreads();
-  return all;
+  return (uint32_t)__builtin_amdgcn_readlane((int)x, 15);
 }
 // Inclusive sum over the block's threads; *all: over all of them.
 __device__ __forceinline__ uint64_t sm_block_scan(SampleShared& sh, uint64_t x, uint64_t* all) {
-  const uint32_t wave = threadIdx.x >> 6;
-  uint64_t upto = sm_scan(x), before = 0, total = 0;
+  const uint32_t wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+  const uint64_t upto = sm_scan(x);
   if ((threadIdx.x & 63) == 63) sh.wave[wave] = upto;
   __syncthreads();
-  for (uint32_t w = 0; w < SM_WAVES; ++w) {
-    const uint64_t y = sh.wave[w];
-    before += w < wave ? y : 0;
-    total += y;
-  }
+  const uint64_t waves = sm_row_scan(sh.wave[threadIdx.x & 15]);
   __syncthreads();
-  *all = total;
-  return upto + before;
+  *all = sm_lane(waves, 15);
+  return upto + (wave != 0 ? sm_lane(waves, wave - 1) : 0);
 }
 
 // The bin, from the highest on, at which the running sum of the bins, `above` in front, is asked for (asked_of(sum of all bins)(running sum)); sh.above gets that
@@ -457,25 +469,31 @@ struct Sampler {
     }
     __syncthreads();
   }
-  // A bitonic sort, an entry to a thread: partners in the wavefront exchange by shuffles, others through LDS.
+  // A bitonic sort, an entry to a thread: partners in other wavefronts exchange through LDS, others by shuffles, in the same sixteen by moves within them.
   __device__ __forceinline__ uint64_t sorted_one(uint64_t x) {
     const uint32_t t = threadIdx.x;
 #pragma unroll 1
-    for (uint32_t size = 2; size <= SM_LIST; size <<= 1)
-#pragma unroll 1
-      for (uint32_t by = size >> 1; by > 0; by >>= 1) {
-        uint64_t y;
-        if (by < 64) {
-          y = (uint64_t)(uint32_t)__shfl_xor((uint32_t)(x >> 32), by, 64) << 32 | (uint32_t)__shfl_xor((uint32_t)x, by, 64);
-        } else {
-          sh.weight[t] = x;
-          __syncthreads();
-          y = sh.weight[t ^ by];
-          __syncthreads();
-        }
+    for (uint32_t size = 2; size <= SM_LIST; size <<= 1) {
+      auto take = [&](uint64_t y, uint32_t by) {
         const bool small = ((t & by) == 0) == ((t & size) == 0);
         x = (x < y) == small ? x : y;
+      };
+      auto far = [&](uint32_t by) { return (uint64_t)(uint32_t)__shfl_xor((uint32_t)(x >> 32), by, 64) << 32 | (uint32_t)__shfl_xor((uint32_t)x, by, 64); };
+#pragma unroll 1
+      for (uint32_t by = size >> 1; by >= 64; by >>= 1) {
+        sh.weight[t] = x;
+        __syncthreads();
+        const uint64_t y = sh.weight[t ^ by];
+        __syncthreads();
+        take(y, by);
       }
+      if (size >= 64) take(far(32), 32);
+      if (size >= 32) take(far(16), 16);
+      if (size >= 16) take(sm_dpp<0x128, 0xF>(x), 8);                        // sixteen turned by eight
+      if (size >= 8) take(sm_dpp<0x1B, 0xF>(sm_dpp<0x141, 0xF>(x)), 4);      // 7 - i of eight, then 3 - i of four
+      if (size >= 4) take(sm_dpp<0x4E, 0xF>(x), 2);                          // 2 3 0 1 of four
+      take(sm_dpp<0xB1, 0xF>(x), 1);                                         // 1 0 3 2
+    }
     return x;
   }
   __device__ __forceinline__ uint32_t ranked_key(uint32_t rank) const { return ~(uint32_t)(sh.sorted[rank] >> 32); }
@@ -662,6 +680,10 @@ struct Sampler {
   __device__ __forceinline__ void run() {
     sh.table[threadIdx.x] = ldexp(sm_exp2((double)threadIdx.x * (1.0 / 1024.0)), (int)a.shift);
     for (uint32_t b = threadIdx.x; b < SM_BINS; b += SM_THREADS) sh.bins[b] = 0;      // (for the first histogram; a barrier comes with the largest logit)
+    // (what the temperature gives, while the row is on its way)
+    sc.table = sh.table;
+    sc.steps.per = 1.44269504088896340736 * 1024.0 / (double)temperature;
+    const double near_per = 65504.0 / (double)fmaxf(40.f * temperature, 64.f);
     // the largest logit, and where the first vector with it lies; and this thread's largest
     float mine = -INFINITY;
     uint32_t at = 0xFFFFFFFFu;
@@ -669,10 +691,10 @@ struct Sampler {
       const float x = row.largest(v);
       if (x > mine) { mine = x; at = first; }
     });
-    top = wave_max(mine);
+    top = sm_max(mine);
     if (lane == 0) sh.best[wave] = top;
     __syncthreads();
-    for (uint32_t w = 0; w < SM_WAVES; ++w) top = fmaxf(top, sh.best[w]);
+    top = sm_max(sh.best[lane & 15]);
     if (top == -INFINITY || !(temperature > 0.f)) {
       at = mine == top && top > -INFINITY ? at : 0xFFFFFFFFu;
 #pragma unroll
@@ -699,10 +721,9 @@ struct Sampler {
       mine = mine == INFINITY ? 0.f : -INFINITY;
       top = 0.f;
     }
-    sc.table = sh.table;
-    sc.steps = {(double)top, 1.44269504088896340736 * 1024.0 / (double)temperature};
+    sc.steps.top = (double)top;
     // For counts, logits are divided into steps near the largest one, whatever the temperature.
-    const SampleSteps near = {(double)top, 65504.0 / (double)fmaxf(40.f * temperature, 64.f)};
+    const SampleSteps near = {(double)top, near_per};
     uint32_t least = kKeyNone, equal = 0;
     bool by_k = top_k > 0 && (uint32_t)top_k < row.vocab;
     if (by_k) {
