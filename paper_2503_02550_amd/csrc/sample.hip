@@ -26,7 +26,7 @@
 
 namespace sif {
 
-constexpr uint32_t SM_THREADS = 1024, SM_WAVES = SM_THREADS / 64, SM_BINS = 4096, SM_LIST = 1024, SM_COUNTED = 512;
+constexpr uint32_t SM_THREADS = 1024, SM_WAVES = SM_THREADS / 64, SM_BINS = 4096, SM_LIST = 1024, SM_COUNTED = 384;
 constexpr uint32_t SM_FEW = 512;       // a top-k that the threads' largest bound
 constexpr uint32_t kKeyNone = 0x007FFFFFu;      // of -inf
 
@@ -444,7 +444,7 @@ struct Sampler {
       sh.number[place] = at;
     }
     if (m <= SM_COUNTED) {
-      // Every entry counts those in front of it, a share of the list for each of the threads that it gets.  (One row, top-k 200: 17.4 us so, 22.6 sorted; 500, some 800 listed: 32.2 and 23.3.)
+      // Every entry counts those in front of it, a share of the list for each of the threads that it gets.  (One row, top-k 200: 15.7 us so, 18.7 sorted; 256 rows, 300: 26.2 and 26.8, 400, some 500 listed: 29.1 and 27.0.)
       if (t < m) {
         sh.order[t] = x;
         sh.rank[t] = 0;
@@ -464,16 +464,16 @@ struct Sampler {
       __syncthreads();
       if (t < m) sh.sorted[sh.rank[t]] = x;
     } else {
-      x = sorted_one(x);
+      x = sorted_one(x, m <= SM_LIST / 2 ? SM_LIST / 2 : SM_LIST);
       if (t < m) sh.sorted[t] = x;
     }
     __syncthreads();
   }
-  // A bitonic sort, an entry to a thread: partners in other wavefronts exchange through LDS, others by shuffles, in the same sixteen by moves within them.
-  __device__ __forceinline__ uint64_t sorted_one(uint64_t x) {
+  // A bitonic sort of the first `all` threads' entries (a power of two): partners in other wavefronts exchange through LDS, others by shuffles, in the same sixteen by moves within them.
+  __device__ __forceinline__ uint64_t sorted_one(uint64_t x, uint32_t all) {
     const uint32_t t = threadIdx.x;
 #pragma unroll 1
-    for (uint32_t size = 2; size <= SM_LIST; size <<= 1) {
+    for (uint32_t size = 2; size <= all; size <<= 1) {
       auto take = [&](uint64_t y, uint32_t by) {
         const bool small = ((t & by) == 0) == ((t & size) == 0);
         x = (x < y) == small ? x : y;
@@ -501,7 +501,7 @@ struct Sampler {
   // The token, where the list holds everything that is left (and what the limits leave out).  whole_sum: of all probabilities, where there is no top-k.
   __device__ __forceinline__ void draw_from_list(uint32_t m, bool by_k, uint64_t whole_sum) {
     const uint32_t r = threadIdx.x;
-    const bool alone = m <= 64;                    // one wavefront has them all and waits for nobody (one row, top-k 50: 13.1 -> @D us)
+    const bool alone = m <= 64;                    // one wavefront has them all and waits for nobody (one row, top-k 50: 13.1 -> 11.9 us)
     if (alone && wave != 0) return;
     auto scan = [&](uint64_t x, uint64_t* all) {
       if (!alone) return sm_block_scan(sh, x, all);
