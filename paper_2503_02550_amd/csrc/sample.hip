@@ -268,6 +268,8 @@ struct SampleShared {
   uint64_t order[SM_LIST];            // a listed token's key, turned over, and its number: in this order they are sorted
   uint64_t wave[SM_WAVES];
   uint64_t above;                     // what lies above the bin that was found
+  uint64_t part_sum[SM_WAVES];        // of the row's sixteen parts what is left, their tokens and those that equal the least one
+  uint32_t part_left[SM_WAVES], part_ties[SM_WAVES];
   uint32_t bin, some[SM_WAVES], more[SM_WAVES];
   float best[SM_WAVES];
   uint32_t listed;
@@ -328,6 +330,8 @@ __device__ __forceinline__ void sm_clear(SampleShared& sh) {
 }
 __device__ __forceinline__ void sm_add(SampleShared& sh, uint32_t bin, uint64_t x) { atomicAdd((unsigned long long*)&sh.bins[bin], (unsigned long long)x); }
 
+struct MinP { double mass; float logit; };
+
 template <typename E>
 struct Sampler {
   static constexpr uint32_t N = SampleRow<E>::N, STEP = SampleRow<E>::STEP;
@@ -339,6 +343,7 @@ struct Sampler {
   uint32_t i, wave, lane;
   float temperature, top_p, min_p, random, top;
   int32_t top_k;
+  MinP least;                         // what min-p asks for
 
   template <typename F> __device__ __forceinline__ void each(F&& f) const { row.template walk<false>(f); }
   __device__ __forceinline__ void answer(uint32_t token, float l, uint64_t all, uint32_t kept) const {
@@ -354,7 +359,6 @@ struct Sampler {
 
   // Min-p: what is left has at least this logit, which lies a little below the limit (what is clearly below it needs no exponential), and at least this mass.  A limit below those that
   // masses are told from nothing by is one of the logit alone.
-  struct MinP { double mass; float logit; };
   __device__ __forceinline__ MinP limit() const {
     if (!(min_p > 0.f)) return {0.0, -INFINITY};
     if (min_p >= 0x1p-60f) {
@@ -387,13 +391,41 @@ struct Sampler {
     return sm_value(hi);
   }
 
-  // Lists the tokens with logits from `low` up to below `high`, in no order, and ranks them.  Returns how many there are, more than SM_LIST if they do not fit.
-  __device__ __forceinline__ uint32_t list(float low, float high) {
+  // Adds a vector's tokens with logits from `low` on, and of those what min-p leaves: a lane's sum, a wavefront's number.
+  struct Sums { uint64_t sum = 0; uint32_t left = 0; };
+  __device__ __forceinline__ void weigh(const Vec& v, float low, Sums& to) const {
+    uint64_t in[N], some = 0;
+#pragma unroll
+    for (uint32_t e = 0; e < N; ++e) some |= in[e] = __ballot(v.x[e] >= low);
+    if (some == 0) return;
+    double y[N];                                   // (all of them at once: one by one each would wait for its table entry)
+#pragma unroll
+    for (uint32_t e = 0; e < N; ++e) y[e] = sc.scaled(sc.steps.of(v.x[e] >= low ? v.x[e] : -INFINITY));
+    if (least.mass > 0.0) {
+#pragma unroll
+      for (uint32_t e = 0; e < N; ++e) {
+        in[e] &= __ballot(!(y[e] < least.mass));
+        y[e] = y[e] < least.mass ? 0.0 : y[e];
+      }
+    }
+#pragma unroll
+    for (uint32_t e = 0; e < N; ++e) {
+      to.sum += SampleScale::raw(y[e]);
+      to.left += (uint32_t)__popcll(in[e]);
+    }
+    to.sum -= N * SampleScale::kRaw;
+  }
+
+  // Lists the tokens with logits from `low` up to below `high`, in no order, and ranks them.  Returns how many there are, more than SM_LIST if they do not fit.  WEIGH: and adds up
+  // those from `high` on, by parts of the row.
+  template <bool WEIGH> __device__ __forceinline__ uint32_t list(float low, float high) {
     if (threadIdx.x == 0) sh.listed = 0;
     __syncthreads();
+    Sums above;
     uint32_t listed = 0;                           // by this wavefront, which comes to them in the order of their numbers
     each([&](uint32_t first, const Vec& v) {
       if (!__any(row.largest(v) >= low)) return;   // (of most vectors; NaN is not the largest of numbers)
+      if constexpr (WEIGH) weigh(v, fmaxf(high, least.logit), above);
       uint32_t mine = 0;
 #pragma unroll
       for (uint32_t e = 0; e < N; ++e) mine |= v.x[e] >= low && v.x[e] < high ? 1u << e : 0u;
@@ -415,6 +447,14 @@ struct Sampler {
       }
       listed += n;
     });
+    if constexpr (WEIGH) {
+      const uint64_t sum = sm_scan(above.sum);
+      if (lane == 63) {
+        sh.part_sum[wave] = sum;
+        sh.part_left[wave] = above.left;
+        sh.part_ties[wave] = 0;
+      }
+    }
     if (lane == 0) sh.some[wave] = listed;
     __syncthreads();
     const uint32_t m = sh.listed;
@@ -517,8 +557,7 @@ struct Sampler {
       const uint64_t upto = scan(left ? mass : 0, &all);
       left = left && (double)(upto - mass) < share(by_k ? all : whole_sum);
     }
-    const MinP min = limit();
-    left = left && !(y < min.mass) && sm_value(ranked_key(r)) >= min.logit;
+    left = left && !(y < least.mass) && sm_value(ranked_key(r)) >= least.logit;
     if (r < m) {
       const uint32_t place = (uint32_t)sh.sorted[r];
       sh.weight[place] = left ? mass : 0;
@@ -580,66 +619,63 @@ struct Sampler {
     }
   }
 
-  // The token, by walking the row: logits above that of `least` are left, and the first `equal` of those that are equal to it.  The sums of sixteen pieces say on which one the
-  // random number falls, this one's sixteen pieces go on, down to a vector for a lane.  The equal ones weigh all the same, so pieces only count them.
-  __device__ __forceinline__ void draw_from_row(uint32_t least, uint32_t equal) {
-    const float bound = sm_value(least);
-    const MinP min = limit();
-    const double least_mass = min.mass, tie = sc.scaled(sc.steps.of(bound));
-    if (tie < least_mass || bound < min.logit) equal = 0;
+  // The token, by walking the row: logits above that of `key` are left, and the first `equal` of those that are equal to it.  The sums of sixteen pieces say on which one the
+  // random number falls, this one's sixteen pieces go on, down to a vector for a lane.  The equal ones weigh all the same, so pieces only count them.  GIVEN: the first sums are there, the equal ones in them.
+  template <bool GIVEN> __device__ __forceinline__ void draw_from_row(uint32_t key, uint32_t equal) {
+    const float bound = sm_value(key);
+    const double tie = sc.scaled(sc.steps.of(bound));
+    if (tie < least.mass || bound < least.logit) equal = 0;
     const uint64_t tie_mass = SampleScale::whole(tie);
-    const float low = fmaxf(sm_value(least + 1), min.logit);
+    const float low = fmaxf(sm_value(key + 1), least.logit);
     uint32_t lo = 0, hi = row.vocab, ties_before = 0, kept = 0, piece = 0;
     uint64_t before = 0, all = 0;
     double target = 0.0;
     for (bool whole = true;; whole = false) {
       const uint32_t per = ((hi - lo + SM_WAVES - 1) / SM_WAVES + STEP - 1) / STEP * STEP, first = lo + wave * per, end = std::min(first + per, hi);
-      uint64_t sum = 0;
-      uint32_t left = 0, ties = 0;                 // of the wavefront
-      auto weigh = [&](uint32_t, const Vec& v) {
-        uint64_t in[N], some = 0;
-#pragma unroll
-        for (uint32_t e = 0; e < N; ++e) some |= in[e] = __ballot(v.x[e] >= low);
-        if (equal != 0) {
-#pragma unroll
-          for (uint32_t e = 0; e < N; ++e) ties += (uint32_t)__popcll(__ballot(v.x[e] == bound));
+      const bool mine = lane < SM_WAVES, given = GIVEN && whole;      // a piece to a lane
+      uint32_t equals = 0, more = 0, seen;
+      uint64_t here = 0;
+      if (given) {
+        if (mine) {
+          here = sh.part_sum[lane];
+          equals = sh.part_ties[lane];
+          more = sh.part_left[lane];
         }
-        if (some == 0) return;
-        double y[N];                               // (all of them at once: one by one each would wait for its table entry)
+        seen = sm_scan(equals) - equals;
+      } else {
+        Sums sums;
+        uint32_t ties = 0;
+        auto add = [&](uint32_t, const Vec& v) {
+          if (equal != 0) {
 #pragma unroll
-        for (uint32_t e = 0; e < N; ++e) y[e] = sc.scaled(sc.steps.of(v.x[e] >= low ? v.x[e] : -INFINITY));
-        if (least_mass > 0.0) {
-#pragma unroll
-          for (uint32_t e = 0; e < N; ++e) {
-            in[e] &= __ballot(!(y[e] < least_mass));
-            y[e] = y[e] < least_mass ? 0.0 : y[e];
+            for (uint32_t e = 0; e < N; ++e) ties += (uint32_t)__popcll(__ballot(v.x[e] == bound));
           }
+          weigh(v, low, sums);
+        };
+        if (!GIVEN && whole) each(add); else row.again(first, end, piece, add);
+        const uint64_t sum = sm_scan(sums.sum);
+        if (lane == 63) {
+          sh.wave[wave] = sum;
+          sh.some[wave] = ties;
+          sh.more[wave] = sums.left;
         }
-#pragma unroll
-        for (uint32_t e = 0; e < N; ++e) {
-          sum += SampleScale::raw(y[e]);
-          left += (uint32_t)__popcll(in[e]);
+        __syncthreads();
+        if (mine) {
+          equals = sh.some[lane];
+          more = sh.more[lane];
         }
-        sum -= N * SampleScale::kRaw;
-      };
-      if (whole) each(weigh); else row.again(first, end, piece, weigh);
-      sum = sm_scan(sum);
-      if (lane == 63) {
-        sh.wave[wave] = sum;
-        sh.some[wave] = ties;
-        sh.more[wave] = left;
+        seen = ties_before + sm_scan(equals) - equals;
+        const uint32_t left = std::min(equals, equal - std::min(equal, seen));
+        if (mine) here = sh.wave[lane] + tie_mass * left;
+        more += left;
       }
-      __syncthreads();
-      // the first piece at whose end the sum exceeds the target, a piece to a lane
-      const bool mine = lane < SM_WAVES;
-      const uint32_t equals = mine ? sh.some[lane] : 0, seen = ties_before + sm_scan(equals) - equals;
-      const uint64_t here = mine ? sh.wave[lane] + tie_mass * std::min(equals, equal - std::min(equal, seen)) : 0, upto = before + sm_scan(here);
+      const uint64_t upto = before + sm_scan(here);
       if (whole) {
         all = sm_lane(upto, 63);
-        kept = sm_sum(mine ? sh.more[lane] : 0) + std::min(equal, (uint32_t)__builtin_amdgcn_readlane((int)(seen + equals), 63));
+        kept = sm_sum(more);
         target = goal(all);
       }
-      const uint64_t beyond = __ballot(mine && (double)upto > target);
+      const uint64_t beyond = __ballot(mine && (double)upto > target);      // the first piece at whose end the sum exceeds the target
       const uint32_t won = beyond != 0 ? (uint32_t)__ffsll((unsigned long long)beyond) - 1 : SM_WAVES - 1;
       before = sm_lane(upto - here, won);
       ties_before = (uint32_t)__builtin_amdgcn_readlane((int)seen, (int)won);
@@ -647,7 +683,7 @@ struct Sampler {
       lo += won * per;
       hi = std::min(lo + per, hi);
       if (per == STEP) break;
-      __syncthreads();                             // nobody reads this turn's sums any more
+      if (!given) __syncthreads();                 // nobody reads this turn's sums any more
     }
     if (wave != 0) return;
     row.again(lo, hi, piece, [&](uint32_t i, const Vec& v) {
@@ -659,7 +695,7 @@ struct Sampler {
 #pragma unroll
       for (uint32_t e = 0; e < N; ++e) {
         const double y = sc.scaled(sc.steps.of(v.x[e]));
-        x[e] = v.x[e] >= low && !(y < least_mass) ? SampleScale::whole(y) : 0;
+        x[e] = v.x[e] >= low && !(y < least.mass) ? SampleScale::whole(y) : 0;
         if (v.x[e] == bound && rank++ < equal) x[e] = tie_mass;
         sum += x[e];
       }
@@ -722,9 +758,10 @@ struct Sampler {
       top = 0.f;
     }
     sc.steps.top = (double)top;
+    least = limit();
     // For counts, logits are divided into steps near the largest one, whatever the temperature.
     const SampleSteps near = {(double)top, near_per};
-    uint32_t least = kKeyNone, equal = 0;
+    uint32_t key = kKeyNone, equal = 0;          // the least logit that is left, and how many of those that equal it
     bool by_k = top_k > 0 && (uint32_t)top_k < row.vocab;
     if (by_k) {
       if ((uint32_t)top_k <= SM_FEW) {
@@ -734,7 +771,7 @@ struct Sampler {
         sm_find(sh, 0, [&](uint64_t) { return [&](uint64_t sum) { return sum >= (uint64_t)top_k; }; });
         // (the bin's lower end, a little below where it is; the first one also holds all that is further away)
         const double end = (double)top + ((double)((int)sh.bin - (int)(SM_BINS - 1)) * 16.0 - 1.0) / near.per;
-        const uint32_t m = list(sh.bin > 1 ? fmaxf((float)(end - fabs(end) * 1e-6), -3.4028235e38f) : -3.4028235e38f, INFINITY);
+        const uint32_t m = list<false>(sh.bin > 1 ? fmaxf((float)(end - fabs(end) * 1e-6), -3.4028235e38f) : -3.4028235e38f, INFINITY);
         if (m <= SM_LIST) return draw_from_list(m, true, 0);
       }
       if ((uint32_t)top_k <= SM_FEW) {
@@ -753,16 +790,16 @@ struct Sampler {
         const uint32_t bin = sh.bin, above = (uint32_t)sh.above, here = (uint32_t)sh.bins[bin];
         const bool whole = above + here <= SM_LIST;
         uint32_t m = SM_LIST + 1;
-        if (whole || here <= SM_LIST) m = list(least_of(near, bin), whole || bin + 1 == SM_BINS ? INFINITY : least_of(near, bin + 1));
+        if (whole || here <= SM_LIST) m = list<false>(least_of(near, bin), whole || bin + 1 == SM_BINS ? INFINITY : least_of(near, bin + 1));
         if (m <= SM_LIST && whole) return draw_from_list(m, true, 0);
         if (m <= SM_LIST) {
           const uint32_t need = (uint32_t)top_k - above;                     // of the listed ones, in their order
-          least = ranked_key(need - 1);
-          equal = sm_count(sh, threadIdx.x < need && ranked_key(threadIdx.x) == least ? 1u : 0u);
+          key = ranked_key(need - 1);
+          equal = sm_count(sh, threadIdx.x < need && ranked_key(threadIdx.x) == key ? 1u : 0u);
         } else {
-          by_bits<false>(least, equal);
+          by_bits<false>(key, equal);
         }
-        if (top_p < 1.f) by_bits<true>(least, equal);
+        if (top_p < 1.f) by_bits<true>(key, equal);
       }
     }
     if (!by_k && top_p < 1.f) {
@@ -787,23 +824,32 @@ struct Sampler {
       const uint64_t above = sh.above;
       const float low = least_of(sc.steps, bin);
       // (they are counted only where that many of the least possible weight would not make up far more than there is)
-      const bool whole = (above + sh.bins[bin]) / (16 * SM_LIST) <= sc.mass(low) && count(low) <= SM_LIST;
-      const uint32_t m = list(low, whole || bin + 1 == SM_BINS ? INFINITY : least_of(sc.steps, bin + 1));
-      if (m <= SM_LIST && whole) return draw_from_list(m, false, all);
+      if ((above + sh.bins[bin]) / (16 * SM_LIST) <= sc.mass(low) && count(low) <= SM_LIST) {
+        list<false>(low, INFINITY);
+        return draw_from_list(sh.listed, false, all);
+      }
+      const uint32_t m = list<true>(low, bin + 1 == SM_BINS ? INFINITY : least_of(sc.steps, bin + 1));
       if (m <= SM_LIST) {
-        const uint32_t r = threadIdx.x, key = r < m ? ranked_key(r) : kKeyNone;
-        const uint64_t mass = r < m ? sc.mass(sm_value(key)) : 0;
+        const uint32_t r = threadIdx.x, k = r < m ? ranked_key(r) : kKeyNone, at = r < m ? sh.number[(uint32_t)sh.sorted[r]] : 0;
+        const double y = r < m ? sc.scaled(sc.steps.of(sm_value(k))) : 0.0;
+        const uint64_t mass = SampleScale::whole(y);
         uint64_t sum;
         const uint64_t upto = above + sm_block_scan(sh, mass, &sum);
         const bool left = r < m && (double)(upto - mass) < target;
         const uint32_t need = sm_count(sh, left ? 1u : 0u);
-        least = ranked_key(need - 1);
-        equal = sm_count(sh, left && key == least ? 1u : 0u);
-      } else {
-        by_bits<true>(least, equal);
+        key = ranked_key(need - 1);
+        equal = sm_count(sh, left && k == key ? 1u : 0u);
+        if (left && !(y < least.mass) && sm_value(k) >= least.logit) {
+          atomicAdd((unsigned long long*)&sh.part_sum[at / row.piece()], (unsigned long long)mass);
+          atomicAdd(&sh.part_left[at / row.piece()], 1u);
+        }
+        if (r < m && k == key) atomicAdd(&sh.part_ties[at / row.piece()], 1u);
+        __syncthreads();
+        return draw_from_row<true>(key, equal);
       }
+      by_bits<true>(key, equal);
     }
-    draw_from_row(least, equal);
+    draw_from_row<false>(key, equal);
   }
 };
 
