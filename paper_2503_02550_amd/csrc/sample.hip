@@ -461,15 +461,6 @@ struct Sampler {
     if (m <= SM_LIST) rank(m);
     return m;
   }
-  // How many tokens have logits from `low` on.
-  __device__ __forceinline__ uint32_t count(float low) {
-    uint32_t n = 0;
-    each([&](uint32_t, const Vec& v) {
-#pragma unroll
-      for (uint32_t e = 0; e < N; ++e) n += (uint32_t)__popcll(__ballot(v.x[e] >= low));
-    });
-    return sm_count(sh, lane == 0 ? n : 0);
-  }
   // Ranks the list, by falling logits and rising numbers.  Beside its logit an entry gets in the place of its number the place among the listed ones' numbers, which is of the same
   // order.  sorted[rank]: the entry; number[place].
   __device__ __forceinline__ void rank(uint32_t m) {
@@ -538,8 +529,8 @@ struct Sampler {
   }
   __device__ __forceinline__ uint32_t ranked_key(uint32_t rank) const { return ~(uint32_t)(sh.sorted[rank] >> 32); }
 
-  // The token, where the list holds everything that is left (and what the limits leave out).  whole_sum: of all probabilities, where there is no top-k.
-  __device__ __forceinline__ void draw_from_list(uint32_t m, bool by_k, uint64_t whole_sum) {
+  // The token, where the list holds all that a top-k leaves (and some that it does not).
+  __device__ __forceinline__ void draw_from_list(uint32_t m) {
     const uint32_t r = threadIdx.x;
     const bool alone = m <= 64;                    // one wavefront has them all and waits for nobody (one row, top-k 50: 13.1 -> 11.9 us)
     if (alone && wave != 0) return;
@@ -551,11 +542,11 @@ struct Sampler {
     };
     const double y = r < m ? sc.scaled(sc.steps.of(sm_value(ranked_key(r)))) : 0.0;
     const uint64_t mass = SampleScale::whole(y);
-    bool left = r < (by_k ? std::min(m, (uint32_t)top_k) : m);
+    bool left = r < std::min(m, (uint32_t)top_k);
     if (top_p < 1.f) {
       uint64_t all;
       const uint64_t upto = scan(left ? mass : 0, &all);
-      left = left && (double)(upto - mass) < share(by_k ? all : whole_sum);
+      left = left && (double)(upto - mass) < share(all);
     }
     left = left && !(y < least.mass) && sm_value(ranked_key(r)) >= least.logit;
     if (r < m) {
@@ -772,7 +763,7 @@ struct Sampler {
         // (the bin's lower end, a little below where it is; the first one also holds all that is further away)
         const double end = (double)top + ((double)((int)sh.bin - (int)(SM_BINS - 1)) * 16.0 - 1.0) / near.per;
         const uint32_t m = list<false>(sh.bin > 1 ? fmaxf((float)(end - fabs(end) * 1e-6), -3.4028235e38f) : -3.4028235e38f, INFINITY);
-        if (m <= SM_LIST) return draw_from_list(m, true, 0);
+        if (m <= SM_LIST) return draw_from_list(m);
       }
       if ((uint32_t)top_k <= SM_FEW) {
         __syncthreads();
@@ -791,7 +782,7 @@ struct Sampler {
         const bool whole = above + here <= SM_LIST;
         uint32_t m = SM_LIST + 1;
         if (whole || here <= SM_LIST) m = list<false>(least_of(near, bin), whole || bin + 1 == SM_BINS ? INFINITY : least_of(near, bin + 1));
-        if (m <= SM_LIST && whole) return draw_from_list(m, true, 0);
+        if (m <= SM_LIST && whole) return draw_from_list(m);
         if (m <= SM_LIST) {
           const uint32_t need = (uint32_t)top_k - above;                     // of the listed ones, in their order
           key = ranked_key(need - 1);
@@ -816,18 +807,13 @@ struct Sampler {
       });
       __syncthreads();
       double target = 0.0;
-      const uint64_t all = sm_find(sh, 0, [&](uint64_t sum) {
+      sm_find(sh, 0, [&](uint64_t sum) {
         target = share(sum);
         return [&](uint64_t x) { return (double)x >= target; };
       });
       const uint32_t bin = sh.bin;
       const uint64_t above = sh.above;
       const float low = least_of(sc.steps, bin);
-      // (they are counted only where that many of the least possible weight would not make up far more than there is)
-      if ((above + sh.bins[bin]) / (16 * SM_LIST) <= sc.mass(low) && count(low) <= SM_LIST) {
-        list<false>(low, INFINITY);
-        return draw_from_list(sh.listed, false, all);
-      }
       const uint32_t m = list<true>(low, bin + 1 == SM_BINS ? INFINITY : least_of(sc.steps, bin + 1));
       if (m <= SM_LIST) {
         const uint32_t r = threadIdx.x, k = r < m ? ranked_key(r) : kKeyNone, at = r < m ? sh.number[(uint32_t)sh.sorted[r]] : 0;
