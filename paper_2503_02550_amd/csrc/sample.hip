@@ -5,15 +5,15 @@
 //   the largest logit (a temperature of 0 ends here);
 //   a bound that what is left must reach: for a top-k of up to 512 that of the k-th largest of the threads' own largest logits, else of a histogram of counts or, for top-p, of
 //     probabilities over equal steps of the logit;
-//   the tokens that reach it, listed in the order of their numbers.  Where they fit (1024), all else happens on that list: a token's rank is how many stand before it, sums
-//     over ranks decide about top-p, sums over the list about the token.  Where only those of the bound's own step fit, the list gives the least logit that is left, and
-//     the row is walked once more.  Where neither fits (many equal logits, logits of one step) the least logit is found from the bits of the logits, eleven at a time.
+//   a list of tokens, up to 1024.  For a top-k all that reach the bound, where they fit: then all else happens on that list, sums over ranks decide about top-p, sums over the list
+//     about the token.  For a top-p, and a top-k of more, only those of the bound's own bin: it gives the least logit that is left.  Where they do not fit (many equal logits) the least logit
+//     is found from the bits of the logits, eleven at a time;
+//   the sums of what is left in sixteen parts of the row (for a top-p they were added up while the bin was listed), which say in which part the token lies, and so on in there.
 // A row is read from memory once; a part of it stays in LDS, later walks find the rest in the L2.
 //
-// What bounds it is not the row's bytes (256 rows of 50304 fp32 logits: 7 of 51 us) but the walks of one CU over its row: 1.2 us for a barrier's phase that looks at nothing, 3 to 4 for a walk that
-// compares, 10 for one that adds a histogram of probabilities, 11 for the sums of what is left (some 25 vector instructions an element, four cycles each, on 1/256 of the chip), 5 more for a
-// list of some hundreds.  One row of 50256 in bf16: greedy 5.3 us, top-k 50 13, top-k 200 17, top-k 900 30, nothing but the temperature 19, top-p 0.9 of which 953 are left 38, 21180 42;
-// 256 rows of 50304 in fp32: 11, 21, 25, 40, 25, 51, 50.
+// What bounds it is not the row's bytes (256 rows of 50304 fp32 logits: 6.5 of 44 us) but the walks of one CU over its row: 3 us for a walk that compares, 10 for one that adds up a histogram of probabilities,
+// 11 for the sums of what is left (some 25 vector instructions an element, four cycles each, on 1/256 of the chip), 15 where it lists as well, 1 to 2 for a phase with barriers. One row of 50256 in bf16:
+// greedy 5.1 us, top-k 50 11, 200 16, 900 26, nothing but the temperature 19, top-p 0.9 of which 953 are left 36, 21180 38; 256 rows of 50304 in fp32: 11, 19, 23, 35, 24, 41, 44.
 //
 // Probabilities w = exp((l - l_max) / T) are compared with shares of their sum, and near a border the last bits decide which token comes out; 50000 of them in fp32 would put
 // one row in a hundred on the wrong token.  So they are taken in 64 bits and added as integers w 2^s, s as large as vocab of them fit into 62 bits (sums
