@@ -44,13 +44,15 @@ __device__ __forceinline__ float kv_round_odd(double x) {
   return __uint_as_float(u);
 }
 
-// The exponent that 32 elements share, from the largest one's bits without the sign (as a double): the smallest e with |x| <= 7 2^e.  255 as a byte: NaN.
+// The exponent that 32 elements share, from the largest one's bits without the sign, of a number that is 2^-up of it: the smallest e with |x| <= 7 2^e.  255 as a byte: NaN.
 struct KvPower { int e; uint32_t byte; };
-__device__ __forceinline__ KvPower kv_power(uint64_t top) {
-  if (top > 0x7FF0000000000000ull) return {0, 255u};
-  if (top == 0x7FF0000000000000ull) return {126, 253u};                                 // an infinity: as the largest number in bf16, 1.99 * 2^127
-  int e = (int)(top >> 52) - 1023 - ((top & 0xFFFFFFFFFFFFFull) <= 0xC000000000000ull ? 2 : 1);
-  e = std::min(std::max(e, -127), 127);                                              // (zero and what is below 2^-1022 too)
+__device__ __forceinline__ KvPower kv_power(uint32_t top, int up) {
+  if (top > 0x7F800000u) return {0, 255u};
+  if (top == 0x7F800000u) return {126, 253u};                                           // an infinity: as the largest number in bf16, 1.99 * 2^127
+  const float x = __uint_as_float(top);
+  int e = __builtin_amdgcn_frexp_expf(x) + up - (__builtin_amdgcn_frexp_mantf(x) <= 0.875f ? 3 : 2);
+  if (top == 0) e = -127;
+  e = std::min(std::max(e, -127), 127);
   return {e, (uint32_t)(e + 127)};
 }
 // eight floats over 2^e as 4-bit codes, the first in the lowest bits; infinities are held at +-6
@@ -70,10 +72,9 @@ __device__ __forceinline__ uint32_t kv_spread4(uint32_t h) {
   h = (h | (h << 8)) & 0x00FF00FFu;
   return (h | (h << 4)) & 0x0F0F0F0Fu;
 }
-__device__ __forceinline__ uint64_t kv_max64(uint64_t a, uint64_t b) { return a > b ? a : b; }
-__device__ __forceinline__ uint64_t kv_xor64(uint64_t x, int lane) {
-  const uint32_t lo = __shfl_xor((uint32_t)x, lane, 64), hi = __shfl_xor((uint32_t)(x >> 32), lane, 64);
-  return (uint64_t)hi << 32 | lo;
+__device__ __forceinline__ uint32_t kv_largest_of_4(uint32_t x) {      // of four neighbouring lanes
+  x = std::max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0xB1, 0xF, 0xF, true));
+  return std::max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x4E, 0xF, 0xF, true));
 }
 typedef uint32_t u32x4_kv __attribute__((ext_vector_type(4)));
 __device__ __forceinline__ uint4 kv_uint4(const u32x4_kv& x) { return make_uint4(x[0], x[1], x[2], x[3]); }
@@ -230,28 +231,25 @@ __global__ __launch_bounds__(256) void kv_append_kernel(RopeView r, KvAppend a) 
         at[0] = kv_e4m3x2(g[0], g[1]) | kv_e4m3x2(g[2], g[3]) << 16;
         at[1] = kv_e4m3x2(g[4], g[5]) | kv_e4m3x2(g[6], g[7]) << 16;
       } else {
-        // the largest of 32: four neighbouring lanes have them (they are all here or none is: they share the row and the head)
+        // The largest of 32: four neighbouring lanes have them (they are all here or none is: they share the row and the head).  7 2^e is even in fp32, so it may be told from what is rounded
+        // to odd; a sixteenth of the key, so that what a turn makes of the largest bf16 numbers stays one.
         float f[8], g[8];
         kv_unpack8(val, g);
-        uint64_t top_k = 0, top_v = 0;
+        uint32_t top_k = 0, top_v = 0;
 #pragma unroll
         for (uint32_t e = 0; e < 8; ++e) {
-          top_k = kv_max64(top_k, (uint64_t)__double_as_longlong((double)y[e]) & 0x7FFFFFFFFFFFFFFFull);
-          top_v = kv_max64(top_v, (uint64_t)__double_as_longlong((double)g[e]) & 0x7FFFFFFFFFFFFFFFull);
-          f[e] = kv_round_odd((double)y[e]);
+          f[e] = kv_round_odd((double)y[e] * 0.0625);
+          top_k = std::max(top_k, __float_as_uint(f[e]) & 0x7FFFFFFFu);
+          top_v = std::max(top_v, __float_as_uint(g[e]) & 0x7FFFFFFFu);
         }
-        top_k = kv_max64(top_k, kv_xor64(top_k, 1));
-        top_k = kv_max64(top_k, kv_xor64(top_k, 2));
-        top_v = kv_max64(top_v, kv_xor64(top_v, 1));
-        top_v = kv_max64(top_v, kv_xor64(top_v, 2));
-        const KvPower pk = kv_power(top_k), pv = kv_power(top_v);
-        *reinterpret_cast<uint32_t*>(to + off * (DH / 2) + ch * 4) = pk.byte == 255u ? 0u : kv_codes8(f, pk.e);
+        const KvPower pk = kv_power(kv_largest_of_4(top_k), 4), pv = kv_power(kv_largest_of_4(top_v), 0);
+        *reinterpret_cast<uint32_t*>(to + off * (DH / 2) + ch * 4) = pk.byte == 255u ? 0u : kv_codes8(f, pk.e - 4);
         unsigned char* tv = c.v + pool + head * head_bytes;
         if (ch % 4 == 0) {
           to[((DH / 2) << c.page_lg) + ((ch / 4) << c.page_lg) + off] = (unsigned char)pk.byte;
           tv[((DH / 2) << c.page_lg) + off * (DH / 32) + ch / 4] = (unsigned char)pv.byte;
         }
-        const uint32_t mine = pv.byte == 255u ? 0u : kv_codes8(g, pv.e), over = __shfl_xor(mine, 2, 64);
+        const uint32_t mine = pv.byte == 255u ? 0u : kv_codes8(g, pv.e), over = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)mine, 0x4E, 0xF, 0xF, true);
         if (ch % 4 < 2) {
           uint32_t* at = reinterpret_cast<uint32_t*>(s_v + (hp * kKvRows + row) * ROW + ch / 4 * 16 + ch % 4 * 8);
           at[0] = kv_spread4(mine & 0xFFFFu) | kv_spread4(over & 0xFFFFu) << 4;
