@@ -5,7 +5,7 @@
 // once, and walks the heads.  Keys go out as the vectors they come in as; values pass through LDS, so that lanes which are neighbours in a page's
 // row of tokens store neighbouring elements.
 //
-// Measured: 24600 rows into 4 bits, 32 heads turned and 8 key heads of 128 written, 531 MB: 128 us, 4.1 TB/s; 33000 rows read back, 171 MB: 43 us, 4.0 TB/s (values leave and come in a byte or two
+// Measured: 24600 rows into 4 bits, 32 heads turned and 8 key heads of 128 written, 531 MB: 122 us, 4.4 TB/s; 33000 rows read back, 171 MB: 40 us, 4.3 TB/s (values leave and come in a byte or two
 // at a time).  A token for each of 128 sequences 7.5 us, for four 4.7, of which the launch is 3: in front of the heads stand the list, the length, the table and the sines, each waiting for
 // the one before.  With the first vectors on their way meanwhile and the lists read sixteen entries at a time appending these 24600 rows took 126.5 us for 129.6, with four heads at a time in place of
 // one reading back 43 for 69.6.
@@ -409,7 +409,9 @@ static sif_status launch_append(const char* who, uint32_t dtype, uint32_t d_head
   uint32_t q_blocks = 0;
   if (a.heads != 0) {
     const uint32_t slots = 16 / (r.half / 8 + a.q_copies);
-    q_blocks = kv_share(tiles, (a.heads + slots - 1) / slots);
+    // (Of four turns and more up to 4096 in all: 16384 rows, 32 query heads and 8 key heads of 64 in bf16 49.5 -> 45.8 us, of 128 83 -> 79; with blocks of two turns 8 query heads of 64 took 20.4 us for 18.4.)
+    const uint32_t groups_q = (a.heads + slots - 1) / slots;
+    q_blocks = std::max(kv_share(tiles, groups_q), std::min(groups_q / 4, (4096 + tiles - 1) / tiles));
   }
   a.tiles_lg = kv_tiles_lg(a.c, a.l);
   const dim3 grid(kv_grid_x(tiles, a.tiles_lg), a.kv_blocks + q_blocks);
