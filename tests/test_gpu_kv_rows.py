@@ -252,6 +252,54 @@ def test_lists_as_long_as_they_may_be(dtype):
         assert torch.equal(out[1][known.to(DEV)], v[known.to(DEV)])
 
 
+@pytest.mark.parametrize("dtype", FORMATS)
+@pytest.mark.parametrize("page", [32, 64, 128, 256])
+def test_long_prompts_in_long_pages(dtype, page):
+    """More rows than eight pages have, in one call and sequence by sequence: the same bytes, and back as they went in."""
+    lens, d, kv, heads = [3001, 1, 0, 1500, 4097], 64, 3, 4
+    per = [-(-m // page) for m in lens]
+    total, ld, rows = sum(per), max(per), sum(lens)
+    order = torch.randperm(total, generator=torch.Generator().manual_seed(page)).int()
+    table, at = torch.full((len(lens), ld), -1, dtype=torch.int32), 0
+    for i, m in enumerate(per):
+        table[i, :m] = order[at:at + m]
+        at += m
+    starts = torch.tensor([0] + lens).cumsum(0).int()
+    q, k, v = (_x(31 + i, rows, w).to(DEV) for i, w in enumerate((heads * d, kv * d, kv * d)))
+    rope, kind = S.rope_plan(32), {"bf16": S.SIF_BF16, "e4m3": S.SIF_E4M3, "e2m1": S.SIF_E2M1}[dtype]
+    got = []
+    for one in (True, False):
+        shape = (1, total, kv, page * d * 17 // 32) if dtype == "e2m1" else None
+        kp, vp = (torch.zeros(shape or x, dtype=torch.bfloat16 if dtype == "bf16" else torch.uint8, device=DEV) for x in ((1, total, kv, page, d), (1, total, kv, d, page)))
+        t = (kp, vp, table.to(DEV), torch.tensor(lens, dtype=torch.int32, device=DEV), torch.ones(total, dtype=torch.int32, device=DEV))
+        cache, out = S.kv_cache(*t, kind, page), torch.zeros_like(q)
+        if one:
+            S.sif_k_kv_append(cache, rope, S.kv_append_args(k, v, len(lens), rows=rows, starts=starts.to(DEV), q=q, q_out=out, heads=heads))
+        else:
+            for i, m in enumerate(lens):
+                a = int(starts[i])
+                if m:
+                    S.sif_k_kv_append(cache, rope, S.kv_append_args(k[a:], v[a:], 1, rows=m, seqs=_i32([i]), starts=_i32([0, m]), q=q[a:], q_out=out[a:], heads=heads))
+        kr, vr = torch.zeros_like(k), torch.zeros_like(v)
+        S.sif_k_kv_read(cache, 0, kr, vr, None, len(lens), starts=starts.to(DEV), rows=rows)
+        torch.cuda.synchronize()
+        got.append((kp, vp, out, kr, vr))
+    assert all(torch.equal(x, y) for x, y in zip(*got))
+    kr, vr = got[0][3:]
+    if dtype == "bf16":
+        assert torch.equal(vr, v)
+    step = {"bf16": 0.0, "e4m3": 2.0 ** -4, "e2m1": 0.25}[dtype]
+    # half a step, relative: of the value in 8 bits (2^-10 below its least power); in 4 bits, where the largest of 32 is m 2^e, 3.5 < m <= 7, half a step is at most 2^e, and only where m > 4,
+    # so a quarter of the largest
+    big = v.cpu().double().abs().view(rows, -1, 32).amax(-1, keepdim=True) if dtype == "e2m1" else v.cpu().double().abs().view(rows, -1, 32)
+    assert torch.all((vr.cpu().double() - v.cpu().double()).view(rows, -1, 32).abs() <= step * big + 2.0 ** -10)
+    pos = torch.cat([torch.arange(m) for m in lens])
+    val, off = turned(k.cpu().double().view(rows, kv, d), pos, frequencies(32), False)
+    big = val.abs().view(rows, -1, 32).amax(-1, keepdim=True) if dtype == "e2m1" else val.abs().view(rows, -1, 32)
+    half = step if dtype != "bf16" else HALF
+    assert torch.all((kr.cpu().double().view_as(val) - val).view(rows, -1, 32).abs() <= half * big + off.view(rows, -1, 32) * 2 + 2.0 ** -10)
+
+
 def test_4_bit_pages_are_copied_whole():
     """Forking, extending, copying and compacting move powers along with what they belong to."""
     rows = Rows("e2m1", [20, 70, 0, 0], 32, 3, 64, layers=2, seed=10, spare=5, wider=2)
