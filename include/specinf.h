@@ -445,7 +445,7 @@ sif_status sif_k_kv_extend(const sif_kv_cache* c, const int32_t* seqs_dev, const
 sif_status sif_k_kv_write(const sif_kv_cache* c, uint32_t layer, const void* k_dev, const void* v_dev, uint32_t ld_k, uint32_t ld_v,
                           const int32_t* seqs_dev, const int32_t* starts_dev, uint32_t n, uint32_t rows, void* stream);
 /* sif_k_kv_write with the rotation on the way: a token's position is its place in its sequence, from 0.  Keys are turned and then written as above, rounded once (to 8 and 4 bits from products in 64 bits: next to
- * a border between two of their values a last bit decides about a whole step); values are written as they are.  With heads > 0 the same rows of q
+ * a border between two of their values a last bit decides about a whole step; to 8 bits what is within 2^-24 of a border counts as on it); values are written as they are.  With heads > 0 the same rows of q
  * are turned into q_out, also those of a sequence that was listed before and of tokens without a page; rows of no sequence stay as they were.  q_out may be q (with the same leading dimension). */
 typedef struct sif_kv_append_args {
   uint32_t struct_size;

@@ -218,6 +218,7 @@ __global__ __launch_bounds__(256) void kv_append_kernel(RopeView r, KvAppend a) 
         uint32_t* at = reinterpret_cast<uint32_t*>(s_v + (hp * kKvRows + row) * ROW + ch * 16);
         at[0] = val.x; at[1] = val.y; at[2] = val.z; at[3] = val.w;
       } else if constexpr (FMT == SIF_E4M3) {
+        // (through fp32: what lies within 2^-24 of a border counts as on it, so the reciprocal's rounding takes no quotient off a border that it is on)
         const double inv = 1.0 / (double)ks;
         float f[8], g[8];
 #pragma unroll
