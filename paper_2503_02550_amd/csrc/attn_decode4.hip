@@ -67,6 +67,9 @@ __device__ __forceinline__ void split_q(const uint4 (&x)[4], uint32_t g, SplitQ&
   lo.power = hi.power - 4;
 }
 
+// With this power and the one above it the numbers 4 and 6 are past the largest in bf16: they would become infinite, and infinite times a zero on the other side is NaN.
+constexpr float kFarPower = 0x1p126f;
+
 template <int DH, bool STREAM>
 __global__ __launch_bounds__(256, 2) void attn_decode4_kernel(DecodeArgs a) {
   constexpr uint32_t TOK = 64, NT = 4, NB = DH / 32, KW = DH / 32, DT = DH / 16;      // tiles of 16 tokens; powers of a token; words of a lane's d
@@ -101,7 +104,7 @@ __global__ __launch_bounds__(256, 2) void attn_decode4_kernel(DecodeArgs a) {
 #pragma unroll
   for (uint32_t d = 0; d < DT; ++d) oacc[d] = floatx4{0.f, 0.f, 0.f, 0.f};
   float m_run = -INFINITY, l_run = 0.f;
-  bf16x8 fq[DH == 64 ? KW : 1];                  // heads of 64
+  bf16x8 fq[KW];                                 // heads of 64
   SplitQ hi, lo;                                 // heads of 128
 
   struct Tile { uint32_t k[NT][KW]; uint4 v[NB]; uint4 kpow; uint32_t vpow, base; bool there; };
@@ -130,24 +133,47 @@ __global__ __launch_bounds__(256, 2) void attn_decode4_kernel(DecodeArgs a) {
   };
   auto use = [&](Tile& t) {
     floatx4 sc[NT];                                        // element e of sc[n]: token 4 e + n of the lane's sixteen
-    for_each(std::make_integer_sequence<int, 4>{}, [&](auto nc) {
-      constexpr int n = decltype(nc)::value;
-      sc[n] = floatx4{0.f, 0.f, 0.f, 0.f};
-      if constexpr (DH == 128) {
+    if constexpr (DH == 128) {
+      for_each(std::make_integer_sequence<int, 4>{}, [&](auto nc) {
+        constexpr int n = decltype(nc)::value;
+        sc[n] = floatx4{0.f, 0.f, 0.f, 0.f};
         const uint32_t kp = (n == 0 ? t.kpow.x : n == 1 ? t.kpow.y : n == 2 ? t.kpow.z : t.kpow.w) >> (8 * (col & 3));
         const intx8 x = {(int)t.k[n][0], (int)t.k[n][1], (int)t.k[n][2], (int)t.k[n][3], 0, 0, 0, 0};
         sc[n] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x, hi.x, sc[n], 4, 0, 0, (int)kp, 0, hi.power);
         sc[n] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x, lo.x, sc[n], 4, 0, 0, (int)kp, 0, lo.power);
-      } else {
-        const uint32_t kp = (n == 0 ? t.kpow.x : n == 1 ? t.kpow.y : n == 2 ? t.kpow.z : t.kpow.w) >> (8 * (col & 3));
-        const float power = e2m1_power(kp & 255u);
+      });
+    } else {
+      auto score = [&](floatx4& to, const uint32_t (&k)[KW], float power) {
 #pragma unroll
-        for (uint32_t j = 0; j < KW; ++j) {
-          const uint32_t w = t.k[n][j];
-          sc[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16(make_uint4(e2m1x2<0>(w, power), e2m1x2<1>(w, power), e2m1x2<2>(w, power), e2m1x2<3>(w, power))), fq[j], sc[n], 0, 0, 0);
+        for (uint32_t j = 0; j < KW; ++j)
+          to = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16(make_uint4(e2m1x2<0>(k[j], power), e2m1x2<1>(k[j], power), e2m1x2<2>(k[j], power), e2m1x2<3>(k[j], power))), fq[j], to, 0, 0, 0);
+      };
+      float power[NT];
+#pragma unroll
+      for (uint32_t n = 0; n < NT; ++n) {
+        power[n] = e2m1_power((n == 0 ? t.kpow.x : n == 1 ? t.kpow.y : n == 2 ? t.kpow.z : t.kpow.w) >> (8 * (col & 3)) & 255u);
+        sc[n] = floatx4{0.f, 0.f, 0.f, 0.f};
+      }
+      if (!__any(fmaxf(fmaxf(power[0], power[1]), fmaxf(power[2], power[3])) >= kFarPower)) {      // (NaN is not the largest of numbers)
+#pragma unroll
+        for (uint32_t n = 0; n < NT; ++n) score(sc[n], t.k[n], power[n]);
+      } else {
+        // such keys at a quarter of themselves, into a sum of their own
+#pragma unroll
+        for (uint32_t n = 0; n < NT; ++n) {
+          uint32_t others[KW], those[KW];
+          floatx4 quarter = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (uint32_t j = 0; j < KW; ++j) {
+            others[j] = power[n] >= kFarPower ? 0u : t.k[n][j];
+            those[j] = power[n] >= kFarPower ? t.k[n][j] : 0u;
+          }
+          score(sc[n], others, power[n]);
+          score(quarter, those, 0.25f * power[n]);
+          sc[n] += 4.f * quarter;
         }
       }
-    });
+    }
     float vp[NB];
 #pragma unroll
     for (uint32_t b = 0; b < NB; ++b) vp[b] = e2m1_power(t.vpow >> (8 * b) & 255u);
