@@ -1,4 +1,4 @@
-"""Attention over a cache in 4 bits where numbers end: held keys past the largest in bf16."""
+"""Attention over a cache in 4 bits where numbers end: held keys past the largest in bf16, queries whose 32 elements differ in their powers."""
 import math
 
 import pytest
@@ -49,3 +49,26 @@ def test_small_queries_and_keys_past_the_largest(d):
     q[:, 1, :32:3], q[:, 3, 32:] = 0.0, 0.0
     _attend(rows, q.flatten(1), 4)
     _attend(rows, q.flatten(1), 4, scale=0.01)
+
+
+@pytest.mark.parametrize("up", [[-126, 20, 0, -60], [90, -126, -100, 3], [3, None, -120, -7], [None, -126, None, 120], [-40, 41, 2, None]], ids=str)
+@pytest.mark.parametrize("d", [64, 128])
+def test_blocks_of_q_of_different_powers(d, up):
+    """Each 32 of q times a power of two, those of the keys by as much smaller, so that every block counts alike in the scores (some of q are zeros); keys past the largest number in bf16 among them."""
+    up = up[:d // 32]
+    g = torch.Generator().manual_seed(d)
+    rows = Rows("e2m1", [70, 1, 200], 32, 2, d, layers=1, seed=4)
+    q = torch.zeros(3, 6, d, dtype=torch.float64)
+    for b, e in enumerate(up):
+        if e is not None:
+            q[:, :, b * 32:b * 32 + 32] = (1 + torch.rand(3, 6, 32, generator=g)) * torch.randint(0, 2, (3, 6, 32), generator=g).mul(2).sub(1) * 2.0 ** e
+        byte = torch.randint(-2, 1, rows.power["k"].shape[:-1], generator=g) + 127 - (0 if e is None else e)
+        rows.power["k"][..., b] = byte.clamp(0, 254).to(torch.uint8)
+    q[:, 1, 5::7] = 0.0
+    q[:, 2, ::3] *= 2.0 ** -10                                         # far below their block's largest
+    q[:, 3, 1::2] *= 2.0 ** -14
+    q[:, 4, 1::2] *= 2.0 ** -16
+    q = q.flatten(1).to(torch.bfloat16)
+    assert bool(q.isfinite().all())
+    _attend(rows, q, 6)
+    _attend(rows, q, 6, scale=0.01)
