@@ -162,25 +162,48 @@ __global__ __launch_bounds__(256, 2) void attn_decode4_kernel(DecodeArgs a) {
       for (uint32_t d = 0; d < DT; ++d) oacc[d] *= alpha;
     }
     m_run = m_new;
-    for_each(std::make_integer_sequence<int, 4>{}, [&](auto nc) {
-      constexpr int n = decltype(nc)::value;               // tokens 4 n .. 4 n + 3
-      uint32_t lo_p[4], hi_p[4];                           // beside d, beside d + 16
-#pragma unroll
-      for (uint32_t e = 0; e < 4; ++e) {
-        const float p = __builtin_amdgcn_exp2f(fmaf(sc[n][e], c2, -m_use));
-        l_run += p;
-        lo_p[e] = pack_bf2(p, 0.f);
-        hi_p[e] = lo_p[e] << 16;
-      }
+    // FAR: of a token and 32 d with such a power a quarter of the values, and four times P.
+    auto weigh = [&](auto with_far) {
+      constexpr bool FAR = decltype(with_far)::value;
+      float times[NB];
 #pragma unroll
       for (uint32_t b = 0; b < NB; ++b) {
-        const uint32_t w = n == 0 ? t.v[b].x : n == 1 ? t.v[b].y : n == 2 ? t.v[b].z : t.v[b].w;
-        const bf16x8 x = as_bf16(make_uint4(e2m1x2<0>(w, of_row<4 * n>(vp[b])), e2m1x2<1>(w, of_row<4 * n + 1>(vp[b])),
-                                            e2m1x2<2>(w, of_row<4 * n + 2>(vp[b])), e2m1x2<3>(w, of_row<4 * n + 3>(vp[b]))));
-        oacc[2 * b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, as_bf16(make_uint4(lo_p[0], lo_p[1], lo_p[2], lo_p[3])), oacc[2 * b], 0, 0, 0);
-        oacc[2 * b + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, as_bf16(make_uint4(hi_p[0], hi_p[1], hi_p[2], hi_p[3])), oacc[2 * b + 1], 0, 0, 0);
+        times[b] = FAR && vp[b] >= kFarPower ? 4.f : 1.f;
+        if constexpr (FAR) vp[b] /= times[b];
       }
-    });
+      for_each(std::make_integer_sequence<int, 4>{}, [&](auto nc) {
+        constexpr int n = decltype(nc)::value;               // tokens 4 n .. 4 n + 3
+        float p[4];
+        uint32_t lo_p[4], hi_p[4];                           // beside d, beside d + 16
+#pragma unroll
+        for (uint32_t e = 0; e < 4; ++e) {
+          p[e] = __builtin_amdgcn_exp2f(fmaf(sc[n][e], c2, -m_use));
+          l_run += p[e];
+          lo_p[e] = pack_bf2(p[e], 0.f);
+          hi_p[e] = lo_p[e] << 16;
+        }
+#pragma unroll
+        for (uint32_t b = 0; b < NB; ++b) {
+          const uint32_t w = n == 0 ? t.v[b].x : n == 1 ? t.v[b].y : n == 2 ? t.v[b].z : t.v[b].w;
+          const bf16x8 x = as_bf16(make_uint4(e2m1x2<0>(w, of_row<4 * n>(vp[b])), e2m1x2<1>(w, of_row<4 * n + 1>(vp[b])),
+                                              e2m1x2<2>(w, of_row<4 * n + 2>(vp[b])), e2m1x2<3>(w, of_row<4 * n + 3>(vp[b]))));
+          if constexpr (FAR) {
+            const float f[4] = {of_row<4 * n>(times[b]), of_row<4 * n + 1>(times[b]), of_row<4 * n + 2>(times[b]), of_row<4 * n + 3>(times[b])};
+#pragma unroll
+            for (uint32_t e = 0; e < 4; ++e) {
+              lo_p[e] = pack_bf2(p[e] * f[e], 0.f);
+              hi_p[e] = lo_p[e] << 16;
+            }
+          }
+          oacc[2 * b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, as_bf16(make_uint4(lo_p[0], lo_p[1], lo_p[2], lo_p[3])), oacc[2 * b], 0, 0, 0);
+          oacc[2 * b + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, as_bf16(make_uint4(hi_p[0], hi_p[1], hi_p[2], hi_p[3])), oacc[2 * b + 1], 0, 0, 0);
+        }
+      });
+    };
+    float most = vp[0];
+#pragma unroll
+    for (uint32_t b = 1; b < NB; ++b) most = fmaxf(most, vp[b]);
+    if (!__any(most >= kFarPower)) weigh(std::false_type{}); else weigh(std::true_type{});
   };
   // Every fourth of the split's steps, the next one's contents on the way, in front of them the page numbers of the one after that.  Behind the last step it is fetched
   // once more: a fetch under a condition would make every step wait for all that is under way.

@@ -1,4 +1,4 @@
-"""Attention over a cache in 4 bits where numbers end: held keys past the largest in bf16, queries whose 32 elements differ in their powers."""
+"""Attention over a cache in 4 bits where numbers end: held values and keys past the largest in bf16, queries whose 32 elements differ in their powers, powers that are NaN."""
 import math
 
 import pytest
@@ -72,3 +72,51 @@ def test_blocks_of_q_of_different_powers(d, up):
     assert bool(q.isfinite().all())
     _attend(rows, q, 6)
     _attend(rows, q, 6, scale=0.01)
+
+
+@pytest.mark.parametrize("heads", [1, 20])
+@pytest.mark.parametrize("page", [16, 128])
+@pytest.mark.parametrize("d", [64, 128])
+def test_values_past_the_largest_leave_other_elements_alone(d, page, heads):
+    """A byte of V is an element and the one sixteen on; what one of them holds is nothing to the other.  Their tokens' scores are far below the largest, so all results are finite."""
+    rows = Rows("e2m1", [70, 9, 300], page, 1, d, layers=1, seed=d)
+    q = _q(1, 1, d).repeat(3, heads)
+    for s, m in enumerate(rows.lens):
+        rows.put("k", 0, s, 5, q[:1, :d].double())                     # the largest score, some sqrt(d)
+        for t, element in ((2, dict(e3=math.inf)), (7, dict(e40=-math.inf, e41=1.0)), (m - 1, dict(e20=MOST, e3=-MOST)), (m // 2, dict(e63=-MOST, e47=MOST))):
+            _put(rows, "k", s, t, d)
+            _put(rows, "v", s, t, d, **element)
+    assert int(rows.power["v"].max()) == 253
+    o, _ = _attend(rows, q, heads)
+    assert not bool(o[:, :heads * d].isnan().any())
+    _attend(rows, q, heads, window=100, sinks=8)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_values_past_the_largest_in_several_splits(d):
+    rows = Rows("e2m1", [9000, 4500], 64, 1, d, layers=1, seed=3)
+    q = _q(2, 1, d).repeat(2, 4)
+    for s, m in enumerate(rows.lens):
+        for t in range(5, m, 64):                                      # the largest score of every step
+            rows.put("k", 0, s, t, q[:1, :d].double())
+        for t in (7, 2100, m - 1):
+            _put(rows, "k", s, t, d)
+            _put(rows, "v", s, t, d, e17=math.inf, e34=-MOST)
+    _attend(rows, q, 4)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_powers_that_are_nan(d):
+    rows = Rows("e2m1", [50, 50, 50], 16, 1, d, layers=1, seed=8)
+    last = d // 32 - 1
+    for x, s in (("k", 0), ("v", 1)):
+        rows.power[x][0, rows.place(s, 20), 0, 4, last] = 255
+    _put(rows, "v", 1, 9, d, e1=MOST)                                  # (on the way that the largest numbers take too)
+    rows.put("k", 0, 1, 9, torch.zeros(1, d, dtype=torch.float64))
+    cache = rows.on(S, DEV)
+    q, o = _q(7, 3, d).to(DEV), torch.empty(3, d, dtype=torch.bfloat16, device=DEV)
+    a = S.attn_decode_args(q, o, 3, 1)
+    S.set_workspace(a, torch.empty(1 << 20, dtype=torch.uint8, device=DEV), 1 << 20)
+    S.sif_k_attn_decode(cache, a)
+    o = o.cpu()
+    assert o[0].isnan().all() and o[1, last * 32:].isnan().all() and not o[1, :last * 32].isnan().any() and not o[2].isnan().any()
