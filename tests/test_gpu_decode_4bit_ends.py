@@ -1,4 +1,5 @@
-"""Attention over a cache in 4 bits where numbers end: held values and keys past the largest in bf16, queries whose 32 elements differ in their powers, powers that are NaN."""
+"""Attention over a cache in 4 bits where numbers end: held values and keys past the largest in bf16, queries whose 32 elements differ in their powers or are not finite, powers
+that are NaN; and launches of more blocks than run at once whose sequences are cut into splits."""
 import math
 
 import pytest
@@ -120,3 +121,55 @@ def test_powers_that_are_nan(d):
     S.sif_k_attn_decode(cache, a)
     o = o.cpu()
     assert o[0].isnan().all() and o[1, last * 32:].isnan().all() and not o[1, :last * 32].isnan().any() and not o[2].isnan().any()
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_queries_that_are_not_finite(d):
+    """They make NaN of their own head's results and of nothing else."""
+    rows = Rows("e2m1", [100, 64, 3], 16, 2, d, layers=1, seed=6)
+    cache, q = rows.on(S, DEV), _q(6, 3, 8 * d)
+    want, lse = _attend(rows, q, 8, cache=cache)
+    bad = {(0, 1): math.nan, (0, 6): math.inf, (1, 0): -math.inf, (2, 7): math.nan}
+    x = q.clone().view(3, 8, d)
+    for (i, h), value in bad.items():
+        x[i, h, 37] = value
+    x, o, got = x.view(3, -1).to(DEV), torch.empty(3, 8 * d, dtype=torch.bfloat16, device=DEV), torch.empty(3, 8, device=DEV)
+    a = S.attn_decode_args(x, o, 3, 8, lse=got)
+    S.set_workspace(a, torch.empty(1 << 20, dtype=torch.uint8, device=DEV), 1 << 20)
+    S.sif_k_attn_decode(cache, a)
+    o = o.view(3, 8, d)
+    for i in range(3):
+        for h in range(8):
+            if (i, h) in bad:
+                assert bool(o[i, h].isnan().all()) and bool(got[i, h].isnan()), (i, h)
+            else:
+                assert torch.equal(o[i, h], want[i, h * d:h * d + d]) and torch.equal(got[i, h], lse[i, h]), (i, h)
+
+
+def test_powers_at_their_ends_with_heads_of_128():
+    """Keys' powers down to 2^-127 and values' up to 2^100: scores of zero, results far from one; one token of the largest numbers that bf16 holds."""
+    rows = Rows("e2m1", [70], 16, 1, 128, layers=1, seed=9)
+    some = lambda seed, lo, hi: torch.randint(lo, hi, rows.power["k"].shape, generator=torch.Generator().manual_seed(seed)).to(torch.uint8)      # noqa: E731
+    rows.power["k"], rows.power["v"] = some(1, 0, 3), some(2, 220, 228)
+    _attend(rows, _q(8, 1, 128), 1)
+    rows.power["k"][:], rows.power["v"] = 127, some(2, 20, 28)
+    _attend(rows, _q(8, 1, 256), 2)
+    one = Rows("e2m1", [1], 16, 1, 128, layers=1, seed=10)
+    one.power["v"][:] = 252
+    _attend(one, _q(9, 1, 256), 2)
+
+
+@pytest.mark.parametrize("n,most", [(65, 0), (65, 20000), (130, 0)])
+def test_more_blocks_than_run_at_once_with_splits(n, most):
+    """Table rows of more than 4096 tokens, so that the plan has two splits or three, most sequences too short for them: their other splits have nothing to do."""
+    g = torch.Generator().manual_seed(n)
+    lens = [5000, 0, 1, 2600] + torch.randint(0, 100, (30,), generator=g).tolist()
+    rows = Rows("e2m1", lens, 16, 8 if n == 65 else 4, 64, layers=1, seed=n)
+    seqs = torch.randint(0, len(lens), (n,), generator=g).tolist()
+    seqs[0], seqs[1], seqs[n // 2], seqs[n - 1] = 0, -1, 3, len(lens)
+    heads = 2 * rows.h
+    cache = rows.on(S, DEV)
+    a = S.attn_decode_args(torch.empty(n, heads * 64, dtype=torch.bfloat16, device=DEV), torch.empty(n, heads * 64, dtype=torch.bfloat16, device=DEV), n, heads, max_tokens=most)
+    splits = S.sif_attn_decode_workspace_bytes(cache, a) // (n * heads * (64 + 4) * 4)
+    assert splits >= 2 and n * rows.h * splits > 512
+    _attend(rows, _q(n, n, heads * 64), heads, seqs=seqs, max_tokens=most, cache=cache)
