@@ -692,6 +692,14 @@ def _rows(t, what):
     return ptr(t)
 
 
+def _holds(t, rows, ld, width, what):
+    """Refuses a tensor that ends in front of the last of so many rows: the library reads and writes that far."""
+    if isinstance(t, _Tensor) and rows > 0:
+        there = t.numel() if t.is_contiguous() else sum((n - 1) * by for n, by in zip(t.shape, t.stride())) + 1
+        if (rows - 1) * ld + width > there:
+            raise SifError(SIF_E_INVAL, f"{what} must hold {rows} rows of {width}, {ld} from one to the next")
+
+
 def _fp32(t, what):
     if isinstance(t, _Tensor) and not (t.dtype is _FP32 and t.is_contiguous()):
         raise SifError(SIF_E_INVAL, f"{what} must be a contiguous float32 tensor")
@@ -793,6 +801,12 @@ def kv_append_args(k, v, n, rows=None, layer=0, seqs=None, starts=None, q=None, 
     a.ld_q, a.ld_q_out, a.ld_k, a.ld_v = _ld(q, ld_q, 0), _ld(q_out, ld_q_out, 0), _ld(k, ld_k, 0), _ld(v, ld_v, 0)
     a.seqs_dev, a.starts_dev = _list(seqs, n, "seqs"), _list(starts, n + 1, "starts")
     a.k_dev, a.v_dev, a.q_dev, a.q_out_dev = _rows(k, "k"), _rows(v, "v"), _rows(q, "q"), _rows(q_out, "q_out")
+    # (the cache says how wide they are, and is not known here: a head has 64 elements at least)
+    _holds(k, a.rows, a.ld_k, 64, "k")
+    _holds(v, a.rows, a.ld_v, 64, "v")
+    if heads > 0:
+        _holds(q, a.rows, a.ld_q, 64 * heads, "q")
+        _holds(q_out, a.rows, a.ld_q_out, 64 * heads, "q_out")
     return a
 
 
@@ -802,8 +816,11 @@ def sif_k_kv_append(c, rope, a, stream=None):
 
 def sif_k_kv_read(c, layer, k, v, seqs, n, starts=None, rows=None, ld_k=None, ld_v=None, stream=None):
     width = c.kv_heads * c.d_head
-    return check(lib.sif_k_kv_read(c, layer, _rows(k, "k"), _rows(v, "v"), _ld(k, ld_k, width), _ld(v, ld_v, width), _list(seqs, n, "seqs"),
-                                   _list(starts, n + 1, "starts"), n, n if rows is None else rows, stream_ptr(stream)))
+    rows, ld_k, ld_v = n if rows is None else rows, _ld(k, ld_k, width), _ld(v, ld_v, width)
+    at_k, at_v = _rows(k, "k"), _rows(v, "v")
+    _holds(k, rows, ld_k, width, "k")
+    _holds(v, rows, ld_v, width, "v")
+    return check(lib.sif_k_kv_read(c, layer, at_k, at_v, ld_k, ld_v, _list(seqs, n, "seqs"), _list(starts, n + 1, "starts"), n, rows, stream_ptr(stream)))
 
 
 def sif_k_kv_fork(c, src, dst, n, status=None, stream=None):
@@ -869,6 +886,11 @@ def rope_args(q, q_out, rows, heads, d_head, k=None, k_out=None, kv_heads=0, pos
     a.ld_q, a.ld_q_out, a.ld_k, a.ld_k_out = _ld(q, ld_q, wq), _ld(q_out, ld_q_out, wq), _ld(k, ld_k, wk), _ld(k_out, ld_k_out, wk)
     a.positions_dev = _list(positions, rows, "positions")
     a.q_dev, a.q_out_dev, a.k_dev, a.k_out_dev = _rows(q, "q"), _rows(q_out, "q_out"), _rows(k, "k"), _rows(k_out, "k_out")
+    _holds(q, rows, a.ld_q, wq, "q")
+    _holds(q_out, rows, a.ld_q_out, wq, "q_out")
+    if kv_heads > 0:
+        _holds(k, rows, a.ld_k, wk, "k")
+        _holds(k_out, rows, a.ld_k_out, wk, "k_out")
     return a
 
 
@@ -888,6 +910,7 @@ def sample_args(logits, token, n, vocab, random=None, temperature=1.0, top_k=0, 
     a = sif_sample_args()
     a.struct_size = C.sizeof(sif_sample_args)
     a.dtype, a.n, a.vocab, a.ld = SIF_F32 if logits.dtype is _FP32 else SIF_BF16, n, vocab, _ld(logits, ld, vocab)
+    _holds(logits, n, a.ld, vocab, "logits")
     for name, x in (("temperature", temperature), ("top_p", top_p), ("min_p", min_p)):
         setattr(a, name + "_dev" if isinstance(x, _Tensor) else name, numbers(x, name) if isinstance(x, _Tensor) else x)
     if isinstance(top_k, _Tensor):

@@ -188,3 +188,35 @@ def test_the_binding_refuses_rows_and_numbers():
             _refused(lambda: S.sample_args(**{**dict(logits=z, token=good, n=4, vocab=128, random=f), name: bad}))
     a = S.sample_args(z.float(), good, 4, 128, random=f, temperature=f, top_k=3, top_p=0.5)
     assert (a.dtype, a.ld, a.top_k, a.top_p, a.temperature_dev) == (S.SIF_F32, 128, 3, 0.5, f.data_ptr())
+
+
+def test_the_binding_refuses_rows_that_are_not_there():
+    """A tensor that ends in front of the last row that a call would read or write."""
+    z, f, good = torch.zeros(4, 128, dtype=torch.bfloat16), torch.zeros(5), _i32(0, 1, 2, 3, 4)
+    wide = torch.zeros(4, 256, dtype=torch.bfloat16)
+    for name in ("q", "q_out", "k", "k_out"):
+        x = {**dict.fromkeys(("q", "q_out", "k", "k_out"), wide), "heads": 4, "kv_heads": 4, "d_head": 64, "seq": 4}
+        S.rope_args(**x, rows=4)
+        S.rope_args(**{**x, name: wide[:, :128], "heads": 2, "kv_heads": 2}, rows=4)
+        S.rope_args(**{**x, name: wide.view(4, 4, 64)}, rows=4)
+        for bad in (wide[:3], wide.view(-1)[:-1], wide.view(4, 4, 64)[:3], wide[:, :128], wide[:0], wide[0]):
+            assert f"{name} must hold 4 rows of 256" in _refused(lambda: S.rope_args(**{**x, name: bad}, rows=4))
+        _refused(lambda: S.rope_args(**x, rows=5))
+    for name in ("k", "v", "q", "q_out"):
+        x = {**dict.fromkeys(("k", "v", "q", "q_out"), z), "heads": 2}
+        S.kv_append_args(**x, n=4)
+        S.kv_append_args(**x, n=2, rows=4)
+        for bad in (z[:3], z[:0], z.view(-1)[:384].view(3, 128)):
+            assert f"{name} must hold 4 rows" in _refused(lambda: S.kv_append_args(**{**x, name: bad}, n=2, rows=4))
+        _refused(lambda: S.kv_append_args(**x, n=5))
+    for bad in (z[:3], z.view(-1)[:-1], z[:, :64], z[:0]):
+        assert "k must hold 4 rows of 128" in _refused(lambda: S.sif_k_kv_read(_cache(), 0, bad, z, None, 4))
+        assert "v must hold 4 rows of 128" in _refused(lambda: S.sif_k_kv_read(_cache(), 0, z, bad, None, 2, starts=_i32(0, 1, 4), rows=4))
+    for x in (z, z.float()):
+        S.sample_args(x, good, 4, 121, random=f)
+        S.sample_args(x[:, :100], good, 4, 100, random=f)
+        for bad in (x[:3], x.view(-1)[:511], x[:, :100], x[:0], x[0]):
+            assert "logits must hold 4 rows of 128" in _refused(lambda: S.sample_args(bad, good, 4, 128, random=f))
+        _refused(lambda: S.sample_args(x, good, 5, 128, random=f))
+        _refused(lambda: S.sample_args(x, good, 4, 129, random=f))
+        _refused(lambda: S.sample_args(x, good, 3, 128, random=f, ld=256))
