@@ -409,7 +409,7 @@ sif_status sif_k_rope(const sif_rope* r, const sif_rope_args* a, void* stream);
  *   values  [d_head / 32][16][token], element 32b + c in the lower half of byte (b, c), 32b + c + 16 in the upper one;    then [token][d_head / 32] bytes
  * Written there, e is the smallest from -127 to 127 with |x| <= 7 2^e for all 32, and each x / 2^e goes to the nearest of the values, from the middle to
  * the one with an even mantissa, so that no element is more than half a step off (-0 stays -0); infinities count as the largest number in bf16 and are held as +-6 2^e, one NaN makes
- * NaN of its 32. */
+ * NaN of its 32.  An element held as 2^128 or more is read back as an infinity; attention takes it as the number that it is, with sums in 32 bits. */
 typedef struct sif_kv_cache {
   uint32_t struct_size;
   uint32_t dtype;                     /* SIF_BF16, SIF_E4M3 or SIF_E2M1                                              */
@@ -446,7 +446,8 @@ sif_status sif_k_kv_write(const sif_kv_cache* c, uint32_t layer, const void* k_d
                           const int32_t* seqs_dev, const int32_t* starts_dev, uint32_t n, uint32_t rows, void* stream);
 /* sif_k_kv_write with the rotation on the way: a token's position is its place in its sequence, from 0.  Keys are turned and then written as above, rounded once (to 8 and 4 bits from products in 64 bits: next to
  * a border between two of their values a last bit decides about a whole step; to 8 bits what is within 2^-24 of a border counts as on it); values are written as they are.  With heads > 0 the same rows of q
- * are turned into q_out, also those of a sequence that was listed before and of tokens without a page; rows of no sequence stay as they were.  q_out may be q (with the same leading dimension). */
+ * are turned into q_out, also those of a sequence that was listed before and of tokens without a page; rows of no sequence, and rows in front of their sequence's first token (more rows than it has tokens), which have no
+ * position, stay as they were.  q_out may be q (with the same leading dimension). */
 typedef struct sif_kv_append_args {
   uint32_t struct_size;
   uint32_t layer, n, rows;            /* as sif_k_kv_write                                                           */
