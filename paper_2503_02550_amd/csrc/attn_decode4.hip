@@ -14,7 +14,7 @@
 // fetch took half a line, 79.5; with V through the caches 4 to 6 us more for sequences of equal length; with three blocks a CU registers spill (151).  One sequence of 262011 tokens: 56 us with the join's 5, 5.6 TB/s.
 // The matrix units also take K's numbers and powers as they lie (16x16x128, numbers of 4 bits by such of 8, q as the sum of two), 73.4 and 53.4 us, but add eight neighbouring products with no more than
 // 13 bits below the largest exponent among them: where elements of q differ by 2^8 and more, scores were off by up to 2^-14.6 of what is added, in bf16 by 2^-23.6.
-// What P loses by its rounding to bf16, 2^-9 of each, is what a bf16 result loses: 0.0020 to 0.0022 in the norm where rounding the exact result gives 0.0016.
+// What P loses by its rounding to bf16, up to 2^-8 of each, is what a bf16 result loses: 0.0021 to 0.0022 in the norm where rounding the exact result gives 0.0016.
 #include <type_traits>
 #include <utility>
 

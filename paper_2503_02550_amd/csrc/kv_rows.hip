@@ -410,7 +410,7 @@ static sif_status launch_append(const char* who, uint32_t dtype, uint32_t d_head
   uint32_t q_blocks = 0;
   if (a.heads != 0) {
     const uint32_t slots = 16 / (r.half / 8 + a.q_copies);
-    // (Of four turns and more up to 4096 in all: 16384 rows, 32 query heads and 8 key heads of 64 in bf16 49.5 -> 45.8 us, of 128 83 -> 79; with blocks of two turns 8 query heads of 64 took 20.4 us for 18.4.)
+    // (Of four turns and more up to 4096 in all: 16384 rows, 32 query heads and 8 key heads of 64 in bf16 49.5 -> 46 us, of 128 83 -> 79; with blocks of two turns 8 query heads of 64 took 20.4 us for 18.4.)
     const uint32_t groups_q = (a.heads + slots - 1) / slots;
     q_blocks = std::max(kv_share(tiles, groups_q), std::min(groups_q / 4, (4096 + tiles - 1) / tiles));
   }
